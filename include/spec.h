@@ -369,6 +369,95 @@ spec_status spec_stream_read(const void* d_buf, size_t bytes, uint32_t* d_sink, 
                              hipStream_t stream);
 spec_status spec_timing_read(spec_ctx* ctx, int32_t kind, int64_t* launches, double* ms, double* bytes);
 
+/* ---- operators without a context ------------------------------------------ */
+
+/* They take device memory of the current device and enqueue on `stream` of that
+ * device without waiting; nothing is allocated, and every call can be captured
+ * into a graph.  A failed call enqueues nothing, and spec_last_error(NULL) gives
+ * its text.  Workspaces are the caller's: 256-byte aligned, of at least the bytes
+ * that the matching _workspace_bytes names, their contents of no matter before a
+ * call and after it.  Calls that may overlap in time (other streams, graphs that
+ * replay together) need workspaces of their own. */
+
+/* A KV cache of one layer whose leading pages are held in 8 bits.  Sequence b's
+ * page i (slots [64 i, 64 i + 64)) is page table[b][i] of the 8-bit pool for i <
+ * packed[b], else of the bf16 pool, which is laid out as a context's own pages.
+ * 8-bit pages hold e4m3 codes (sign, 4 exponent, 3 mantissa bits; no infinity) and
+ * one scale for each page and kv head: the value is scale * code. */
+typedef struct spec_kv8 {
+  int32_t kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t pages8, pages16;   /* pages of the two pools (either may be 0, its pointers then NULL) */
+  void* k8;                  /* [pages8][kv_heads][SPEC_KV_PAGE][head_dim], 16-byte aligned */
+  void* v8;                  /* [pages8][kv_heads][head_dim][SPEC_KV_PAGE] (transposed), 16-byte aligned */
+  float* k_scale;            /* [pages8][kv_heads], positive and finite */
+  float* v_scale;
+  const void* k16;           /* bf16 [pages16][kv_heads][SPEC_KV_PAGE][head_dim], 16-byte aligned */
+  const void* v16;           /* bf16 [pages16][kv_heads][head_dim][SPEC_KV_PAGE] */
+} spec_kv8;
+
+/* Packs the keys (as the cache holds them, after rotation) and values of `rows`
+ * >= 1 tokens into 8-bit pages: rows [64 i, 64 i + 64) into pool page d_pages[i]
+ * (device int32, ceil(rows / 64) entries, no page twice).  k, v: bf16 rows of
+ * [kv_heads][head_dim], 16-byte aligned, row_stride elements apart (a multiple of
+ * 8; the rows may lie in a fused projection).  A page and head's scale is the
+ * smallest power of two s, at least 2^-126, with max |x| <= 448 s over its finite
+ * values (1 if all are zero); codes are x / s to nearest even.  NaN and infinities
+ * become NaN.  Slots past the rows are set to zero.  What a page stands for is
+ * exact in bf16 (but for magnitudes from 248 * 2^120, which round to 2^128).  An entry of d_pages outside the pool is skipped and sets *d_err
+ * (device int32, may be NULL; otherwise left alone) to SPEC_E_INVAL. */
+spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, int64_t row_stride, int32_t rows,
+                          const int32_t* d_pages, int32_t* d_err, hipStream_t stream);
+
+/* Grouped-query attention of a pass's rows over such a cache: row j of sequence b
+ * sees slots [0, n) with n = d_visible[b*rows + j], and for query head h of kv head
+ * h / (q_heads / kv_heads)
+ *   out = sum_s p_s v_s,  p = softmax(scale * q . k_s),  lse = ln sum_s e^(scale * q . k_s).
+ * n = 0: out = 0 and lse = -infinity.  n < 0: no such row; its out and lse are left
+ * as they were.  Slots that a row does not see have no influence on it, whatever
+ * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS.
+ *   d_table      [batch][table_stride] device int32; entries past a sequence's
+ *                visible pages are not read
+ *   d_packed     [batch] device int32
+ *   d_visible    [batch][rows] device int32, at most table_stride * 64
+ *   q, out       bf16, row b*rows + j at (b*rows + j) * stride, [q_heads][head_dim];
+ *                strides are multiples of 8, pointers 16-byte aligned
+ *   d_lse        [batch*rows][q_heads] device float, or NULL
+ *   d_err        device int32 or NULL: set to SPEC_E_INVAL, else left alone, if a
+ *                table entry lay outside its pool or a scale was not positive and
+ *                finite (the page is then taken as not visible), or a row wanted
+ *                more slots than the table has
+ * Sums are formed in 32 bits, in an order fixed by the arguments and lengths. */
+spec_status spec_kv8_attn(const spec_kv8* cache, int32_t batch, int32_t rows, int32_t q_heads, const int32_t* d_table,
+                          int32_t table_stride, const int32_t* d_packed, const int32_t* d_visible, const void* q,
+                          int64_t q_stride, float scale, void* out, int64_t out_stride, float* d_lse, int32_t* d_err,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+spec_status spec_kv8_attn_workspace_bytes(const spec_kv8* cache, int32_t batch, int32_t rows, int32_t q_heads,
+                                          int32_t table_stride, size_t* bytes);
+
+#define SPEC_MAX_TOP 32      /* alternatives of a row */
+#define SPEC_BF16 0          /* element types of logits */
+#define SPEC_F16 1
+#define SPEC_F32 2
+
+/* Scores of rows of logits, such as those a spec_verify hands out, under p =
+ * softmax(row).  logits: `dtype` (SPEC_BF16 / F16 / F32), row r at r * row_stride
+ * elements (>= vocab; any), 1 <= vocab <= 2^20, 1 <= rows <= 65535.
+ *   d_logprob      [rows][n_tokens] float: ln p of the tokens d_tokens
+ *                  [rows][n_tokens] (int32); NaN for an id outside [0, vocab)
+ *   d_entropy      [rows] float: -sum p ln p, or NULL
+ *   d_top_token    [rows][top] int32: the `top` (0..SPEC_MAX_TOP) most probable
+ *                  tokens, most probable first, the lowest index on ties, NaN as
+ *                  -infinity (spec_verify's rule); d_top_logprob [rows][top]: their ln p
+ * Logits of -infinity have p = 0 and ln p = -infinity.  A row with a NaN or
+ * +infinity, or with nothing above -infinity, has no distribution: its log
+ * probabilities and entropy are NaN.  Arrays of no elements may be NULL. */
+spec_status spec_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                          const int32_t* d_tokens, int32_t n_tokens, int32_t top, float* d_logprob, float* d_entropy,
+                          int32_t* d_top_token, float* d_top_logprob, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream);
+spec_status spec_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

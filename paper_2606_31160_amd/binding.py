@@ -30,6 +30,8 @@ SPEC_FLAG_BLOCK_DRAFT = 32
 SPEC_FLAG_COND = 64
 SPEC_FLAG_FULL_DRAFT_ROWS = 128
 SPEC_FLAG_COND_CROSS = 256
+SPEC_MAX_TOP = 32
+SPEC_BF16, SPEC_F16, SPEC_F32 = 0, 1, 2
 STATUS = {0: "SPEC_OK", 1: "SPEC_E_INVAL", 2: "SPEC_E_STATE", 3: "SPEC_E_CAPACITY", 5: "SPEC_E_HIP",
           6: "SPEC_E_NUMERIC"}
 KERNEL_KINDS = {"qkv": 0, "o": 1, "gateup": 2, "down": 3, "lmhead": 4, "attn": 5, "other": 6}
@@ -65,6 +67,12 @@ class spec_seq_init(Structure):
     _fields_ = [("prefix_len", c_int32), ("n_blocks", c_int32), ("blocks", POINTER(spec_vision_block)),
                 ("pending_token", c_int32), ("tgt_k", POINTER(c_void_p)), ("tgt_v", POINTER(c_void_p)),
                 ("drf_k", POINTER(c_void_p)), ("drf_v", POINTER(c_void_p)), ("page_table", POINTER(c_int32))]
+
+
+class spec_kv8(Structure):
+    _fields_ = [("kv_heads", c_int32), ("head_dim", c_int32), ("pages8", c_int32), ("pages16", c_int32),
+                ("k8", c_void_p), ("v8", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("k16", c_void_p),
+                ("v16", c_void_p)]
 
 
 class SpecError(RuntimeError):
@@ -104,6 +112,12 @@ def lib():
             "spec_debug_path": [P, POINTER(c_int32)],
             "spec_debug_attn_pages": [POINTER(spec_config), POINTER(spec_seq_init), POINTER(c_int32)],
             "spec_debug_feature": [P, c_int32, c_int32, c_int32, P],
+            "spec_kv8_pack": [POINTER(spec_kv8), P, P, c_int64, c_int32, P, P, P],
+            "spec_kv8_attn": [POINTER(spec_kv8), c_int32, c_int32, c_int32, P, c_int32, P, P, P, c_int64, c_float, P,
+                              c_int64, P, P, P, c_size_t, P],
+            "spec_kv8_attn_workspace_bytes": [POINTER(spec_kv8), c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)],
+            "spec_logprobs": [P, c_int32, c_int32, c_int32, c_int64, P, c_int32, c_int32, P, P, P, P, P, c_size_t, P],
+            "spec_logprobs_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -240,6 +254,45 @@ def spec_debug_attn_pages(cfg: spec_config, seqs) -> int:
 def spec_stream_read(d_buf: int, nbytes: int, d_sink: int, sink_words: int, stream: int) -> None:
     _check(lib().spec_stream_read(c_void_p(d_buf), nbytes, c_void_p(d_sink), sink_words, c_void_p(stream or None)),
            "spec_stream_read")
+
+
+def kv8(kv_heads: int, head_dim: int, pages8: int, k8: int, v8: int, k_scale: int, v_scale: int, pages16: int = 0,
+        k16: int = 0, v16: int = 0) -> spec_kv8:
+    """The description of a cache whose leading pages are held in 8 bits."""
+    return spec_kv8(kv_heads, head_dim, pages8, pages16, k8, v8, k_scale, v_scale, k16, v16)
+
+
+def spec_kv8_pack(cache: spec_kv8, k: int, v: int, row_stride: int, rows: int, d_pages: int, d_err: int = 0,
+                  stream: int = 0) -> None:
+    _check(lib().spec_kv8_pack(cache, k, v, row_stride, rows, d_pages, d_err, stream), "spec_kv8_pack")
+
+
+def spec_kv8_attn_workspace_bytes(cache: spec_kv8, batch: int, rows: int, q_heads: int, table_stride: int) -> int:
+    n = c_size_t(0)
+    _check(lib().spec_kv8_attn_workspace_bytes(cache, batch, rows, q_heads, table_stride, ctypes.byref(n)),
+           "spec_kv8_attn_workspace_bytes")
+    return n.value
+
+
+def spec_kv8_attn(cache: spec_kv8, batch: int, rows: int, q_heads: int, d_table: int, table_stride: int, d_packed: int,
+                  d_visible: int, q: int, q_stride: int, scale: float, out: int, out_stride: int, d_lse: int = 0,
+                  d_err: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().spec_kv8_attn(cache, batch, rows, q_heads, d_table, table_stride, d_packed, d_visible, q, q_stride,
+                               scale, out, out_stride, d_lse, d_err, workspace, workspace_bytes, stream),
+           "spec_kv8_attn")
+
+
+def spec_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    n = c_size_t(0)
+    _check(lib().spec_logprobs_workspace_bytes(rows, vocab, top, ctypes.byref(n)), "spec_logprobs_workspace_bytes")
+    return n.value
+
+
+def spec_logprobs(logits: int, dtype: int, rows: int, vocab: int, row_stride: int, d_tokens: int, n_tokens: int, top: int,
+                  d_logprob: int, d_entropy: int, d_top_token: int, d_top_logprob: int, workspace: int,
+                  workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().spec_logprobs(logits, dtype, rows, vocab, row_stride, d_tokens, n_tokens, top, d_logprob, d_entropy,
+                               d_top_token, d_top_logprob, workspace, workspace_bytes, stream), "spec_logprobs")
 
 
 def spec_timing(ctx, enable: bool) -> None:

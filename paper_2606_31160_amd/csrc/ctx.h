@@ -240,4 +240,7 @@ int down_splits(int M, int Kd, int ncu);
 int num_cus();
 void init_kernel_attributes();
 
+// The text that spec_last_error(NULL) gives on this thread (runtime.cpp).
+void set_global_error(const std::string& text);
+
 }  // namespace specdec

@@ -1,0 +1,668 @@
+// A KV cache whose leading pages are held in 8 bits: packing a prompt into such
+// pages, and split attention over them.
+//
+// A page holds kAttnChunk = 64 slots of every kv head of one layer, keys
+// [nkv][64][D] and values transposed, [nkv][D][64], as the bf16 pages do, in e4m3
+// (no infinity; largest 448) with one scale per page, kv head and operand:
+//   s = the smallest power of two with max |x| <= 448 s (at least 2^-126; 1 for a page of zeros)
+//   code = e4m3(x / s), to nearest even
+// A power of two costs a floating format nothing but range, and what a code stands
+// for, s e4m3, is a bf16 number: reading a page in bf16 or fp16 rounds nothing.
+#include <hip/hip_ext.h>
+
+#include <algorithm>
+
+#include "device.h"
+#include "kv8.h"
+
+namespace specdec {
+
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------------------
+// Packing: one workgroup of 256 threads per (page, kv head, keys / values).  Keys
+// may be rotated on the way (a context's prompt), rounded to bf16 as the bf16
+// cache would hold them.  Infinities become NaN and count for no scale.  Slots
+// past the rows are zero.
+// ---------------------------------------------------------------------------
+template <int D, bool ROT>
+__global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
+  constexpr int KC = D / 8, U = KC / 4;             // 16-byte chunks of a row; chunks of a thread
+  constexpr int kVs = kAttnChunk + 4;               // LDS row of a value dimension
+  __shared__ float red[4];
+  __shared__ __align__(16) uint8_t vs[D * kVs];
+  const int h = blockIdx.y, s0 = blockIdx.x * kAttnChunk;
+  const bool val = blockIdx.z != 0;
+  const int page = a.to[blockIdx.x];
+  if (page < 0 || page >= a.pages8) {               // workgroup-uniform
+    if (a.err && threadIdx.x == 0) *a.err = SPEC_E_INVAL;
+    return;
+  }
+  const bf16_t* src = val ? a.v : a.k;
+  float x[U][8];
+  float big = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = threadIdx.x + 256 * u, off = i / KC, c = i % KC, s = s0 + off;
+    u32x4 r = ld16(src + (int64_t)min(s, a.rows - 1) * a.stride + (int64_t)h * D + 8 * c);
+    if (s >= a.rows) r = u32x4{0, 0, 0, 0};
+    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    if (ROT && !val && s < a.rows) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int d = 4 * c + k;
+        const float2 t = a.cs[(size_t)a.pos3[a.axis[d] * a.cap + s] * (D / 2) + d];
+        const float e = __uint_as_float(w[k] << 16), o = __uint_as_float(w[k] & 0xffff0000u);
+        w[k] = pack2(e * t.x - o * t.y, e * t.y + o * t.x);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[u][e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+      const float m = fabsf(x[u][e]);
+      big = fmaxf(big, m < INFINITY ? m : 0.f);     // neither infinities nor NaN
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor(big, o));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
+  __syncthreads();
+  big = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  // big = f 2^e with f in [1/2, 1): 448 = 7/8 2^9
+  int e;
+  const float f = frexpf(big, &e);
+  e = big > 0.f ? max(f <= 0.875f ? e - 9 : e - 8, -126) : 0;
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);   // 2^-e, e in [-126, 120]
+  const size_t pg = (size_t)page * a.nkv + h;
+  if (threadIdx.x == 0) (val ? a.vs : a.ks)[pg] = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = threadIdx.x + 256 * u, off = i / KC, c = i % KC;
+    uint32_t code[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float v = x[u][4 * q + k];
+        y[k] = fabsf(v) < INFINITY ? v * inv : NAN;
+      }
+      int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      code[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+    }
+    if (!val) {
+      *reinterpret_cast<u32x2*>(a.k8 + (pg * kAttnChunk + off) * D + 8 * c) = u32x2{code[0], code[1]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) vs[(8 * c + k) * kVs + off] = (uint8_t)(code[k >> 2] >> (8 * (k & 3)));
+    }
+  }
+  if (!val) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < D * 4; i += 256) {
+    const int d = i >> 2, c = i & 3;
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(vs + d * kVs + 16 * c);
+    *reinterpret_cast<u32x4*>(a.v8 + (pg * D + d) * kAttnChunk + 16 * c) = u32x4{r[0], r[1], r[2], r[3]};
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention.  Rows r = j G + g of a kv head (pass row j, query head g of the
+// group) stand against the head's pages in groups of ppw pages; a group's
+// workgroup leaves unnormalised sums, which k_kv8_combine joins.  With running
+// maximum m, sum l and output O of the softmax in log2 units,
+//   m' = max(m, max s),  l' = 2^(m - m') l + sum 2^(s - m'),  O' = 2^(m - m') O + sum 2^(s - m') v.
+// ---------------------------------------------------------------------------
+
+// Slots that row j of sequence b sees; negative: no such row.
+__device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, int b, int j) {
+  if (!a.st) return a.vis[b * a.R + j];
+  const SeqState& s = a.st[b];
+  return j < s.count ? s.base + (j < s.causal ? j + 1 : s.count) : -1;
+}
+
+__device__ __forceinline__ int seq_pages(const Kv8AttnArgs& a, int b) {
+  int end = 0;
+  if (a.st) {
+    const SeqState& s = a.st[b];
+    end = s.count > 0 ? s.base + s.count : 0;
+  } else {
+    for (int j = 0; j < a.R; ++j) end = max(end, a.vis[b * a.R + j]);
+  }
+  return min((end + kAttnChunk - 1) / kAttnChunk, a.stride);
+}
+
+// Groups are numbered sequence by sequence, a sequence's kv head by kv head.
+// Every wave of a workgroup counts them for itself, lane l sequences l, l + 64, ..
+struct Groups {
+  int ppw;
+  int pages[3], first[3];   // of sequence lane + 64 i: pages, number of its first group
+  int total;
+};
+
+__device__ __forceinline__ Groups count_groups(const Kv8AttnArgs& a) {
+  const int lane = threadIdx.x & 63;
+  Groups g;
+  int all = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int b = lane + 64 * i;
+    g.pages[i] = b < a.B ? seq_pages(a, b) : 0;
+    all += g.pages[i];
+  }
+  for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+  g.ppw = a.ppw;
+  if (g.ppw == 0) g.ppw = min(max((int)(((int64_t)all * a.nkv + a.target - 1) / a.target), 1), kKv8MaxPages);
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int n = a.nkv * ((g.pages[i] + g.ppw - 1) / g.ppw);
+    int sum = n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(sum, o);
+      if (lane >= o) sum += x;
+    }
+    g.first[i] = before + sum - n;
+    before += __shfl(sum, 63);
+  }
+  g.total = before;
+  return g;
+}
+
+__device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  const b2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)};
+  return __builtin_bit_cast(u32x4, r);
+}
+__device__ __forceinline__ u32x4 f16_of_e4m3(uint32_t lo, uint32_t hi) {
+  const f16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
+  return __builtin_bit_cast(u32x4, r);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const f16x2 v = {(_Float16)lo, (_Float16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Whether a word holds a NaN code.
+__device__ __forceinline__ bool has_nan8(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
+__device__ __forceinline__ bool not_finite16(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+constexpr int kWaves = 4;
+
+// grid (groups, row blocks / NRB), 4 waves; wave w takes pages w, w + 4, .. of the
+// group for all 16 NRB rows, so that every code is read and converted once.
+//
+// S^T = K Q^T and O^T = V^T P^T by 16x16x32 MFMA, lane (n = lane & 15, g = lane >> 4)
+// holding row n.  Row i of key tile t is key 16 (i >> 2) + 4 t + (i & 3): the 16
+// scores of a lane belong to the consecutive keys 16 g .. 16 g + 15, one 16-byte read
+// of a value row; and a lane's 16 bytes of a key row serve two steps over the head
+// dimension, whose order is the same in Q's operand.
+//   Keys are read as bf16, like Q.  Values and probabilities are read as fp16: an
+// e4m3 code is exact in it, and a probability (at most 1) keeps 11 bits, as a
+// rounding to bf16 would show in the bf16 result.  bf16 pages take their values as
+// they are and each probability as the sum of two bf16 numbers.
+//   O is held in units of the last page's value scale.
+template <int D, int NRB>
+__global__ __launch_bounds__(256) void k_kv8_attn(Kv8AttnArgs a) {
+  constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kWaves;
+  __shared__ f32x4 s_o[2][kWaves][kWaves - 1][ND4][64];
+  __shared__ float s_m[kWaves][NRB * 16], s_l[kWaves][NRB * 16];
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int n16 = lane & 15, g4 = lane >> 4;
+  const Groups gr = count_groups(a);
+  const int id = blockIdx.x;
+  if (id >= gr.total) return;
+  int b = 0, pages = 0, first = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    // the last sequence whose first group is not after this one, of those that have any
+    const uint64_t m = __ballot(gr.pages[i] > 0 && gr.first[i] <= id);
+    if (m) {
+      const int l = 63 - __builtin_clzll(m);
+      b = l + 64 * i;
+      pages = __shfl(gr.pages[i], l);
+      first = __shfl(gr.first[i], l);
+    }
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  pages = __builtin_amdgcn_readfirstlane(pages);
+  const int per = (pages + gr.ppw - 1) / gr.ppw;
+  const int kvh = __builtin_amdgcn_readfirstlane((id - first) / per);
+  const int p0 = __builtin_amdgcn_readfirstlane((id - first) % per * gr.ppw);   // first page
+  const int np = min(gr.ppw, pages - p0);
+  const int packed = min(max(a.packed[b], 0), a.stride);
+  const int n8 = min(max(packed - p0, 0), np);
+
+  // lane l: the group's l-th page and its scales; -1: not to be read
+  int page = -1;
+  float ks = 1.f, vsc = 1.f;
+  if (lane < np) {
+    page = a.table[(size_t)b * a.stride + p0 + lane];
+    const bool in8 = lane < n8;
+    if (page < 0 || page >= (in8 ? a.pages8 : a.pages16)) page = -1;
+    if (in8 && page >= 0) {
+      ks = a.ks[(size_t)page * a.nkv + kvh];
+      vsc = a.vs[(size_t)page * a.nkv + kvh];
+      if (!(ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY)) page = -1;
+    }
+    if (page < 0 && a.err) *a.err = SPEC_E_INVAL;
+  }
+
+  // rows of this workgroup
+  const int rows = a.R * a.G, r0 = blockIdx.y * NRB * 16;
+  int vis[NRB], vmin = INT32_MAX, vmax = 0;
+  u32x4 qf[NRB][2 * KH];
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    const int r = r0 + 16 * rb + n16;
+    const bool in = r < rows;
+    const int j = in ? r / a.G : 0, hq = kvh * a.G + (in ? r % a.G : 0);
+    const int v = in ? row_vis(a, b, j) : -1;
+    if (v > a.stride * kAttnChunk && a.err) *a.err = SPEC_E_INVAL;
+    vis[rb] = v < 0 ? INT32_MAX : v;                // rows that nobody asked for need no mask
+    vmin = min(vmin, vis[rb]);
+    vmax = max(vmax, v);
+    // (a row that is not there reads one that is)
+    const bf16_t* qp = a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)hq * D + 16 * g4;
+#pragma unroll
+    for (int t = 0; t < 2 * KH; ++t) qf[rb][t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+  }
+  for (int o = 8; o > 0; o >>= 1) {
+    vmin = min(vmin, __shfl_xor(vmin, o));
+    vmax = max(vmax, __shfl_xor(vmax, o));
+  }
+  vmin = __builtin_amdgcn_readfirstlane(vmin);
+  vmax = __builtin_amdgcn_readfirstlane(vmax);      // slots that no row of the workgroup sees: from here
+
+  float m[NRB], l[NRB], u = 0.f;                    // u: unit of o
+  f32x4 o[NRB][NDT];
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    m[rb] = -INFINITY;
+    l[rb] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[rb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int p = wave; p < np; p += kWaves) {
+    const int pg = __builtin_amdgcn_readlane(page, p);
+    if (pg < 0) continue;
+    const bool in8 = p < n8;
+    const size_t at = ((size_t)pg * a.nkv + kvh) * kAttnChunk * D;   // element of the page's first key or value
+    const int k0 = (p0 + p) * kAttnChunk;
+    if (k0 >= vmax) continue;
+    const bool full = k0 + kAttnChunk <= vmin;
+    float s[NRB][16];                               // scores, then probabilities, of keys 16 g4 + i
+    float sc = a.scale_log2;
+    const int krow = 16 * (n16 >> 2) + (n16 & 3);   // key of this lane in tile 0
+    if (in8) {
+      sc *= __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), p));
+      const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
+      u32x4 kr[4][KH];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kr[t][h] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * h);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f32x4 acc[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < KH; ++h) {
+          const u32x4 lo = bf16_of_e4m3(kr[t][h].x, kr[t][h].y), hi = bf16_of_e4m3(kr[t][h].z, kr[t][h].w);
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) {
+            acc[rb] = mfma16x16x32(lo, qf[rb][2 * h], acc[rb]);
+            acc[rb] = mfma16x16x32(hi, qf[rb][2 * h + 1], acc[rb]);
+          }
+        }
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
+      }
+    } else {
+      const bf16_t* kp = a.k16 + at + krow * D + 16 * g4;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f32x4 acc[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2 * KH; ++h) {
+          const u32x4 kk = ld16(kp + 4 * t * D + 64 * (h >> 1) + 8 * (h & 1));
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(kk, qf[rb][h], acc[rb]);
+        }
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
+      }
+    }
+    if (!full) {
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (k0 + 16 * g4 + i >= vis[rb]) s[rb][i] = -INFINITY;
+    }
+    // (a scale far below the unit would take o out of range: the probabilities carry it)
+    const float own = in8 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), p)) : 1.f;
+    const float unit = fmaxf(own, u * 0x1p-60f), turn = u / unit;
+    u = unit;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      float pm = s[rb][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) pm = fmaxf(pm, s[rb][i]);
+      pm = fmaxf(pm, __shfl_xor(pm, 16));
+      pm = fmaxf(pm, __shfl_xor(pm, 32));
+      const float mn = fmaxf(m[rb], pm * sc);
+      const float mm = mn == -INFINITY ? 0.f : mn;  // no key seen yet: all probabilities zero
+      const float alpha = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
+      float ls = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[rb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i], sc, -mm));
+        ls += s[rb][i];
+      }
+      l[rb] = l[rb] * alpha + ls;
+      m[rb] = mn;
+      if (own != unit)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[rb][i] *= own / unit;
+      const float f = alpha == 0.f ? 0.f : alpha * turn;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) o[rb][dt] *= f;
+    }
+    const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;   // of this lane's 16 keys
+    bool odd = false;                               // a value that is not finite, where not every row sees the page
+    if (in8) {
+      const uint8_t* vp = a.v8 + at + n16 * kAttnChunk + 16 * g4;
+      u32x4 pb[NRB][2];
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float* q = s[rb] + 8 * e;
+          pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
+        }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        u32x4 vr = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
+        if (!full) {
+          uint32_t w[4] = {vr.x, vr.y, vr.z, vr.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = min(max(valid - 4 * k, 0), 4);
+            w[k] &= c == 4 ? 0xffffffffu : (1u << (8 * c)) - 1;
+            if (has_nan8(w[k])) {
+              odd = true;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (((w[k] >> (8 * e)) & 0x7f) == 0x7f) w[k] &= ~(0xffu << (8 * e));
+            }
+          }
+          vr = u32x4{w[0], w[1], w[2], w[3]};
+        }
+        const u32x4 lo = f16_of_e4m3(vr.x, vr.y), hi = f16_of_e4m3(vr.z, vr.w);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+          o[rb][dt] = mfma_f16(lo, pb[rb][0], o[rb][dt]);
+          o[rb][dt] = mfma_f16(hi, pb[rb][1], o[rb][dt]);
+        }
+      }
+    } else {
+      const bf16_t* vp = a.v16 + at + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        u32x4 ph[NRB], pl[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+          const float* q = s[rb] + 8 * e;
+          uint32_t w[4], x[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            w[k] = pack2(q[2 * k], q[2 * k + 1]);
+            x[k] = pack2(q[2 * k] - __uint_as_float(w[k] << 16), q[2 * k + 1] - __uint_as_float(w[k] & 0xffff0000u));
+          }
+          ph[rb] = u32x4{w[0], w[1], w[2], w[3]};
+          pl[rb] = u32x4{x[0], x[1], x[2], x[3]};
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) {
+          u32x4 vr = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
+          if (!full) {
+            uint32_t w[4] = {vr.x, vr.y, vr.z, vr.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int c = valid - 8 * e - 2 * k;
+              w[k] = c >= 2 ? w[k] : c == 1 ? w[k] & 0xffffu : 0u;
+              if (not_finite16(w[k])) {
+                odd = true;
+                if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+                if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
+              }
+            }
+            vr = u32x4{w[0], w[1], w[2], w[3]};
+          }
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) {
+            o[rb][dt] = mfma16x16x32(vr, ph[rb], o[rb][dt]);
+            o[rb][dt] = mfma16x16x32(vr, pl[rb], o[rb][dt]);
+          }
+        }
+      }
+    }
+    if (!full && __any(odd)) {
+      // The page's values that are not finite were taken as zero above, as zero
+      // probability times one is not zero: only rows that see the slot get them.
+      const int end = min(vmax - k0, kAttnChunk);
+      for (int k = 0; k < end; ++k)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const size_t v = at + (size_t)(16 * dt + 4 * g4 + i) * kAttnChunk + k;
+            const float x = in8 ? ((a.v8[v] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[v]);
+            if (!(fabsf(x) < INFINITY)) {
+#pragma unroll
+              for (int rb = 0; rb < NRB; ++rb)
+                if (k0 + k < vis[rb]) o[rb][dt][i] += x;
+            }
+          }
+    }
+  }
+
+  // Join the four waves' sums: wave w the head dimensions of tiles ND4 w ..
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    l[rb] += __shfl_xor(l[rb], 16);
+    l[rb] += __shfl_xor(l[rb], 32);
+    if (g4 == 0) {
+      s_m[wave][16 * rb + n16] = m[rb];
+      s_l[wave][16 * rb + n16] = l[rb];
+    }
+  }
+  __syncthreads();
+  const int nrb = gridDim.y * NRB;                  // row blocks of the partials
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    float mx[kWaves], M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      mx[w] = s_m[w][16 * rb + n16];
+      M = fmaxf(M, mx[w]);
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      L += mx[w] == -INFINITY ? s_l[w][16 * rb + n16] : __builtin_amdgcn_exp2f(mx[w] - M) * s_l[w][16 * rb + n16];
+    const float f = m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - M);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) o[rb][dt] *= f * u;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (w != wave)
+#pragma unroll
+        for (int d = 0; d < ND4; ++d) s_o[rb & 1][w][(wave - w + kWaves) % kWaves - 1][d][lane] = o[rb][w * ND4 + d];
+    __syncthreads();
+    // (the buffer is written again two blocks on, behind the next barrier)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (w == wave) {
+#pragma unroll
+        for (int d = 0; d < ND4; ++d) {
+          f32x4 v = o[rb][w * ND4 + d];
+#pragma unroll
+          for (int k = 0; k < kWaves - 1; ++k) v += s_o[rb & 1][w][k][d][lane];
+          const size_t tile = ((size_t)id * nrb + blockIdx.y * NRB + rb) * NDT + w * ND4 + d;
+          *reinterpret_cast<f32x4*>(a.part + (tile * 64 + lane) * 4) = v;
+        }
+      }
+    if (wave == 0 && g4 == 0) a.ml[((size_t)id * nrb + blockIdx.y * NRB + rb) * 16 + n16] = make_float2(M, L);
+  }
+}
+
+// Joins the groups of a (sequence, kv head): grid (sequences x kv heads, row
+// blocks, D / 16), 4 waves, wave w groups w, w + 4, ..  A lane holds four columns
+// of one row, as the partials do.
+template <int D>
+__global__ __launch_bounds__(256) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
+  constexpr int NDT = D / 16;
+  __shared__ f32x4 s_o[kWaves][64];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int n16 = lane & 15, g4 = lane >> 4;
+  const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
+  const Groups gr = count_groups(a);
+  int pages = 0, first = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (b >> 6 == i) {
+      pages = __shfl(gr.pages[i], b & 63);
+      first = __shfl(gr.first[i], b & 63);
+    }
+  const int per = (pages + gr.ppw - 1) / gr.ppw;
+  first += kvh * per;
+  float M = -INFINITY, L = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = wave; i < per; i += kWaves) {
+    const size_t blk = (size_t)(first + i) * nrb + rb;
+    const float2 ml = a.ml[blk * 16 + n16];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
+    const float mn = fmaxf(M, ml.x);
+    const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
+    const float f1 = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - mn);
+    o = o * f0 + v * f1;
+    L = L * f0 + ml.y * f1;
+    M = mn;
+  }
+  s_o[wave][lane] = o;
+  if (g4 == 0) {
+    s_m[wave][n16] = M;
+    s_l[wave][n16] = L;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const int r = 16 * rb + n16;
+  if (r >= a.R * a.G) return;
+  const int j = r / a.G, hq = kvh * a.G + r % a.G, vis = row_vis(a, b, j);
+  if (vis < 0) return;                              // no such row: left as it was
+  float mx[kWaves];
+  M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    mx[w] = s_m[w][n16];
+    M = fmaxf(M, mx[w]);
+  }
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  L = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = mx[w] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx[w] - M);
+    o += s_o[w][lane] * f;
+    L += s_l[w][n16] * f;
+  }
+  if (vis == 0) {
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+    o *= 1.f / L;
+  }
+  const int row = b * a.R + j, d = hq * D + 16 * dt + 4 * g4;
+  bf16_t* out = a.out + (a.opk ? (int64_t)xop_at(row, d, a.opk) : (int64_t)row * a.out_stride + d);
+  *reinterpret_cast<u32x2*>(out) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
+  if (a.lse && dt == 0 && g4 == 0)
+    a.lse[(size_t)row * a.nq + hq] = vis == 0 ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+int row_blocks(int rows) { return (rows + 15) / 16; }
+// Row blocks of a workgroup.
+int wg_blocks(int rows) {
+  const int n = row_blocks(rows), y = (n + 3) / 4;
+  return (n + y - 1) / y;
+}
+
+}  // namespace
+
+hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
+  const dim3 grid((a.rows + kAttnChunk - 1) / kAttnChunk, a.nkv, 2);
+  if (a.cs)
+    hipLaunchKernelGGL((D == 128 ? k_kv8_pack<128, true> : k_kv8_pack<64, true>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((D == 128 ? k_kv8_pack<128, false> : k_kv8_pack<64, false>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+int kv8_target_groups(int rows, int ncu) {
+  const int n = row_blocks(rows), y = (n + 3) / 4;
+  return std::max(1, 2 * ncu / y);
+}
+
+int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target) {
+  const int64_t pages = (int64_t)B * nkv * stride, most = ppw ? ppw : kKv8MaxPages;
+  const int64_t fixed = (int64_t)B * nkv * ((stride + most - 1) / most);
+  return ppw ? fixed : std::min(pages, std::max<int64_t>(fixed, (int64_t)target + (int64_t)B * nkv));
+}
+
+static int padded_blocks(int rows) {
+  const int n = row_blocks(rows), w = wg_blocks(rows);
+  return (n + w - 1) / w * w;
+}
+size_t kv8_part_bytes(int64_t groups, int rows, int D) { return (size_t)groups * padded_blocks(rows) * 16 * D * sizeof(float); }
+size_t kv8_ml_bytes(int64_t groups, int rows) { return (size_t)groups * padded_blocks(rows) * 16 * sizeof(float2); }
+
+hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const int rows = a.R * a.G, w = wg_blocks(rows);
+  const dim3 grid((unsigned)groups, padded_blocks(rows) / w);
+  void (*f)(Kv8AttnArgs) = nullptr;
+  if (D == 128)
+    f = w == 1 ? k_kv8_attn<128, 1> : w == 2 ? k_kv8_attn<128, 2> : w == 3 ? k_kv8_attn<128, 3> : k_kv8_attn<128, 4>;
+  else
+    f = w == 1 ? k_kv8_attn<64, 1> : w == 2 ? k_kv8_attn<64, 2> : w == 3 ? k_kv8_attn<64, 3> : k_kv8_attn<64, 4>;
+  hipExtLaunchKernelGGL(f, grid, dim3(256), 0, s, e0, e1, 0, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+  const int rows = a.R * a.G;
+  const dim3 grid(a.B * a.nkv, row_blocks(rows), D / 16);
+  hipExtLaunchKernelGGL((D == 128 ? k_kv8_combine<128> : k_kv8_combine<64>), grid, dim3(256), 0, s, e0, e1, 0, a,
+                        padded_blocks(rows));
+  return hipGetLastError();
+}
+
+}  // namespace specdec

@@ -842,6 +842,8 @@ spec_status guarded(spec_ctx* ctx, F f) {
 
 }  // namespace
 
+void specdec::set_global_error(const std::string& text) { g_init_error = text; }
+
 extern "C" {
 
 int32_t spec_seq_pages(const spec_config* cfg, const spec_seq_init* seq) {
