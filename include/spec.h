@@ -111,6 +111,13 @@ typedef struct spec_dims {
                                       pass of one row per sequence on the tile-packed GEMV, when the
                                       batch is at most 32, a packed weight copy exists and neither
                                       SPEC_FLAG_BLOCK_DRAFT nor SPEC_FLAG_COND is set */
+#define SPEC_FLAG_KV8 512          /* the target's prompt cache in 8 bits: every whole page of a prompt is held
+                                      as spec_kv8_pack packs it (after rotation), the prompt's last slots and
+                                      all later ones in bf16, as spec_kv8_attn reads them.  What a round rolls
+                                      back never enters an 8-bit page, so greedy output stays the same for
+                                      every K.  The target's caches take half the bytes.  Each kind's pages
+                                      lie in a pool of their own, in the order of their page_table numbers.
+                                      The attention-budget readout of the target is not available. */
 #define SPEC_FLAG_DRAFT_MROPE 16   /* the draft rotates with 3D M-RoPE (its own mrope_section and
                                       interleaved, validated as the target's) instead of FlatRoPE: the
                                       comparison arm of the attention-budget readout (Sec. 4.2) */
@@ -287,7 +294,8 @@ spec_status spec_commit(spec_ctx* ctx, int32_t* d_accept_len, int32_t* d_committ
  * Rows a pass does not run (finished sequences, rows past a draft pass's
  * count) are left unchanged.  The armed pass is launched kernel by kernel
  * (no graph replay); the readout then disarms.  d_out = NULL disarms.
- * Any state. */
+ * Any state; the target of a SPEC_FLAG_KV8 context has no readout
+ * (SPEC_E_STATE). */
 spec_status spec_attn_readout(spec_ctx* ctx, int32_t model, int32_t layer, float* d_out);
 
 /* Synchronising: waits for the stream, then reports how many sequences have
@@ -316,7 +324,8 @@ spec_status spec_debug_state(spec_ctx* ctx, int32_t b, int32_t* host_out);
 
 /* Cached keys (which = 0, after rotation) or values (which = 1) of sequence
  * b, model 0 = target / 1 = draft, layer, slots [pos0, pos0+npos) into
- * host_out [npos][kv_heads][head_dim] bf16. */
+ * host_out [npos][kv_heads][head_dim] bf16 (of 8-bit pages the values they
+ * stand for). */
 spec_status spec_debug_kv(spec_ctx* ctx, int32_t b, int32_t model, int32_t layer, int32_t which,
                           int32_t pos0, int32_t npos, void* host_out);
 
@@ -331,7 +340,8 @@ spec_status spec_debug_feature(spec_ctx* ctx, int32_t b, int32_t slot0, int32_t 
 #define SPEC_PATH_PACKED 1
 spec_status spec_debug_path(const spec_ctx* ctx, int32_t* path);
 
-/* Cache pages one attention workgroup takes in every pass of a context opened
+/* Cache pages one attention workgroup takes in every pass (with SPEC_FLAG_KV8,
+ * every target pass) of a context opened
  * with these arguments, into *pages (a pass with an armed readout takes one).
  * Does not synchronise; needs no context. */
 spec_status spec_debug_attn_pages(const spec_config* cfg, const spec_seq_init* seqs /* [batch] */, int32_t* pages);

@@ -30,6 +30,7 @@ SPEC_FLAG_BLOCK_DRAFT = 32
 SPEC_FLAG_COND = 64
 SPEC_FLAG_FULL_DRAFT_ROWS = 128
 SPEC_FLAG_COND_CROSS = 256
+SPEC_FLAG_KV8 = 512
 SPEC_MAX_TOP = 32
 SPEC_BF16, SPEC_F16, SPEC_F32 = 0, 1, 2
 STATUS = {0: "SPEC_OK", 1: "SPEC_E_INVAL", 2: "SPEC_E_STATE", 3: "SPEC_E_CAPACITY", 5: "SPEC_E_HIP",

@@ -74,6 +74,7 @@ struct Model {
   int s_down = 1;                  // k-splits of the down projection
   int s_o = 1;                     // k-splits of the o projection on the batched-row GEMM
   size_t kv_layer = 0;              // elements of one layer's key (or value) cache
+  int32_t* pt = nullptr;            // [B][pps] page of each sequence page in kc / vt (8-bit pages: in k8 / v8)
   // tile-packed weights (sgemv.h) of every layer: q/k/v, o, gate/up pairs, down
   bf16_t* pk = nullptr;
   size_t pk_layer = 0, pk_o = 0, pk_gu = 0, pk_dn = 0;   // elements per layer; offsets inside a layer
@@ -159,6 +160,23 @@ struct Ctx {
   bf16_t* junk_kc = nullptr;
   bf16_t* junk_vt = nullptr;
 
+  // SPEC_FLAG_KV8: the target's whole prompt pages in 8 bits (kv8.h); its kc / vt
+  // hold the later pages only
+  bool kv8 = false;
+  int pool8 = 0, pool16 = 0;         // target pages in 8 bits, and the others
+  std::vector<int32_t> n8;           // [B] pages in 8 bits
+  std::vector<int32_t> kv8_pt_host;  // [B][pps]
+  int32_t* kv8_packed = nullptr;     // [B] the same
+  int32_t* kv8_pt = nullptr;         // [B][pps] the target's page table
+  uint8_t *k8 = nullptr, *v8 = nullptr;   // [layers][pool8][kv_heads][kAttnChunk * head_dim]
+  float *k8s = nullptr, *v8s = nullptr;   // [layers][pool8][kv_heads]
+  size_t kv8_layer = 0;              // bytes of one layer's keys (or values) in 8 bits
+  int kv8_ppw = 1;                   // pages of a group
+  int64_t kv8_groups = 0;
+  size_t kv8_part_bytes = 0, kv8_ml_bytes = 0;
+  float* kv8_part = nullptr;
+  float2* kv8_ml = nullptr;
+
   // host state machine
   enum Phase { READY = 0, DRAFTING = 1, VERIFIED = 2 } phase = READY;
   int dsteps = 0;
@@ -211,6 +229,7 @@ hipError_t launch_hold(Ctx& c, double ms);   // bounded device-side wait (timing
 hipError_t launch_rope_table(Ctx& c);        // fills cs
 hipError_t launch_prefix_kv(Ctx& c, Model& m, int layer, int b, int prefix_len,
                             const bf16_t* k_pre, const bf16_t* v);
+hipError_t launch_prefix_kv8(Ctx& c, int layer, int b, int prefix_len, const bf16_t* k_pre, const bf16_t* v);
 bf16_t* logits_target(const Ctx& c, void* d_logits);   // null if d_logits is
 hipError_t launch_stage_verify(Ctx& c, const int32_t* d_override, bf16_t* logits);
 hipError_t launch_forward(Ctx& c, PassMode mode);   // embed .. accept / draft pick

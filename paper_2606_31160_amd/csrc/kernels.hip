@@ -19,6 +19,7 @@
 #include "ctx.h"
 #include "device.h"
 #include "gemv.h"
+#include "kv8.h"
 #include "sgemv.h"
 
 namespace specdec {
@@ -106,14 +107,15 @@ struct PrefixArgs {
   const float2* cs;      // [cap][D/2]
   const int8_t* axis;    // [D/2]
   int P, nkv, D, cap, flat;
+  int page0;             // first page to fill
 };
 
 template <int D>
 __global__ __launch_bounds__(256) void k_prefix_kv(PrefixArgs a) {
   constexpr int KC = D / 8, kVs = kAttnChunk + 2;   // chunks of a row; LDS row of a value dimension (odd word count)
   __shared__ uint16_t vs[D * kVs];
-  const int h = blockIdx.y, s0 = blockIdx.x * kAttnChunk;
-  const size_t pg = (size_t)a.pt[blockIdx.x] * a.nkv + h;
+  const int h = blockIdx.y, sp = a.page0 + blockIdx.x, s0 = sp * kAttnChunk;
+  const size_t pg = (size_t)a.pt[sp] * a.nkv + h;
   u32x4 kr[KC / 4], vr[KC / 4];
 #pragma unroll
   for (int u = 0; u < KC / 4; ++u) {
@@ -1817,6 +1819,40 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
   bf16_t* kc = m.kc + m.kv_layer * li;
   bf16_t* vt = m.vt + m.kv_layer * li;
   const int G = nq / nkv;
+  if (c.kv8 && &m == &c.tgt) {
+    Kv8AttnArgs p{};
+    p.st = c.st;
+    p.packed = c.kv8_packed;
+    p.table = m.pt;
+    p.stride = c.pps;
+    p.k8 = c.k8 + c.kv8_layer * li;
+    p.v8 = c.v8 + c.kv8_layer * li;
+    p.ks = c.k8s + (size_t)c.pool8 * nkv * li;
+    p.vs = c.v8s + (size_t)c.pool8 * nkv * li;
+    p.k16 = kc;
+    p.v16 = vt;
+    p.pages8 = c.pool8;
+    p.pages16 = c.pool16;
+    p.q = c.q;
+    p.out = c.o;
+    p.q_stride = p.out_stride = (int64_t)nq * D;
+    p.opk = wide_o(c) ? c.Mpad / 16 : 0;
+    p.part = c.kv8_part;
+    p.ml = c.kv8_ml;
+    p.B = c.B;
+    p.R = c.R;
+    p.nq = nq;
+    p.nkv = nkv;
+    p.G = G;
+    p.ppw = c.kv8_ppw;
+    p.scale_log2 = kLog2e / sqrtf((float)D);
+    {
+      Timed t(c, SPEC_KERNEL_ATTN, 0);
+      CK(launch_kv8_attn(p, D, c.kv8_groups, c.stream, t.e0, t.e1));
+    }
+    Timed t2(c, SPEC_KERNEL_OTHER, 0);
+    return launch_kv8_combine(p, D, c.stream, t2.e0, t2.e1);
+  }
   const bool ro = c.ro_out && c.ro_m == &m && c.ro_layer == li;
   const int cross = (c.cross && &m == &c.drf && li == 0) ? 1 : 0;
   // the context's pages per workgroup (attn_pages_per_workgroup); a readout pass
@@ -1827,7 +1863,7 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
   // workgroups of 8 waves, so that each page is staged once for all of them
   const int nw = c.R * G > 64 ? 8 : 4;
   const int rb = (c.R * G + 16 * nw - 1) / (16 * nw);
-  AttnArgs p{c.st, c.q, kc, vt, c.pt, c.op, c.mp, c.lp, nq, nkv, G, c.R, c.B, c.pps, c.attn_chunk, rb,
+  AttnArgs p{c.st, c.q, kc, vt, m.pt, c.op, c.mp, c.lp, nq, nkv, G, c.R, c.B, c.pps, c.attn_chunk, rb,
              kLog2e / sqrtf((float)D), c.cls, c.rp, c.cap, cross, ppw};
   dim3 grid((c.attn_splits + ppw - 1) / ppw, nkv * rb, c.B);
   if (ppw > 1) {   // k_attn_pages numbers the groups that the sequences can have
@@ -1944,7 +1980,7 @@ hipError_t launch_qkv_rm(Ctx& c, Model& m, int li, bf16_t* kc, bf16_t* vt) {
   g.nq = nq;
   g.nkv = nkv;
   g.D = D;
-  g.pt = c.pt;
+  g.pt = m.pt;
   g.pps = c.pps;
   g.pw = pk;
   const int sq = c.gemm_rows ? gemm_qkv_splits_for(g.N, H, M, c.ncu, c.gemm_wide) : 1;
@@ -1958,7 +1994,7 @@ hipError_t launch_qkv_rm(Ctx& c, Model& m, int li, bf16_t* kc, bf16_t* vt) {
       g.xpk = 1;
     }
     CK(gemm_run(c, EPI_STORE, g, SPEC_KERNEL_QKV, gemv_bytes(g.N, H, M, 4.0 * sq)));
-    QkvFinishArgs p{c.st, c.part, sq, M, g.N, c.R, c.Mpad, H, d.rms_eps, c.ss, c.rinv, c.rcs, c.pt,
+    QkvFinishArgs p{c.st, c.part, sq, M, g.N, c.R, c.Mpad, H, d.rms_eps, c.ss, c.rinv, c.rcs, m.pt,
                     nq, nkv, D, c.pps, c.q, kc, vt};
     Timed t(c, SPEC_KERNEL_OTHER, 0);
     hipExtLaunchKernelGGL(k_qkv_finish, dim3((g.N / 2 + 255) / 256, M), dim3(256), 0, S(c), t.e0, t.e1, 0, p);
@@ -2197,7 +2233,7 @@ bool sg_build_jobs(Ctx& c, Model& m, bool draft, bool fill) {
     const bool junk = c.cross && draft && li == 0;
     j[0].kc = junk ? c.junk_kc : (m.kc ? m.kc + m.kv_layer * li : nullptr);
     j[0].vt = junk ? c.junk_vt : (m.vt ? m.vt + m.kv_layer * li : nullptr);
-    j[0].pt = c.pt;
+    j[0].pt = m.pt;
     j[0].pps = c.pps;
     j[0].rcs = c.rcs;
     j[0].nq = nq;
@@ -2328,12 +2364,15 @@ hipError_t launch_zero(Ctx& c, void* p, size_t bytes) {
 hipError_t launch_prefix_kv(Ctx& c, Model& m, int layer, int b, int prefix_len, const bf16_t* k_pre,
                             const bf16_t* v) {
   const spec_dims& d = m.d;
+  const int page0 = c.kv8 && &m == &c.tgt ? prefix_len / kAttnChunk : 0;   // before it: launch_prefix_kv8
+  const int pages = (prefix_len + kAttnChunk - 1) / kAttnChunk - page0;
+  if (pages == 0) return hipSuccess;
   const size_t kvl = m.kv_layer;
   PrefixArgs p{k_pre,
                v,
                m.kc + kvl * layer,
                m.vt + kvl * layer,
-               c.pt + (size_t)b * c.pps,
+               m.pt + (size_t)b * c.pps,
                c.pos3 + (size_t)b * 3 * c.cap,
                c.cs,
                m.axis,
@@ -2341,13 +2380,38 @@ hipError_t launch_prefix_kv(Ctx& c, Model& m, int layer, int b, int prefix_len, 
                d.kv_heads,
                d.head_dim,
                c.cap,
-               m.flat ? 1 : 0};
-  const dim3 grid((prefix_len + kAttnChunk - 1) / kAttnChunk, d.kv_heads);
+               m.flat ? 1 : 0,
+               page0};
+  const dim3 grid(pages, d.kv_heads);
   if (d.head_dim == 128)
     hipLaunchKernelGGL(k_prefix_kv<128>, grid, dim3(256), 0, c.stream, p);
   else
     hipLaunchKernelGGL(k_prefix_kv<64>, grid, dim3(256), 0, c.stream, p);
   return hipGetLastError();
+}
+
+// The target's whole prompt pages, rotated and packed in 8 bits.
+hipError_t launch_prefix_kv8(Ctx& c, int layer, int b, int prefix_len, const bf16_t* k_pre, const bf16_t* v) {
+  const spec_dims& d = c.tgt.d;
+  const int pages = prefix_len / kAttnChunk;
+  if (pages == 0) return hipSuccess;
+  Kv8PackArgs p{};
+  p.k = k_pre;
+  p.v = v;
+  p.stride = (int64_t)d.kv_heads * d.head_dim;
+  p.rows = pages * kAttnChunk;
+  p.nkv = d.kv_heads;
+  p.pages8 = c.pool8;
+  p.to = c.tgt.pt + (size_t)b * c.pps;
+  p.k8 = c.k8 + c.kv8_layer * layer;
+  p.v8 = c.v8 + c.kv8_layer * layer;
+  p.ks = c.k8s + (size_t)c.pool8 * d.kv_heads * layer;
+  p.vs = c.v8s + (size_t)c.pool8 * d.kv_heads * layer;
+  p.cs = c.cs;
+  p.pos3 = c.pos3 + (size_t)b * 3 * c.cap;
+  p.axis = c.tgt.axis;
+  p.cap = c.cap;
+  return launch_kv8_pack(p, d.head_dim, c.stream);
 }
 
 hipError_t launch_rope_table(Ctx& c) {

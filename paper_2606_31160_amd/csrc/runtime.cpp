@@ -15,6 +15,7 @@
 
 #include "ctx.h"
 #include "gemv.h"
+#include "kv8.h"
 #include "sgemv.h"
 
 using namespace specdec;
@@ -29,7 +30,8 @@ thread_local std::string g_init_error;
 
 constexpr size_t kAlign = 256;
 constexpr int32_t kKnownFlags = SPEC_FLAG_NO_GRAPHS | SPEC_FLAG_ROWMAJOR | SPEC_FLAG_BLOCK_DRAFT | SPEC_FLAG_COND |
-                                SPEC_FLAG_DRAFT_MROPE | SPEC_FLAG_FULL_DRAFT_ROWS | SPEC_FLAG_COND_CROSS;
+                                SPEC_FLAG_DRAFT_MROPE | SPEC_FLAG_FULL_DRAFT_ROWS | SPEC_FLAG_COND_CROSS |
+                                SPEC_FLAG_KV8;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -443,6 +445,15 @@ int attn_pages_per_workgroup(const spec_config* cfg, const spec_seq_init* seqs, 
   return ppw;
 }
 
+// Pages of a group of the attention over a cache in 8 bits: as many as leave two
+// groups per CU at the prompts, which, as above, fixes it for every K.
+int kv8_pages_per_group(const spec_config* cfg, const spec_seq_init* seqs, int ncu) {
+  long long pages = 0;
+  for (int b = 0; b < cfg->batch; ++b) pages += seqs[b].prefix_len / kAttnChunk + 1;
+  const long long want = (pages * cfg->target.kv_heads + 2 * ncu - 1) / (2 * ncu);
+  return (int)std::min<long long>(std::max<long long>(want, 1), kKv8MaxPages);
+}
+
 // Carves the workspace (base == nullptr only measures).  Returns total bytes.
 size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has_draft, char* base) {
   const Layout L = make_layout(cfg, seqs);
@@ -491,6 +502,17 @@ size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has
   c.st = cv.take<SeqState>(L.B);
   c.hist = cv.take<int32_t>((size_t)L.B * L.cap);
   c.pt = cv.take<int32_t>((size_t)L.B * L.splits);
+  c.kv8 = (cfg->flags & SPEC_FLAG_KV8) != 0;
+  c.n8.assign(L.B, 0);
+  c.pool8 = 0;
+  if (c.kv8) {
+    for (int b = 0; b < L.B; ++b) c.pool8 += c.n8[b] = seqs[b].prefix_len / kAttnChunk;
+    c.kv8_pt = cv.take<int32_t>((size_t)L.B * L.splits);
+    c.kv8_packed = cv.take<int32_t>(L.B);
+  }
+  c.pool16 = L.pool - c.pool8;
+  c.tgt.pt = c.kv8 ? c.kv8_pt : c.pt;
+  c.drf.pt = c.pt;
   c.pos3 = cv.take<int32_t>((size_t)L.B * 3 * L.cap);
   c.tgt.axis = cv.take<int8_t>(D / 2);
   c.drf.axis = cv.take<int8_t>(D / 2);
@@ -523,9 +545,25 @@ size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has
     c.feat = cv.take<bf16_t>((size_t)L.B * L.cap * H);
     c.cat2 = cv.take<bf16_t>((size_t)L.Mpad * 2 * H);
   }
-  c.tgt.kv_layer = (size_t)L.pool * t.kv_heads * kAttnChunk * D;
+  c.tgt.kv_layer = (size_t)c.pool16 * t.kv_heads * kAttnChunk * D;
   c.tgt.kc = cv.take<bf16_t>(c.tgt.kv_layer * t.layers);
   c.tgt.vt = cv.take<bf16_t>(c.tgt.kv_layer * t.layers);
+  if (c.kv8) {
+    c.kv8_layer = (size_t)c.pool8 * t.kv_heads * kAttnChunk * D;
+    c.k8 = cv.take<uint8_t>(c.kv8_layer * t.layers);
+    c.v8 = cv.take<uint8_t>(c.kv8_layer * t.layers);
+    c.k8s = cv.take<float>((size_t)c.pool8 * t.kv_heads * t.layers);
+    c.v8s = cv.take<float>((size_t)c.pool8 * t.kv_heads * t.layers);
+    c.kv8_ppw = kv8_pages_per_group(cfg, seqs, c.ncu);
+    c.kv8_groups = 0;
+    for (int b = 0; b < L.B; ++b) c.kv8_groups += (seq_pages(cfg, seqs[b]) + c.kv8_ppw - 1) / c.kv8_ppw;
+    c.kv8_groups *= t.kv_heads;
+    const int rows = L.R * (t.q_heads / t.kv_heads);
+    c.kv8_part_bytes = kv8_part_bytes(c.kv8_groups, rows, D);
+    c.kv8_ml_bytes = kv8_ml_bytes(c.kv8_groups, rows);
+    c.kv8_part = reinterpret_cast<float*>(cv.take<char>(c.kv8_part_bytes));
+    c.kv8_ml = reinterpret_cast<float2*>(cv.take<char>(c.kv8_ml_bytes));
+  }
   if (has_draft) {
     c.drf.kv_layer = (size_t)L.pool * cfg->draft.kv_heads * kAttnChunk * D;
     c.drf.kc = cv.take<bf16_t>(c.drf.kv_layer * cfg->draft.layers);
@@ -758,6 +796,7 @@ spec_status run_commit(Ctx& c) {
 // pairs, logits staging).  Offsets are 256-byte aligned.
 struct ScratchPlan {
   size_t op = 0, mp = 0, lp = 0, rp = 0, part = 0, sg_part = 0, sg_cnt = 0, amax_v = 0, amax_i = 0, logits = 0;
+  size_t kv8_part = 0, kv8_ml = 0;
   size_t cnt_bytes = 0;   // counters to clear (a multiple of 16)
   size_t bytes = 0;
 };
@@ -773,10 +812,14 @@ ScratchPlan scratch_plan(const Ctx& c) {
   };
   const int D = c.tgt.d.head_dim;
   const size_t amax = (size_t)(c.V / kTile) * c.Mpad;
-  p.op = take(c.attn_rows * D * sizeof(bf16_t));
-  p.mp = take(c.attn_rows * sizeof(float));
-  p.lp = take(c.attn_rows * sizeof(float));
-  p.rp = take(c.attn_rows * 4 * sizeof(float));
+  // (a verify of a cache in 8 bits has other attention partials)
+  const size_t attn_rows = c.kv8 ? 0 : c.attn_rows;
+  p.op = take(attn_rows * D * sizeof(bf16_t));
+  p.mp = take(attn_rows * sizeof(float));
+  p.lp = take(attn_rows * sizeof(float));
+  p.rp = take(attn_rows * 4 * sizeof(float));
+  p.kv8_part = take(c.kv8_part_bytes);
+  p.kv8_ml = take(c.kv8_ml_bytes);
   p.part = take(c.part_elems * sizeof(float));
   p.sg_part = take(c.sg ? c.sg_part_floats * sizeof(float) : 0);
   p.cnt_bytes = c.sg ? align_up((size_t)(c.sg_units + 1) * sizeof(unsigned), 16) : 0;
@@ -793,17 +836,20 @@ ScratchPlan scratch_plan(const Ctx& c) {
 struct ScratchSwap {
   Ctx& c;
   bf16_t* op;
-  float *mp, *lp, *rp, *part, *sg_part, *amax_v;
+  float *mp, *lp, *rp, *part, *sg_part, *amax_v, *kv8_part;
+  float2* kv8_ml;
   unsigned* sg_cnt;
   int32_t* amax_i;
   bf16_t* logits;
   ScratchSwap(Ctx& ctx, char* base, const ScratchPlan& p)
       : c(ctx), op(ctx.op), mp(ctx.mp), lp(ctx.lp), rp(ctx.rp), part(ctx.part), sg_part(ctx.sg_part),
-        amax_v(ctx.amax_v), sg_cnt(ctx.sg_cnt), amax_i(ctx.amax_i), logits(ctx.logits) {
+        amax_v(ctx.amax_v), kv8_part(ctx.kv8_part), kv8_ml(ctx.kv8_ml), sg_cnt(ctx.sg_cnt), amax_i(ctx.amax_i), logits(ctx.logits) {
     c.op = reinterpret_cast<bf16_t*>(base + p.op);
     c.mp = reinterpret_cast<float*>(base + p.mp);
     c.lp = reinterpret_cast<float*>(base + p.lp);
     c.rp = reinterpret_cast<float*>(base + p.rp);
+    c.kv8_part = reinterpret_cast<float*>(base + p.kv8_part);
+    c.kv8_ml = reinterpret_cast<float2*>(base + p.kv8_ml);
     c.part = reinterpret_cast<float*>(base + p.part);
     c.sg_part = c.sg ? reinterpret_cast<float*>(base + p.sg_part) : nullptr;
     c.sg_cnt = c.sg ? reinterpret_cast<unsigned*>(base + p.sg_cnt) : nullptr;
@@ -816,6 +862,8 @@ struct ScratchSwap {
     c.mp = mp;
     c.lp = lp;
     c.rp = rp;
+    c.kv8_part = kv8_part;
+    c.kv8_ml = kv8_ml;
     c.part = part;
     c.sg_part = sg_part;
     c.sg_cnt = sg_cnt;
@@ -824,6 +872,28 @@ struct ScratchSwap {
     c.logits = logits;
   }
 };
+
+// What a target page in 8 bits stands for, as bf16 (spec_debug_kv).
+hipError_t read_page8(Ctx& c, int layer, int which, size_t page, std::vector<bf16_t>& out) {
+  const size_t nkv = c.tgt.d.kv_heads, each = (size_t)kAttnChunk * c.tgt.d.head_dim;
+  std::vector<uint8_t> code(nkv * each);
+  std::vector<float> scale(nkv);
+  hipError_t e = hipMemcpy(code.data(), (which == 0 ? c.k8 : c.v8) + c.kv8_layer * layer + page * code.size(), code.size(),
+                           hipMemcpyDeviceToHost);
+  if (e == hipSuccess)
+    e = hipMemcpy(scale.data(), (which == 0 ? c.k8s : c.v8s) + ((size_t)c.pool8 * layer + page) * nkv, nkv * sizeof(float),
+                  hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return e;
+  for (size_t i = 0; i < code.size(); ++i) {
+    const int x = (code[i] & 127) >> 3, m = code[i] & 7;
+    float v = x == 15 && m == 7 ? NAN : x ? std::ldexp(8.f + m, x - 10) : std::ldexp((float)m, -9);
+    v = (code[i] & 128 ? -v : v) * scale[i / each];
+    uint32_t bits;
+    memcpy(&bits, &v, sizeof bits);
+    out[i] = (bf16_t)(bits >> 16);   // exact
+  }
+  return hipSuccess;
+}
 
 template <class F>
 spec_status guarded(spec_ctx* ctx, F f) {
@@ -977,6 +1047,21 @@ spec_status spec_init(const spec_config* cfg, const void* embed, const spec_mode
       next += n;
     }
     std::copy(c.pt_host.begin(), c.pt_host.end(), host(c.pt));
+    if (c.kv8) {
+      // The target's pages in 8 bits and its others lie in pools of their own, in
+      // the order of their page numbers.
+      std::vector<char> in8(c.pool, 0);
+      for (int b = 0; b < c.B; ++b)
+        for (int i = 0; i < c.n8[b]; ++i) in8[c.pt_host[(size_t)b * c.pps + i]] = 1;
+      std::vector<int32_t> to(c.pool);
+      for (int p = 0, n8 = 0, n16 = 0; p < c.pool; ++p) to[p] = in8[p] ? n8++ : n16++;
+      c.kv8_pt_host.assign((size_t)c.B * c.pps, 0);
+      for (int b = 0; b < c.B; ++b)
+        for (int i = 0; i < c.npages[b]; ++i)
+          c.kv8_pt_host[(size_t)b * c.pps + i] = to[c.pt_host[(size_t)b * c.pps + i]];
+      std::copy(c.kv8_pt_host.begin(), c.kv8_pt_host.end(), host(c.kv8_pt));
+      std::copy(c.n8.begin(), c.n8.end(), host(c.kv8_packed));
+    }
     // token class of every slot for the attention-budget readout (Sec. 4.2):
     // vision-block slots, other prompt slots, generated slots
     for (int b = 0; b < c.B; ++b) {
@@ -1034,10 +1119,12 @@ spec_status spec_init(const spec_config* cfg, const void* embed, const spec_mode
         return hip_fail(e, "weight packing");
     }
     for (int b = 0; b < c.B; ++b) {
-      for (int l = 0; l < c.tgt.d.layers; ++l)
-        if ((e = launch_prefix_kv(c, c.tgt, l, b, seqs[b].prefix_len, static_cast<const bf16_t*>(seqs[b].tgt_k[l]),
-                                  static_cast<const bf16_t*>(seqs[b].tgt_v[l]))) != hipSuccess)
+      for (int l = 0; l < c.tgt.d.layers; ++l) {
+        const bf16_t *k = static_cast<const bf16_t*>(seqs[b].tgt_k[l]), *v = static_cast<const bf16_t*>(seqs[b].tgt_v[l]);
+        if ((e = launch_prefix_kv(c, c.tgt, l, b, seqs[b].prefix_len, k, v)) != hipSuccess ||
+            (c.kv8 && (e = launch_prefix_kv8(c, l, b, seqs[b].prefix_len, k, v)) != hipSuccess))
           return hip_fail(e, "prefix K/V");
+      }
       if (has_draft)
         for (int l = 0; l < c.drf.d.layers; ++l)
           if ((e = launch_prefix_kv(c, c.drf, l, b, seqs[b].prefix_len,
@@ -1204,6 +1291,7 @@ spec_status spec_attn_readout(spec_ctx* ctx, int32_t model, int32_t layer, float
     if (model != 0 && model != 1) return set_err(c, SPEC_E_INVAL, "spec_attn_readout: model must be 0 or 1");
     if (model == 1 && !c.has_draft) return set_err(c, SPEC_E_STATE, "spec_attn_readout: no draft model");
     const Model& m = model ? c.drf : c.tgt;
+    if (model == 0 && c.kv8) return set_err(c, SPEC_E_STATE, "spec_attn_readout: the target's cache is held in 8 bits");
     if (layer < 0 || layer >= m.d.layers) return set_err(c, SPEC_E_INVAL, "spec_attn_readout: layer out of range");
     if (!aligned16(d_out)) return set_err(c, SPEC_E_INVAL, "spec_attn_readout: d_out must be 16-byte aligned");
     c.ro_arm_model = model;
@@ -1304,7 +1392,8 @@ spec_status spec_debug_attn_pages(const spec_config* cfg, const spec_seq_init* s
       g_init_error = err;
       return SPEC_E_INVAL;
     }
-    *pages = attn_pages_per_workgroup(cfg, seqs, num_cus());
+    *pages = (cfg->flags & SPEC_FLAG_KV8) ? kv8_pages_per_group(cfg, seqs, num_cus())
+                                          : attn_pages_per_workgroup(cfg, seqs, num_cus());
     return SPEC_OK;
   } catch (...) {
     return SPEC_E_INVAL;
@@ -1325,12 +1414,17 @@ spec_status spec_debug_kv(spec_ctx* ctx, int32_t b, int32_t model, int32_t layer
     // one page (all kv heads) at a time: keys [nkv][page][D], values [nkv][D][page]
     const size_t page_elems = (size_t)nkv * kAttnChunk * D;
     std::vector<bf16_t> tmp(page_elems);
+    const std::vector<int32_t>& pt = c.kv8 && model == 0 ? c.kv8_pt_host : c.pt_host;
     for (int s = pos0; s < pos0 + npos;) {
       const int pi = s / kAttnChunk, off = s % kAttnChunk;
       const int n = std::min(kAttnChunk - off, pos0 + npos - s);
-      const bf16_t* src = (which == 0 ? m.kc : m.vt) + m.kv_layer * layer +
-                          (size_t)c.pt_host[(size_t)b * c.pps + pi] * page_elems;
-      HIPCHK(c, hipMemcpy(tmp.data(), src, page_elems * 2, hipMemcpyDeviceToHost), "kv read");
+      const size_t page = pt[(size_t)b * c.pps + pi];
+      if (c.kv8 && model == 0 && pi < c.n8[b]) {
+        HIPCHK(c, read_page8(c, layer, which, page, tmp), "kv read");
+      } else {
+        const bf16_t* src = (which == 0 ? m.kc : m.vt) + m.kv_layer * layer + page * page_elems;
+        HIPCHK(c, hipMemcpy(tmp.data(), src, page_elems * 2, hipMemcpyDeviceToHost), "kv read");
+      }
       for (int i = 0; i < n; ++i)
         for (int h = 0; h < nkv; ++h)
           for (int d = 0; d < D; ++d)

@@ -1,0 +1,258 @@
+"""Contexts whose prompt cache is held in 8 bits (SPEC_FLAG_KV8): the cache bit for bit, verifies against the oracle over
+the values that cache stands for, greedy equivalence, and the scores of what they commit."""
+import numpy as np
+import pytest
+
+import workloads as W
+from oracle import numerics as ON
+from tests import _operators as ref
+from tests import _support as S
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+
+def _session(w, flags=0, **kw):
+    from paper_2606_31160_amd import binding as B
+    from paper_2606_31160_amd.harness import Session
+    return Session(w, flags=flags | B.SPEC_FLAG_KV8, **kw)
+
+
+def _plain_session(w, flags=0, **kw):
+    from paper_2606_31160_amd.harness import Session
+    return Session(w, flags=flags, **kw)
+
+
+def _packed(bits, n8):
+    """The values that prompt rows [P][nkv][D] stand for with their first n8 pages in 8 bits."""
+    x = ref.bf16_value(bits).copy()
+    for i in range(n8):
+        for h in range(x.shape[1]):
+            p = x[PAGE * i:PAGE * i + PAGE, h]
+            s = ref.page_scale(p)
+            x[PAGE * i:PAGE * i + PAGE, h] = ref.e4m3_round(p / s) * s
+    return x
+
+
+def _oracle(w, b, T, D, s, **kw):
+    """The oracle's sequence b over the prompt values that session s holds."""
+    seq = S.oracle_sequence(w, b, T, D, **kw)
+    P = w.seqs[b].prefix_len
+    for li in range(w.target.layers):
+        seq.tc.k[li][:P] = ON.decode(s.kv(b, 0, li, 0, 0, P))
+        seq.tc.v[li][:P] = ON.decode(s.kv(b, 0, li, 1, 0, P))
+    return seq
+
+
+def _tiny(prompts, **kw):
+    w = W.get("C1").with_(seqs=tuple(W.c5_layout(p) if p >= 256 else W.SeqLayout(p) for p in prompts),
+                          p_accept=(0.8,) * len(prompts))
+    return w.with_(**kw) if kw else w
+
+
+@pytest.mark.parametrize("prompts,page_seed", [((320,), None), ((63,), None), ((64,), 1), ((200, 320, 1, 130, 65), 3)])
+def test_prompt_caches_bit_for_bit(prompts, page_seed):
+    w = _tiny(prompts)
+    s, p = _session(w, page_seed=page_seed), _plain_session(w, page_seed=page_seed)
+    assert s.ws_bytes < p.ws_bytes or max(prompts) < PAGE
+    for b, n in enumerate(prompts):
+        for li in range(w.target.layers):
+            for which in (0, 1):
+                want = _packed(p.kv(b, 0, li, which, 0, n), n // PAGE)
+                np.testing.assert_array_equal(ref.bf16_value(s.kv(b, 0, li, which, 0, n)), want)
+        for which in (0, 1):                      # the draft's cache stays as it is
+            np.testing.assert_array_equal(s.kv(b, 1, 0, which, 0, n), p.kv(b, 1, 0, which, 0, n))
+    s.close()
+    p.close()
+
+
+@pytest.mark.parametrize("flags", [0, 1, 8])      # replayed graphs, direct launches, row-major weights
+@pytest.mark.parametrize("prompts", [(320,), (63,), (100, 320, 65)])
+def test_verify_against_the_oracle(flags, prompts):
+    w = _tiny(prompts)
+    T, D = S.oracle_decoders(w, W.HostWeights(w))
+    s = _session(w, flags, page_seed=7)
+    seqs = [_oracle(w, b, T, D, s) for b in range(s.B)]
+    rng = np.random.default_rng(5)
+    for _ in range(2):                            # the second round reads what the first one appended
+        drafts = rng.integers(0, w.vocab, (s.B, w.K)).astype(np.int32)
+        before = [s.state(b)["seq_len"] for b in range(s.B)]
+        s.verify(drafts, logits=True)
+        s.commit()
+        coms, acc, _ = s.committed()
+        gl = s.logits.float().cpu().numpy()
+        for b, seq in enumerate(seqs):
+            r = seq.verify(drafts[b])
+            for j in range(w.K + 1):
+                assert S.normwise_err(gl[b, j], r.logits[j]) <= S.LOGIT_RTOL, (b, j)
+            pinned = S.margin(r.logits) > S.MARGIN
+            assert pinned[:r.accept_len + 1].all()
+            assert coms[b] == list(r.committed) and int(acc[b]) == r.accept_len
+            for li in range(w.target.layers):
+                for which, cache in ((0, seq.tc.k), (1, seq.tc.v)):
+                    got = ON.decode(s.kv(b, 0, li, which, before[b], w.K + 1))
+                    assert S.normwise_err(got, cache[li][before[b]:before[b] + w.K + 1]) <= S.LOGIT_RTOL
+    assert s.sync() == 0
+    s.close()
+
+
+def test_sixteen_scenes_against_the_oracle():
+    """80 rows: the wide-unit GEMM takes the attention's rows in operand order."""
+    prompts = tuple(int(n) for n in np.random.default_rng(2).integers(40, 700, 16))
+    w = _tiny(prompts)
+    T, D = S.oracle_decoders(w, W.HostWeights(w))
+    s = _session(w, page_seed=11)
+    drafts = np.random.default_rng(6).integers(0, w.vocab, (16, w.K)).astype(np.int32)
+    s.verify(drafts, logits=True)
+    gl = s.logits.float().cpu().numpy()
+    for b in range(0, 16, 3):
+        r = _oracle(w, b, T, D, s).verify(drafts[b])
+        for j in range(w.K + 1):
+            assert S.normwise_err(gl[b, j], r.logits[j]) <= S.LOGIT_RTOL, (b, j)
+    s.close()
+
+
+def test_7b_width_layer_against_the_oracle():
+    w = W.scaled(W.get("C2"), prefix_scale=0.25).with_(draft=None)
+    T, _ = S.oracle_decoders(w, W.HostWeights(w))
+    s = _session(w, with_draft=False)
+    drafts = np.random.default_rng(8).integers(0, w.vocab, (1, w.K)).astype(np.int32)
+    s.verify(drafts, logits=True)
+    r = _oracle(w, 0, T, None, s, with_draft=False).verify(drafts[0])
+    gl = s.logits[0].float().cpu().numpy()
+    for j in range(w.K + 1):
+        assert S.normwise_err(gl[j], r.logits[j]) <= S.LOGIT_RTOL, j
+    s.close()
+
+
+def _loop(s, mode):
+    out = [[] for _ in range(s.B)]
+    for _ in range(200):
+        if mode == "draft":
+            s.draft_steps(s.K)
+        s.verify(None)
+        s.commit()
+        coms, _, fin = s.committed()
+        for b in range(s.B):
+            out[b] += [int(t) for t in coms[b]]
+        if fin.all():
+            return out
+    raise AssertionError("not finished")
+
+
+@pytest.mark.parametrize("extra", ["chain", "block", "cond", "cross"])
+def test_speculation_keeps_the_greedy_output(extra):
+    """K = 4 with the draft's own proposals against K = 0, token by token, on caches in 8 bits."""
+    from paper_2606_31160_amd import binding as B
+    w = _tiny((320, 150), max_new_tokens=90)
+    kw = {}
+    flags = 0
+    if extra == "block":
+        flags = B.SPEC_FLAG_BLOCK_DRAFT
+    elif extra in ("cond", "cross"):
+        kw = dict(cond_layers=(0, 1, 1), cond_cross=extra == "cross")
+    s = _session(w, flags, **kw)
+    spec = _loop(s, "draft")
+    s.close()
+    s = _session(w, K=0, with_draft=False)
+    greedy = _loop(s, "ar")
+    s.close()
+    assert spec == greedy
+
+
+def test_speculation_keeps_the_greedy_output_at_7b_heads():
+    """63 rows of a kv head against 7: another form of the attention, the same sums."""
+    w = W.scaled(W.get("C3"), layers=2, vocab=2048, prefix_scale=0.3).with_(max_new_tokens=40)
+    runs = []
+    for K in (8, 0, 3):
+        s = _session(w, source="device", K=K, with_draft=False)
+        out = []
+        greedy = runs[0] if runs else None
+        while True:
+            if K == 0:
+                s.verify(None)
+            else:
+                i = len(out)
+                d = np.zeros((1, K), np.int32)
+                if greedy:                        # right proposals, but for every fourth
+                    t = (greedy[i:i + K] + [0] * K)[:K]
+                    d[0] = [x if j % 4 != 3 else (x + 1) % w.vocab for j, x in enumerate(t)]
+                s.verify(d)
+            s.commit()
+            coms, _, fin = s.committed()
+            out += [int(t) for t in coms[0]]
+            if fin[0]:
+                break
+        s.close()
+        runs.append(out)
+    assert runs[0] == runs[1] == runs[2]
+
+
+def test_scratch_verify_and_repeated_opening():
+    """spec_verify_scratch gives the same logits; so does the context opened again on the same workspace."""
+    from paper_2606_31160_amd import binding as B
+    w = _tiny((320, 90))
+    drafts = np.random.default_rng(9).integers(0, w.vocab, (2, w.K)).astype(np.int32)
+    s = _session(w)
+    s.verify(drafts, logits=True)
+    s.sync()
+    first = s.logits.clone()
+    s.close()
+    s.ctx = B.spec_init(s.cfg, s.embed.data_ptr(), s.tgt_struct, s.drf_struct, _keep_prompt(s, w), s.ws.data_ptr(),
+                        s.ws_bytes, s.stream.cuda_stream)
+    s.vtok.copy_(s.torch.as_tensor(drafts))
+    s.logits.zero_()
+    B.spec_verify_scratch(s.ctx, s.vtok.data_ptr(), s.logits.data_ptr())
+    s.sync()
+    assert s.torch.equal(s.logits, first)
+    s.close()
+
+
+def _keep_prompt(s, w):
+    """The session's sequences with prompt K/V on the device again (a session lets go of them)."""
+    from paper_2606_31160_amd.harness import ctypes_void_array
+    s._again = []
+    for b in range(s.B):
+        for model, shape, kn, vn in (("target", w.target, "tgt_k", "tgt_v"), ("draft", w.draft, "drf_k", "drf_v")):
+            for which, name in (("k", kn), ("v", vn)):
+                ts = [s._prefix(b, model, li, which) for li in range(shape.layers)]
+                arr = ctypes_void_array(len(ts))(*[t.data_ptr() for t in ts])
+                s._again += ts + [arr]
+                setattr(s.seqs[b], name, arr)
+    return s.seqs
+
+
+def test_readout_is_refused_for_the_target_only():
+    from paper_2606_31160_amd import binding as B
+    s = _session(_tiny((320,)))
+    with pytest.raises(B.SpecError) as e:
+        s.attn_readout(0, 0)
+    assert e.value.status == 2
+    out = s.attn_readout(1, 0)
+    s.draft_steps(s.K)
+    s.sync()
+    got = out.cpu().numpy()
+    assert np.isfinite(got[0, 0]).all() and np.allclose(got[0, 0, :, :3].sum(-1), 1, atol=1e-3)
+    s.close()
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+def test_scores_of_committed_tokens(kv8):
+    """Pack, attend, verify, commit and score, as a program uses them together, over several rounds."""
+    w = _tiny((320, 100))
+    s = (_session if kv8 else _plain_session)(w)
+    for _ in range(3):
+        s.draft_steps(s.K)
+        s.verify(None, logits=True)
+        s.commit()
+        got = {k: v.double().cpu().numpy() for k, v in s.logprobs(top=5).items()}
+        coms, _, _ = s.committed()
+        z = s.logits.double().cpu().numpy()
+        for b in range(s.B):
+            for j, t in enumerate(coms[b]):
+                g, h, order, glp, _ = ref.scores(z[b, j], [t], 5)
+                # fp32 results of at most 1024 terms: far within 2^-18 of ln V
+                assert abs(got["logprob"][b, j] - g[0]) <= 2.0 ** -18 * 7 and abs(got["entropy"][b, j] - h) <= 2.0 ** -18 * 7
+                assert (got["top_token"][b, j] == order).all()
+                assert np.abs(got["top_logprob"][b, j] - glp).max() <= 2.0 ** -18 * 7
+    s.close()

@@ -109,3 +109,17 @@ def test_logprobs_refuses_a_small_workspace():
         refused(lambda: B.spec_logprobs_workspace_bytes(*bad), INVAL, "spec_logprobs_workspace_bytes")
     assert B.lib().spec_logprobs_workspace_bytes(1, 10, 1, None) == INVAL
     assert B.lib().spec_kv8_attn_workspace_bytes(ctypes.byref(cache()), 1, 1, 4, 1, None) == INVAL
+
+
+def test_contexts_with_prompts_in_8_bits_take_less_workspace():
+    import workloads as W
+    from tests.test_abi_host import _blocks, _cfg, _seqs
+    w = W.get("C1")
+    n = []
+    for flags in (0, B.SPEC_FLAG_KV8):
+        cfg = _cfg(w)
+        cfg.flags = flags
+        seqs, keep = _seqs(w, cfg, blocks=_blocks(w))
+        n.append(B.spec_workspace_bytes(cfg, seqs))
+        assert B.spec_debug_attn_pages(cfg, seqs) >= 1
+    assert n[1] < n[0]
