@@ -426,6 +426,7 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  * n = 0: out = 0 and lse = -infinity.  n < 0: no such row; its out and lse are left
  * as they were.  Slots that a row does not see have no influence on it, whatever
  * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS.
+ *   scale        positive and finite
  *   d_table      [batch][table_stride] device int32; entries past a sequence's
  *                visible pages are not read
  *   d_packed     [batch] device int32

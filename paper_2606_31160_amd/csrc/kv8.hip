@@ -116,6 +116,8 @@ __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
 //   m' = max(m, max s),  l' = 2^(m - m') l + sum 2^(s - m'),  O' = 2^(m - m') O + sum 2^(s - m') v.
 // ---------------------------------------------------------------------------
 
+constexpr int kKeyWaves = 4;    // waves that share a group's pages: wave w takes pages w, w + 4, ..
+
 // Slots that row j of sequence b sees; negative: no such row.
 __device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, int b, int j) {
   if (!a.st) return a.vis[b * a.R + j];
@@ -123,41 +125,66 @@ __device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, int b, int j) {
   return j < s.count ? s.base + (j < s.causal ? j + 1 : s.count) : -1;
 }
 
-__device__ __forceinline__ int seq_pages(const Kv8AttnArgs& a, int b) {
-  int end = 0;
+// Pages of sequences lane, lane + 64 and lane + 128; tmp: LDS of SPEC_MAX_ROWS
+// words of this wave's own.
+__device__ __forceinline__ void seq_pages(const Kv8AttnArgs& a, int (&pages)[3], int* tmp) {
+  const int lane = threadIdx.x & 63;
+  int end[3] = {0, 0, 0};
   if (a.st) {
-    const SeqState& s = a.st[b];
-    end = s.count > 0 ? s.base + s.count : 0;
+    if (lane < a.B) {
+      const SeqState& s = a.st[lane];
+      end[0] = s.count > 0 ? s.base + s.count : 0;
+    }
   } else {
-    for (int j = 0; j < a.R; ++j) end = max(end, a.vis[b * a.R + j]);
+    const int n = a.B * a.R;
+    int v[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] = lane + 64 * i < n ? a.vis[lane + 64 * i] : 0;
+    if (a.R == 1) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) end[i] = v[i];
+    } else if (a.B == 1) {
+      int m = max(max(v[0], v[1]), v[2]);
+      for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o));
+      end[0] = lane == 0 ? m : 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (lane + 64 * i < n) tmp[lane + 64 * i] = v[i];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (lane + 64 * i < a.B)
+          for (int j = 0; j < a.R; ++j) end[i] = max(end[i], tmp[(lane + 64 * i) * a.R + j]);
+    }
   }
-  return min((end + kAttnChunk - 1) / kAttnChunk, a.stride);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) pages[i] = min((max(end[i], 0) + kAttnChunk - 1) / kAttnChunk, a.stride);
 }
 
 // Groups are numbered sequence by sequence, a sequence's kv head by kv head.
-// Every wave of a workgroup counts them for itself, lane l sequences l, l + 64, ..
+// Every wave of a workgroup counts them for itself.
 struct Groups {
   int ppw;
   int pages[3], first[3];   // of sequence lane + 64 i: pages, number of its first group
   int total;
 };
 
-__device__ __forceinline__ Groups count_groups(const Kv8AttnArgs& a) {
+__device__ __forceinline__ Groups count_groups(const Kv8AttnArgs& a, int* tmp) {
   const int lane = threadIdx.x & 63;
   Groups g;
-  int all = 0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int b = lane + 64 * i;
-    g.pages[i] = b < a.B ? seq_pages(a, b) : 0;
-    all += g.pages[i];
-  }
-  for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+  seq_pages(a, g.pages, tmp);
   g.ppw = a.ppw;
-  if (g.ppw == 0) g.ppw = min(max((int)(((int64_t)all * a.nkv + a.target - 1) / a.target), 1), kKv8MaxPages);
+  if (g.ppw == 0) {
+    int all = g.pages[0] + g.pages[1] + g.pages[2];
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+    g.ppw = kv8_group_pages((int64_t)all * a.nkv, a.target);
+  }
   int before = 0;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
+    g.first[i] = before;
+    if (64 * i >= a.B) continue;
     const int n = a.nkv * ((g.pages[i] + g.ppw - 1) / g.ppw);
     int sum = n;
     for (int o = 1; o < 64; o <<= 1) {
@@ -186,9 +213,9 @@ __device__ __forceinline__ u32x4 f16_of_e4m3(uint32_t lo, uint32_t hi) {
                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
   return __builtin_bit_cast(u32x4, r);
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const f16x2 v = {(_Float16)lo, (_Float16)hi};
-  return __builtin_bit_cast(uint32_t, v);
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), f16x2));
 }
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -198,30 +225,90 @@ __device__ __forceinline__ bool has_nan8(uint32_t w) { return (((w & 0x7f7f7f7fu
 __device__ __forceinline__ bool not_finite16(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
+__device__ __forceinline__ float lane_f(float x, int l) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
+}
 
-constexpr int kWaves = 4;
+// The softmax state of a wave's rows (lane: row lane & 15 of each block).
+template <int NRB, int NDT>
+struct RowState {
+  float m[NRB], l[NRB];
+  f32x4 o[NRB][NDT];
+};
 
-// grid (groups, row blocks / NRB), 4 waves; wave w takes pages w, w + 4, .. of the
-// group for all 16 NRB rows, so that every code is read and converted once.
+constexpr float kGrow = 8.f, kHead = 7.f;
+
+// Scores s of 16 keys per lane -> probabilities 2^(s sc - m + off), and l.  The
+// maximum follows only when a row's scores pass it by 2^8, so that the sums are
+// seldom rescaled and lanes seldom compared: a probability is at most 2^(8 + off).
+template <int NRB, int NDT>
+__device__ __forceinline__ void soft(RowState<NRB, NDT>& st, float (&s)[NRB][16], float sc, float off) {
+  bool grow = false;
+  float pm[NRB];
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    pm[rb] = s[rb][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) pm[rb] = fmaxf(pm[rb], s[rb][i]);
+    grow |= pm[rb] * sc > st.m[rb] + kGrow;
+  }
+  if (__any(grow)) {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 16));
+      pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 32));
+      const float mn = pm[rb] * sc;
+      if (mn > st.m[rb] + kGrow) {                  // (a row's own matter: the others' sums stay as they are)
+        const float alpha = st.m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[rb] - mn);
+        st.m[rb] = mn;
+        st.l[rb] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= alpha;
+      }
+    }
+  }
+  const float back = __builtin_amdgcn_exp2f(-off);
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    const float c = off - (st.m[rb] == -INFINITY ? 0.f : st.m[rb]);   // no key seen yet: all probabilities zero
+    float ls = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[rb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i], sc, c));
+      ls += s[rb][i];
+    }
+    st.l[rb] = __builtin_fmaf(ls, back, st.l[rb]);
+  }
+}
+
+// grid (groups, row blocks / (NRB WR)), WR x 4 waves: wave w has row blocks NRB (w %
+// WR) .. and pages w / WR, + 4, .. of the group.
 //
 // S^T = K Q^T and O^T = V^T P^T by 16x16x32 MFMA, lane (n = lane & 15, g = lane >> 4)
 // holding row n.  Row i of key tile t is key 16 (i >> 2) + 4 t + (i & 3): the 16
 // scores of a lane belong to the consecutive keys 16 g .. 16 g + 15, one 16-byte read
 // of a value row; and a lane's 16 bytes of a key row serve two steps over the head
-// dimension, whose order is the same in Q's operand.
+// dimension, whose order is the same in Q's operand.  The next page's keys are
+// loaded while this one's softmax runs, its values while the next scores are formed.
 //   Keys are read as bf16, like Q.  Values and probabilities are read as fp16: an
-// e4m3 code is exact in it, and a probability (at most 1) keeps 11 bits, as a
-// rounding to bf16 would show in the bf16 result.  bf16 pages take their values as
-// they are and each probability as the sum of two bf16 numbers.
-//   O is held in units of the last page's value scale.
-template <int D, int NRB>
-__global__ __launch_bounds__(256) void k_kv8_attn(Kv8AttnArgs a) {
-  constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kWaves;
-  __shared__ f32x4 s_o[2][kWaves][kWaves - 1][ND4][64];
-  __shared__ float s_m[kWaves][NRB * 16], s_l[kWaves][NRB * 16];
+// e4m3 code is exact in it, and a probability keeps 11 bits, as a rounding to bf16
+// would show in the bf16 result.  The value scale is part of the probability's
+// exponent: with u the largest one of the group, p vs / u 2^7 is in fp16's normal
+// range down to 2^-21 (a page whose scale is further below u has O turned to its
+// own unit for as long).  bf16 pages take their values as they are and each
+// probability as the sum of two bf16 numbers.
+//   Which pages share a wave depends on the group only, and a row's sums on no
+// other row, so contexts that differ in K, and so in NRB and WR, sum alike.
+template <int D, int NRB, int WR>
+__global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs a) {
+  constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kKeyWaves;
+  __shared__ f32x4 s_o[2][WR][kKeyWaves][kKeyWaves - 1][ND4][64];
+  __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
+  __shared__ int s_tmp[WR * kKeyWaves][SPEC_MAX_ROWS];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int wr = wave % WR, wk = wave / WR;
   const int n16 = lane & 15, g4 = lane >> 4;
-  const Groups gr = count_groups(a);
+  const Groups gr = count_groups(a, s_tmp[wave]);
   const int id = blockIdx.x;
   if (id >= gr.total) return;
   int b = 0, pages = 0, first = 0;
@@ -232,8 +319,8 @@ __global__ __launch_bounds__(256) void k_kv8_attn(Kv8AttnArgs a) {
     if (m) {
       const int l = 63 - __builtin_clzll(m);
       b = l + 64 * i;
-      pages = __shfl(gr.pages[i], l);
-      first = __shfl(gr.first[i], l);
+      pages = __builtin_amdgcn_readlane(gr.pages[i], l);
+      first = __builtin_amdgcn_readlane(gr.first[i], l);
     }
   }
   b = __builtin_amdgcn_readfirstlane(b);
@@ -245,23 +332,13 @@ __global__ __launch_bounds__(256) void k_kv8_attn(Kv8AttnArgs a) {
   const int packed = min(max(a.packed[b], 0), a.stride);
   const int n8 = min(max(packed - p0, 0), np);
 
-  // lane l: the group's l-th page and its scales; -1: not to be read
+  // lane l: the group's l-th page and its scales
   int page = -1;
   float ks = 1.f, vsc = 1.f;
-  if (lane < np) {
-    page = a.table[(size_t)b * a.stride + p0 + lane];
-    const bool in8 = lane < n8;
-    if (page < 0 || page >= (in8 ? a.pages8 : a.pages16)) page = -1;
-    if (in8 && page >= 0) {
-      ks = a.ks[(size_t)page * a.nkv + kvh];
-      vsc = a.vs[(size_t)page * a.nkv + kvh];
-      if (!(ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY)) page = -1;
-    }
-    if (page < 0 && a.err) *a.err = SPEC_E_INVAL;
-  }
+  if (lane < np) page = a.table[(size_t)b * a.stride + p0 + lane];
 
-  // rows of this workgroup
-  const int rows = a.R * a.G, r0 = blockIdx.y * NRB * 16;
+  // rows of this wave
+  const int rows = a.R * a.G, r0 = (blockIdx.y * WR + wr) * NRB * 16;
   int vis[NRB], vmin = INT32_MAX, vmax = 0;
   u32x4 qf[NRB][2 * KH];
 #pragma unroll
@@ -284,292 +361,357 @@ __global__ __launch_bounds__(256) void k_kv8_attn(Kv8AttnArgs a) {
     vmax = max(vmax, __shfl_xor(vmax, o));
   }
   vmin = __builtin_amdgcn_readfirstlane(vmin);
-  vmax = __builtin_amdgcn_readfirstlane(vmax);      // slots that no row of the workgroup sees: from here
+  vmax = __builtin_amdgcn_readfirstlane(vmax);      // slots that no row of this wave sees: from here
 
-  float m[NRB], l[NRB], u = 0.f;                    // u: unit of o
-  f32x4 o[NRB][NDT];
+  // pages that may be read, and those that this wave has to
+  if (page < 0 || page >= (lane < n8 ? a.pages8 : a.pages16)) page = -1;
+  if (lane < n8 && page >= 0) {
+    ks = a.ks[(size_t)page * a.nkv + kvh];
+    vsc = a.vs[(size_t)page * a.nkv + kvh];
+  }
+  const int seen = vmax <= p0 * kAttnChunk ? 0 : min(np, (vmax - p0 * kAttnChunk + kAttnChunk - 1) / kAttnChunk);
+  uint64_t todo = __ballot(lane < seen && page >= 0 && lane % kKeyWaves == wk);
+  const uint64_t mask8 = n8 >= 64 ? ~0ull : (1ull << n8) - 1;
+
+  RowState<NRB, NDT> st;
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
-    m[rb] = -INFINITY;
-    l[rb] = 0.f;
+    st.m[rb] = -INFINITY;
+    st.l[rb] = 0.f;
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) o[rb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int p = wave; p < np; p += kWaves) {
-    const int pg = __builtin_amdgcn_readlane(page, p);
-    if (pg < 0) continue;
-    const bool in8 = p < n8;
-    const size_t at = ((size_t)pg * a.nkv + kvh) * kAttnChunk * D;   // element of the page's first key or value
+  const int krow = 16 * (n16 >> 2) + (n16 & 3);     // key of this lane in tile 0
+  u32x4 kr[4][KH], vr[NDT];
+  auto at_of = [&](int p) {                         // element of the page's first key or value
+    return ((size_t)__builtin_amdgcn_readlane(page, p) * a.nkv + kvh) * kAttnChunk * D;
+  };
+  auto load_k = [&](int p) {
+    const uint8_t* kp = a.k8 + at_of(p) + krow * D + 16 * g4;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int h = 0; h < KH; ++h) kr[t][h] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * h);
+  };
+  auto load_v = [&](int p) {
+    const uint8_t* vp = a.v8 + at_of(p) + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
+  };
+  auto mask = [&](float (&s)[NRB][16], int k0) {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (k0 + 16 * g4 + i >= vis[rb]) s[rb][i] = -INFINITY;
+  };
+  auto turn_o = [&](float f) {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= f;
+  };
+  // A page whose unit is far from u: O is turned by 2^far while it is added, and
+  // what 2^60 leaves (seen in no sound cache) is taken by the probabilities.
+  auto far_of = [](float off) { return fabsf(off) > 16.f ? fminf(fmaxf(-off, -60.f), 60.f) : 0.f; };
+  auto times = [](float (&s)[NRB][16], float f) {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[rb][i] *= f;
+  };
+  // A page's values that are not finite were taken as zero where not every row sees
+  // the page, as zero probability times one is not zero: only rows that see the
+  // slot get them.
+  auto add_odd = [&](int p, bool in8) {
+    const int k0 = (p0 + p) * kAttnChunk, end = min(vmax - k0, kAttnChunk);
+    const size_t at = at_of(p);
+    for (int k = 0; k < end; ++k)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const size_t v = at + (size_t)(16 * dt + 4 * g4 + i) * kAttnChunk + k;
+          const float x = in8 ? ((a.v8[v] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[v]);
+          if (!(fabsf(x) < INFINITY)) {
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
+              if (k0 + k < vis[rb]) st.o[rb][dt][i] += x;
+          }
+        }
+  };
+
+  uint64_t t8 = todo & mask8;
+  int p = t8 ? __builtin_ctzll(t8) : 64;
+  if (p < 64) {
+    load_k(p);
+    load_v(p);
+  }
+  // (the scales arrive while the first page does)
+  const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
+  if (lane < np && (page < 0 || !fine) && a.err) *a.err = SPEC_E_INVAL;
+  const uint64_t good = __ballot(fine);
+  float u = lane < n8 && page >= 0 && fine ? vsc : 0.f;
+  for (int o = 32; o > 0; o >>= 1) u = fmaxf(u, __shfl_xor(u, o));
+  if (u == 0.f) u = 1.f;
+  const float lv = (lane < n8 ? log2f(vsc) : 0.f) - log2f(u);   // lane l: of the group's l-th page
+  while (p < 64) {
+    t8 &= t8 - 1;
+    const int next = t8 ? __builtin_ctzll(t8) : 64;
+    if (!(good >> p & 1)) {                         // a page without scales: not visible
+      if (next < 64) {
+        load_k(next);
+        load_v(next);
+      }
+      p = next;
+      continue;
+    }
     const int k0 = (p0 + p) * kAttnChunk;
-    if (k0 >= vmax) continue;
     const bool full = k0 + kAttnChunk <= vmin;
     float s[NRB][16];                               // scores, then probabilities, of keys 16 g4 + i
-    float sc = a.scale_log2;
-    const int krow = 16 * (n16 >> 2) + (n16 & 3);   // key of this lane in tile 0
-    if (in8) {
-      sc *= __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), p));
-      const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
-      u32x4 kr[4][KH];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+      f32x4 acc[NRB];
 #pragma unroll
-        for (int h = 0; h < KH; ++h) kr[t][h] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * h);
+      for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f32x4 acc[NRB];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < KH; ++h) {
-          const u32x4 lo = bf16_of_e4m3(kr[t][h].x, kr[t][h].y), hi = bf16_of_e4m3(kr[t][h].z, kr[t][h].w);
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) {
-            acc[rb] = mfma16x16x32(lo, qf[rb][2 * h], acc[rb]);
-            acc[rb] = mfma16x16x32(hi, qf[rb][2 * h + 1], acc[rb]);
-          }
-        }
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
-      }
-    } else {
-      const bf16_t* kp = a.k16 + at + krow * D + 16 * g4;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f32x4 acc[NRB];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < 2 * KH; ++h) {
-          const u32x4 kk = ld16(kp + 4 * t * D + 64 * (h >> 1) + 8 * (h & 1));
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(kk, qf[rb][h], acc[rb]);
-        }
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
-      }
-    }
-    if (!full) {
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (k0 + 16 * g4 + i >= vis[rb]) s[rb][i] = -INFINITY;
-    }
-    // (a scale far below the unit would take o out of range: the probabilities carry it)
-    const float own = in8 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), p)) : 1.f;
-    const float unit = fmaxf(own, u * 0x1p-60f), turn = u / unit;
-    u = unit;
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      float pm = s[rb][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) pm = fmaxf(pm, s[rb][i]);
-      pm = fmaxf(pm, __shfl_xor(pm, 16));
-      pm = fmaxf(pm, __shfl_xor(pm, 32));
-      const float mn = fmaxf(m[rb], pm * sc);
-      const float mm = mn == -INFINITY ? 0.f : mn;  // no key seen yet: all probabilities zero
-      const float alpha = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
-      float ls = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[rb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i], sc, -mm));
-        ls += s[rb][i];
-      }
-      l[rb] = l[rb] * alpha + ls;
-      m[rb] = mn;
-      if (own != unit)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[rb][i] *= own / unit;
-      const float f = alpha == 0.f ? 0.f : alpha * turn;
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) o[rb][dt] *= f;
-    }
-    const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;   // of this lane's 16 keys
-    bool odd = false;                               // a value that is not finite, where not every row sees the page
-    if (in8) {
-      const uint8_t* vp = a.v8 + at + n16 * kAttnChunk + 16 * g4;
-      u32x4 pb[NRB][2];
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float* q = s[rb] + 8 * e;
-          pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
-        }
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        u32x4 vr = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
-        if (!full) {
-          uint32_t w[4] = {vr.x, vr.y, vr.z, vr.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = min(max(valid - 4 * k, 0), 4);
-            w[k] &= c == 4 ? 0xffffffffu : (1u << (8 * c)) - 1;
-            if (has_nan8(w[k])) {
-              odd = true;
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (((w[k] >> (8 * e)) & 0x7f) == 0x7f) w[k] &= ~(0xffu << (8 * e));
-            }
-          }
-          vr = u32x4{w[0], w[1], w[2], w[3]};
-        }
-        const u32x4 lo = f16_of_e4m3(vr.x, vr.y), hi = f16_of_e4m3(vr.z, vr.w);
+      for (int h = 0; h < KH; ++h) {
+        const u32x4 lo = bf16_of_e4m3(kr[t][h].x, kr[t][h].y), hi = bf16_of_e4m3(kr[t][h].z, kr[t][h].w);
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-          o[rb][dt] = mfma_f16(lo, pb[rb][0], o[rb][dt]);
-          o[rb][dt] = mfma_f16(hi, pb[rb][1], o[rb][dt]);
+          acc[rb] = mfma16x16x32(lo, qf[rb][2 * h], acc[rb]);
+          acc[rb] = mfma16x16x32(hi, qf[rb][2 * h + 1], acc[rb]);
         }
       }
-    } else {
-      const bf16_t* vp = a.v16 + at + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
+    }
+    if (next < 64) load_k(next);
+    if (!full) mask(s, k0);
+    const float off = lane_f(lv, p), far = far_of(off);
+    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
+    soft(st, s, fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f), far != 0.f ? kHead : off + kHead);
+    if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
+    u32x4 pb[NRB][2];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        u32x4 ph[NRB], pl[NRB];
+        const float* q = s[rb] + 8 * e;
+        pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
+      }
+    bool odd = false;
+    if (!full) {
+      const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;   // of this lane's 16 keys
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-          const float* q = s[rb] + 8 * e;
-          uint32_t w[4], x[4];
+      for (int dt = 0; dt < NDT; ++dt) {
+        uint32_t w[4] = {vr[dt].x, vr[dt].y, vr[dt].z, vr[dt].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = min(max(valid - 4 * k, 0), 4);
+          w[k] &= c == 4 ? 0xffffffffu : (1u << (8 * c)) - 1;
+          if (has_nan8(w[k])) {
+            odd = true;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (((w[k] >> (8 * e)) & 0x7f) == 0x7f) w[k] &= ~(0xffu << (8 * e));
+          }
+        }
+        vr[dt] = u32x4{w[0], w[1], w[2], w[3]};
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      const u32x4 lo = f16_of_e4m3(vr[dt].x, vr[dt].y), hi = f16_of_e4m3(vr[dt].z, vr[dt].w);
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        st.o[rb][dt] = mfma_f16(lo, pb[rb][0], st.o[rb][dt]);
+        st.o[rb][dt] = mfma_f16(hi, pb[rb][1], st.o[rb][dt]);
+      }
+    }
+    if (next < 64) load_v(next);
+    if (__any(odd)) add_odd(p, true);
+    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
+    p = next;
+  }
+
+  for (uint64_t t16 = todo & ~mask8; t16; t16 &= t16 - 1) {
+    const int q = __builtin_ctzll(t16);
+    const size_t at = at_of(q);
+    const int k0 = (p0 + q) * kAttnChunk;
+    const bool full = k0 + kAttnChunk <= vmin;
+    float s[NRB][16];
+    const bf16_t* kp = a.k16 + at + krow * D + 16 * g4;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 acc[NRB];
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < 2 * KH; ++h) {
+        const u32x4 kk = ld16(kp + 4 * t * D + 64 * (h >> 1) + 8 * (h & 1));
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(kk, qf[rb][h], acc[rb]);
+      }
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
+    }
+    if (!full) mask(s, k0);
+    const float off = lane_f(lv, q), far = far_of(off);
+    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
+    soft(st, s, a.scale_log2, far != 0.f ? kHead : off + kHead);
+    if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
+    const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;
+    bool odd = false;
+    const bf16_t* vp = a.v16 + at + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      u32x4 ph[NRB], pl[NRB];
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        const float* pr = s[rb] + 8 * e;
+        uint32_t w[4], x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          w[k] = pack2(pr[2 * k], pr[2 * k + 1]);
+          x[k] = pack2(pr[2 * k] - __uint_as_float(w[k] << 16), pr[2 * k + 1] - __uint_as_float(w[k] & 0xffff0000u));
+        }
+        ph[rb] = u32x4{w[0], w[1], w[2], w[3]};
+        pl[rb] = u32x4{x[0], x[1], x[2], x[3]};
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        u32x4 v = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
+        if (!full) {
+          uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            w[k] = pack2(q[2 * k], q[2 * k + 1]);
-            x[k] = pack2(q[2 * k] - __uint_as_float(w[k] << 16), q[2 * k + 1] - __uint_as_float(w[k] & 0xffff0000u));
+            const int c = valid - 8 * e - 2 * k;
+            w[k] = c >= 2 ? w[k] : c == 1 ? w[k] & 0xffffu : 0u;
+            if (not_finite16(w[k])) {
+              odd = true;
+              if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+              if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
+            }
           }
-          ph[rb] = u32x4{w[0], w[1], w[2], w[3]};
-          pl[rb] = u32x4{x[0], x[1], x[2], x[3]};
+          v = u32x4{w[0], w[1], w[2], w[3]};
         }
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          u32x4 vr = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
-          if (!full) {
-            uint32_t w[4] = {vr.x, vr.y, vr.z, vr.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int c = valid - 8 * e - 2 * k;
-              w[k] = c >= 2 ? w[k] : c == 1 ? w[k] & 0xffffu : 0u;
-              if (not_finite16(w[k])) {
-                odd = true;
-                if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
-                if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
-              }
-            }
-            vr = u32x4{w[0], w[1], w[2], w[3]};
-          }
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) {
-            o[rb][dt] = mfma16x16x32(vr, ph[rb], o[rb][dt]);
-            o[rb][dt] = mfma16x16x32(vr, pl[rb], o[rb][dt]);
-          }
+        for (int rb = 0; rb < NRB; ++rb) {
+          st.o[rb][dt] = mfma16x16x32(v, ph[rb], st.o[rb][dt]);
+          st.o[rb][dt] = mfma16x16x32(v, pl[rb], st.o[rb][dt]);
         }
       }
     }
-    if (!full && __any(odd)) {
-      // The page's values that are not finite were taken as zero above, as zero
-      // probability times one is not zero: only rows that see the slot get them.
-      const int end = min(vmax - k0, kAttnChunk);
-      for (int k = 0; k < end; ++k)
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const size_t v = at + (size_t)(16 * dt + 4 * g4 + i) * kAttnChunk + k;
-            const float x = in8 ? ((a.v8[v] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[v]);
-            if (!(fabsf(x) < INFINITY)) {
-#pragma unroll
-              for (int rb = 0; rb < NRB; ++rb)
-                if (k0 + k < vis[rb]) o[rb][dt][i] += x;
-            }
-          }
-    }
+    if (__any(odd)) add_odd(q, false);
+    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
   }
 
-  // Join the four waves' sums: wave w the head dimensions of tiles ND4 w ..
+  // Join the four key waves' sums: key wave w the head dimensions of tiles ND4 w ..
+  u *= __builtin_amdgcn_exp2f(-kHead);
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
-    l[rb] += __shfl_xor(l[rb], 16);
-    l[rb] += __shfl_xor(l[rb], 32);
+    st.l[rb] += __shfl_xor(st.l[rb], 16);
+    st.l[rb] += __shfl_xor(st.l[rb], 32);
     if (g4 == 0) {
-      s_m[wave][16 * rb + n16] = m[rb];
-      s_l[wave][16 * rb + n16] = l[rb];
+      s_m[wk][wr][16 * rb + n16] = st.m[rb];
+      s_l[wk][wr][16 * rb + n16] = st.l[rb];
     }
   }
   __syncthreads();
-  const int nrb = gridDim.y * NRB;                  // row blocks of the partials
+  const int nrb = gridDim.y * WR * NRB;             // row blocks of the partials
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
-    float mx[kWaves], M = -INFINITY, L = 0.f;
+    float mx[kKeyWaves], M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      mx[w] = s_m[w][16 * rb + n16];
+    for (int w = 0; w < kKeyWaves; ++w) {
+      mx[w] = s_m[w][wr][16 * rb + n16];
       M = fmaxf(M, mx[w]);
     }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      L += mx[w] == -INFINITY ? s_l[w][16 * rb + n16] : __builtin_amdgcn_exp2f(mx[w] - M) * s_l[w][16 * rb + n16];
-    const float f = m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - M);
+    for (int w = 0; w < kKeyWaves; ++w) {
+      const float f = mx[w] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx[w] - M);
+      L = __builtin_fmaf(f, s_l[w][wr][16 * rb + n16], L);
+    }
+    const float f = (st.m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[rb] - M)) * u;
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) o[rb][dt] *= f * u;
+    for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      if (w != wave)
+    for (int w = 0; w < kKeyWaves; ++w)
+      if (w != wk)
 #pragma unroll
-        for (int d = 0; d < ND4; ++d) s_o[rb & 1][w][(wave - w + kWaves) % kWaves - 1][d][lane] = o[rb][w * ND4 + d];
+        for (int d = 0; d < ND4; ++d)
+          s_o[rb & 1][wr][w][(wk - w + kKeyWaves) % kKeyWaves - 1][d][lane] = st.o[rb][w * ND4 + d];
     __syncthreads();
     // (the buffer is written again two blocks on, behind the next barrier)
+    const size_t blk = (size_t)id * nrb + (blockIdx.y * WR + wr) * NRB + rb;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      if (w == wave) {
+    for (int w = 0; w < kKeyWaves; ++w)
+      if (w == wk) {
 #pragma unroll
         for (int d = 0; d < ND4; ++d) {
-          f32x4 v = o[rb][w * ND4 + d];
+          f32x4 v = st.o[rb][w * ND4 + d];
 #pragma unroll
-          for (int k = 0; k < kWaves - 1; ++k) v += s_o[rb & 1][w][k][d][lane];
-          const size_t tile = ((size_t)id * nrb + blockIdx.y * NRB + rb) * NDT + w * ND4 + d;
-          *reinterpret_cast<f32x4*>(a.part + (tile * 64 + lane) * 4) = v;
+          for (int k = 0; k < kKeyWaves - 1; ++k) v += s_o[rb & 1][wr][w][k][d][lane];
+          *reinterpret_cast<f32x4*>(a.part + ((blk * NDT + w * ND4 + d) * 64 + lane) * 4) = v;
         }
       }
-    if (wave == 0 && g4 == 0) a.ml[((size_t)id * nrb + blockIdx.y * NRB + rb) * 16 + n16] = make_float2(M, L);
+    if (wk == 0 && g4 == 0) a.ml[blk * 16 + n16] = make_float2(M, L);
   }
 }
 
 // Joins the groups of a (sequence, kv head): grid (sequences x kv heads, row
-// blocks, D / 16), 4 waves, wave w groups w, w + 4, ..  A lane holds four columns
+// blocks, D / 16), NW waves, wave w groups w, w + NW, ..  A lane holds four columns
 // of one row, as the partials do.
-template <int D>
-__global__ __launch_bounds__(256) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
-  constexpr int NDT = D / 16;
-  __shared__ f32x4 s_o[kWaves][64];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
+  constexpr int NDT = D / 16, U = 4;
+  __shared__ f32x4 s_o[NW][64];
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ int s_tmp[NW][SPEC_MAX_ROWS];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n16 = lane & 15, g4 = lane >> 4;
   const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
-  const Groups gr = count_groups(a);
+  const Groups gr = count_groups(a, s_tmp[wave]);
   int pages = 0, first = 0;
 #pragma unroll
   for (int i = 0; i < 3; ++i)
     if (b >> 6 == i) {
-      pages = __shfl(gr.pages[i], b & 63);
-      first = __shfl(gr.first[i], b & 63);
+      pages = __builtin_amdgcn_readlane(gr.pages[i], b & 63);
+      first = __builtin_amdgcn_readlane(gr.first[i], b & 63);
     }
   const int per = (pages + gr.ppw - 1) / gr.ppw;
   first += kvh * per;
   float M = -INFINITY, L = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = wave; i < per; i += kWaves) {
-    const size_t blk = (size_t)(first + i) * nrb + rb;
-    const float2 ml = a.ml[blk * 16 + n16];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
-    const float mn = fmaxf(M, ml.x);
-    const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
-    const float f1 = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - mn);
-    o = o * f0 + v * f1;
-    L = L * f0 + ml.y * f1;
-    M = mn;
+  for (int i = wave; i < per; i += NW * U) {
+    float2 ml[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool in = i + NW * k < per;
+      const size_t blk = (size_t)(first + (in ? i + NW * k : i)) * nrb + rb;
+      ml[k] = a.ml[blk * 16 + n16];
+      v[k] = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
+      if (!in) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float mn = fmaxf(M, ml[k].x);
+      const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
+      const float f1 = ml[k].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[k].x - mn);
+      o = o * f0 + v[k] * f1;
+      L = L * f0 + ml[k].y * f1;
+      M = mn;
+    }
   }
   s_o[wave][lane] = o;
   if (g4 == 0) {
@@ -582,18 +724,14 @@ __global__ __launch_bounds__(256) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
   if (r >= a.R * a.G) return;
   const int j = r / a.G, hq = kvh * a.G + r % a.G, vis = row_vis(a, b, j);
   if (vis < 0) return;                              // no such row: left as it was
-  float mx[kWaves];
   M = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    mx[w] = s_m[w][n16];
-    M = fmaxf(M, mx[w]);
-  }
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][n16]);
   o = f32x4{0.f, 0.f, 0.f, 0.f};
   L = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = mx[w] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx[w] - M);
+  for (int w = 0; w < NW; ++w) {
+    const float m = s_m[w][n16], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
     o += s_o[w][lane] * f;
     L += s_l[w][n16] * f;
   }
@@ -610,10 +748,19 @@ __global__ __launch_bounds__(256) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
 }
 
 int row_blocks(int rows) { return (rows + 15) / 16; }
-// Row blocks of a workgroup.
-int wg_blocks(int rows) {
-  const int n = row_blocks(rows), y = (n + 3) / 4;
-  return (n + y - 1) / y;
+
+// How a workgroup takes a pass's row blocks: NRB x WR of them, y workgroups.
+struct Shape {
+  int nrb, wr, y;
+};
+Shape shape_of(int rows) {
+  const int n = row_blocks(rows);
+  if (n <= 2) return {n, 1, 1};
+  return {2, 2, (n + 3) / 4};
+}
+int padded_blocks(int rows) {
+  const Shape s = shape_of(rows);
+  return s.nrb * s.wr * s.y;
 }
 
 }  // namespace
@@ -627,41 +774,40 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-int kv8_target_groups(int rows, int ncu) {
-  const int n = row_blocks(rows), y = (n + 3) / 4;
-  return std::max(1, 2 * ncu / y);
-}
+int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
 
 int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target) {
-  const int64_t pages = (int64_t)B * nkv * stride, most = ppw ? ppw : kKv8MaxPages;
+  const int64_t most = ppw ? ppw : kKv8MaxPages, least = ppw ? ppw : kKv8MinPages;
   const int64_t fixed = (int64_t)B * nkv * ((stride + most - 1) / most);
-  return ppw ? fixed : std::min(pages, std::max<int64_t>(fixed, (int64_t)target + (int64_t)B * nkv));
+  if (ppw) return fixed;
+  return std::min((int64_t)B * nkv * ((stride + least - 1) / least), std::max<int64_t>(fixed, (int64_t)target + (int64_t)B * nkv));
 }
 
-static int padded_blocks(int rows) {
-  const int n = row_blocks(rows), w = wg_blocks(rows);
-  return (n + w - 1) / w * w;
-}
 size_t kv8_part_bytes(int64_t groups, int rows, int D) { return (size_t)groups * padded_blocks(rows) * 16 * D * sizeof(float); }
 size_t kv8_ml_bytes(int64_t groups, int rows) { return (size_t)groups * padded_blocks(rows) * 16 * sizeof(float2); }
 
 hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-  const int rows = a.R * a.G, w = wg_blocks(rows);
-  const dim3 grid((unsigned)groups, padded_blocks(rows) / w);
+  const Shape h = shape_of(a.R * a.G);
   void (*f)(Kv8AttnArgs) = nullptr;
   if (D == 128)
-    f = w == 1 ? k_kv8_attn<128, 1> : w == 2 ? k_kv8_attn<128, 2> : w == 3 ? k_kv8_attn<128, 3> : k_kv8_attn<128, 4>;
+    f = h.wr == 2 ? k_kv8_attn<128, 2, 2> : h.nrb == 2 ? k_kv8_attn<128, 2, 1> : k_kv8_attn<128, 1, 1>;
   else
-    f = w == 1 ? k_kv8_attn<64, 1> : w == 2 ? k_kv8_attn<64, 2> : w == 3 ? k_kv8_attn<64, 3> : k_kv8_attn<64, 4>;
-  hipExtLaunchKernelGGL(f, grid, dim3(256), 0, s, e0, e1, 0, a);
+    f = h.wr == 2 ? k_kv8_attn<64, 2, 2> : h.nrb == 2 ? k_kv8_attn<64, 2, 1> : k_kv8_attn<64, 1, 1>;
+  hipExtLaunchKernelGGL(f, dim3((unsigned)groups, h.y), dim3(64 * h.wr * kKeyWaves), 0, s, e0, e1, 0, a);
   return hipGetLastError();
 }
 
-hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const int rows = a.R * a.G;
   const dim3 grid(a.B * a.nkv, row_blocks(rows), D / 16);
-  hipExtLaunchKernelGGL((D == 128 ? k_kv8_combine<128> : k_kv8_combine<64>), grid, dim3(256), 0, s, e0, e1, 0, a,
-                        padded_blocks(rows));
+  // few (sequence, kv head) pairs have many groups each
+  const bool many = groups >= (int64_t)32 * a.B * a.nkv;
+  void (*f)(Kv8AttnArgs, int) = nullptr;
+  if (D == 128)
+    f = many ? k_kv8_combine<128, 16> : k_kv8_combine<128, 4>;
+  else
+    f = many ? k_kv8_combine<64, 16> : k_kv8_combine<64, 4>;
+  hipExtLaunchKernelGGL(f, grid, dim3(many ? 1024 : 256), 0, s, e0, e1, 0, a, padded_blocks(rows));
   return hipGetLastError();
 }
 

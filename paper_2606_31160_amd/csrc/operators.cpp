@@ -122,7 +122,7 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   const int64_t width = (int64_t)q_heads * c->head_dim;
   if (q_stride < width || q_stride % 8 || out_stride < width || out_stride % 8)
     return fail(SPEC_E_INVAL, f, "q_stride and out_stride must be multiples of 8 and at least q_heads*head_dim");
-  if (!std::isfinite(scale)) return fail(SPEC_E_INVAL, f, "scale must be finite");
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(SPEC_E_INVAL, f, "scale must be positive and finite");
   if (!aligned(d_table, 4) || !aligned(d_packed, 4) || !aligned(d_visible, 4) || !aligned(q, 16) || !aligned(out, 16) ||
       (d_lse && !aligned(d_lse, 4)) || (d_err && !aligned(d_err, 4)))
     return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
@@ -158,7 +158,7 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   a.target = p.target;
   a.scale_log2 = scale * 1.4426950408889634f;
   const spec_status s = launched(launch_kv8_attn(a, c->head_dim, p.groups, stream), f);
-  return s != SPEC_OK ? s : launched(launch_kv8_combine(a, c->head_dim, stream), f);
+  return s != SPEC_OK ? s : launched(launch_kv8_combine(a, c->head_dim, p.groups, stream), f);
 }
 
 spec_status spec_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top, size_t* bytes) {

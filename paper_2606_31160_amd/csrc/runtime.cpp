@@ -445,13 +445,12 @@ int attn_pages_per_workgroup(const spec_config* cfg, const spec_seq_init* seqs, 
   return ppw;
 }
 
-// Pages of a group of the attention over a cache in 8 bits: as many as leave two
-// groups per CU at the prompts, which, as above, fixes it for every K.
+// Pages of a group of the attention over a cache in 8 bits: fixed by the prompts
+// alone, as above, and so the same for every K.
 int kv8_pages_per_group(const spec_config* cfg, const spec_seq_init* seqs, int ncu) {
   long long pages = 0;
   for (int b = 0; b < cfg->batch; ++b) pages += seqs[b].prefix_len / kAttnChunk + 1;
-  const long long want = (pages * cfg->target.kv_heads + 2 * ncu - 1) / (2 * ncu);
-  return (int)std::min<long long>(std::max<long long>(want, 1), kKv8MaxPages);
+  return kv8_group_pages(pages * cfg->target.kv_heads, ncu);
 }
 
 // Carves the workspace (base == nullptr only measures).  Returns total bytes.

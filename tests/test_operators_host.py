@@ -47,7 +47,7 @@ def test_attention_refuses_a_bad_cache(kw, text):
     (dict(batch=2 ** 30, rows=2 ** 30), "SPEC_MAX_ROWS"), (dict(q_heads=0), "q_heads"), (dict(q_heads=5), "q_heads"),
     (dict(table_stride=0), "table_stride"), (dict(table_stride=2 ** 30), "table_stride"), (dict(q_stride=248), "q_stride"),
     (dict(q_stride=260), "q_stride"), (dict(out_stride=255), "q_stride"), (dict(scale=float("nan")), "scale"),
-    (dict(scale=float("inf")), "scale"), (dict(q=P + 2), "misaligned"), (dict(q=0), "null"), (dict(out=P + 8), "misaligned"),
+    (dict(scale=float("inf")), "scale"), (dict(scale=0.0), "scale"), (dict(scale=-0.1), "scale"), (dict(q=P + 2), "misaligned"), (dict(q=0), "null"), (dict(out=P + 8), "misaligned"),
     (dict(d_table=0), "null"), (dict(d_packed=P + 1), "misaligned"), (dict(d_visible=0), "null"), (dict(d_lse=P + 2), "misaligned"),
     (dict(d_err=P + 2), "misaligned"), (dict(workspace=0), "workspace"), (dict(workspace=P + 16), "workspace")])
 def test_attention_refuses_bad_arguments(kw, text):
