@@ -1839,6 +1839,7 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
     p.opk = wide_o(c) ? c.Mpad / 16 : 0;
     p.part = c.kv8_part;
     p.ml = c.kv8_ml;
+    p.odd = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(c.kv8_ml) + c.kv8_ml_bytes);
     p.B = c.B;
     p.R = c.R;
     p.nq = nq;

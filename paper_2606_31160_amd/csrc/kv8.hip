@@ -220,11 +220,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// Whether a word holds a NaN code.
-__device__ __forceinline__ bool has_nan8(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
-__device__ __forceinline__ bool not_finite16(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
+// Bit 7 of every byte that is a NaN code / bits 15 and 31 for bf16 numbers that are
+// not finite.
+__device__ __forceinline__ uint32_t nan8(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t not_finite16(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ float lane_f(float x, int l) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
 }
@@ -303,8 +302,10 @@ template <int D, int NRB, int WR>
 __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kKeyWaves;
   __shared__ f32x4 s_o[2][WR][kKeyWaves][kKeyWaves - 1][ND4][64];
+  __shared__ u32x4 s_q[WR][NRB][2 * KH][64];        // Q operands: in registers they would not leave room for two pages
   __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
   __shared__ int s_tmp[WR * kKeyWaves][SPEC_MAX_ROWS];
+  __shared__ uint64_t s_odd[kKeyWaves][WR];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int n16 = lane & 15, g4 = lane >> 4;
@@ -340,7 +341,6 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // rows of this wave
   const int rows = a.R * a.G, r0 = (blockIdx.y * WR + wr) * NRB * 16;
   int vis[NRB], vmin = INT32_MAX, vmax = 0;
-  u32x4 qf[NRB][2 * KH];
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
     const int r = r0 + 16 * rb + n16;
@@ -352,9 +352,11 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     vmin = min(vmin, vis[rb]);
     vmax = max(vmax, v);
     // (a row that is not there reads one that is)
-    const bf16_t* qp = a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)hq * D + 16 * g4;
+    if (rb % kKeyWaves == wk) {
+      const bf16_t* qp = a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)hq * D + 16 * g4;
 #pragma unroll
-    for (int t = 0; t < 2 * KH; ++t) qf[rb][t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+      for (int t = 0; t < 2 * KH; ++t) s_q[wr][rb][t][lane] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+    }
   }
   for (int o = 8; o > 0; o >>= 1) {
     vmin = min(vmin, __shfl_xor(vmin, o));
@@ -421,26 +423,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[rb][i] *= f;
   };
-  // A page's values that are not finite were taken as zero where not every row sees
-  // the page, as zero probability times one is not zero: only rows that see the
-  // slot get them.
-  auto add_odd = [&](int p, bool in8) {
-    const int k0 = (p0 + p) * kAttnChunk, end = min(vmax - k0, kAttnChunk);
-    const size_t at = at_of(p);
-    for (int k = 0; k < end; ++k)
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const size_t v = at + (size_t)(16 * dt + 4 * g4 + i) * kAttnChunk + k;
-          const float x = in8 ? ((a.v8[v] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[v]);
-          if (!(fabsf(x) < INFINITY)) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb)
-              if (k0 + k < vis[rb]) st.o[rb][dt][i] += x;
-          }
-        }
-  };
+  // Pages that not every row sees, with values that are not finite: these are taken
+  // as zero here, as zero probability times one is not zero, and the combine gives
+  // them to the rows that see their slots.
+  uint64_t odd_pages = 0;
 
   uint64_t t8 = todo & mask8;
   int p = t8 ? __builtin_ctzll(t8) : 64;
@@ -448,6 +434,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     load_k(p);
     load_v(p);
   }
+  __syncthreads();                                  // s_q
   // (the scales arrive while the first page does)
   const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
   if (lane < np && (page < 0 || !fine) && a.err) *a.err = SPEC_E_INVAL;
@@ -470,6 +457,13 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const int k0 = (p0 + p) * kAttnChunk;
     const bool full = k0 + kAttnChunk <= vmin;
     float s[NRB][16];                               // scores, then probabilities, of keys 16 g4 + i
+    int ql = lane;
+    asm volatile("" : "+v"(ql));                    // (Q is read again for every page)
+    u32x4 qf[NRB][2 * KH];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int t = 0; t < 2 * KH; ++t) qf[rb][t] = s_q[wr][rb][t][ql];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       f32x4 acc[NRB];
@@ -503,25 +497,23 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
         const float* q = s[rb] + 8 * e;
         pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
       }
-    bool odd = false;
     if (!full) {
       const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;   // of this lane's 16 keys
+      uint32_t m[4], odd = 0;
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        uint32_t w[4] = {vr[dt].x, vr[dt].y, vr[dt].z, vr[dt].w};
+      for (int k = 0; k < 4; ++k) {
+        const int c = min(max(valid - 4 * k, 0), 4);
+        m[k] = (uint32_t)((1ull << (8 * c)) - 1);
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int c = min(max(valid - 4 * k, 0), 4);
-          w[k] &= c == 4 ? 0xffffffffu : (1u << (8 * c)) - 1;
-          if (has_nan8(w[k])) {
-            odd = true;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (((w[k] >> (8 * e)) & 0x7f) == 0x7f) w[k] &= ~(0xffu << (8 * e));
-          }
+          const uint32_t w = vr[dt][k] & m[k], x = nan8(w);
+          odd |= x;
+          vr[dt][k] = w & ~((x >> 7) * 0xffu);
         }
-        vr[dt] = u32x4{w[0], w[1], w[2], w[3]};
-      }
+      if (__any(odd != 0)) odd_pages |= 1ull << p;
     }
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) {
@@ -533,7 +525,6 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       }
     }
     if (next < 64) load_v(next);
-    if (__any(odd)) add_odd(p, true);
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
     p = next;
   }
@@ -544,71 +535,76 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const int k0 = (p0 + q) * kAttnChunk;
     const bool full = k0 + kAttnChunk <= vmin;
     float s[NRB][16];
+    int ql = lane;
+    asm volatile("" : "+v"(ql));
+    // all of the page's keys, then all of its values, in flight at once
+    u32x4 w[16 * KH];
     const bf16_t* kp = a.k16 + at + krow * D + 16 * g4;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int h = 0; h < 2 * KH; ++h) w[2 * KH * t + h] = ld16(kp + 4 * t * D + 64 * (h >> 1) + 8 * (h & 1));
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       f32x4 acc[NRB];
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int h = 0; h < 2 * KH; ++h) {
-        const u32x4 kk = ld16(kp + 4 * t * D + 64 * (h >> 1) + 8 * (h & 1));
+      for (int h = 0; h < 2 * KH; ++h)
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(kk, qf[rb][h], acc[rb]);
-      }
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(w[2 * KH * t + h], s_q[wr][rb][h][ql], acc[rb]);
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
     }
+    const bf16_t* vp = a.v16 + at + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) w[2 * dt + e] = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
     if (!full) mask(s, k0);
     const float off = lane_f(lv, q), far = far_of(off);
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
     soft(st, s, a.scale_log2, far != 0.f ? kHead : off + kHead);
     if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
-    const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;
-    bool odd = false;
-    const bf16_t* vp = a.v16 + at + n16 * kAttnChunk + 16 * g4;
+    uint32_t odd = 0;
+    if (!full) {
+      const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t m = (uint32_t)((1ull << (16 * min(max(valid - 8 * e - 2 * k, 0), 2))) - 1);
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const uint32_t v = w[2 * dt + e][k] & m, x = not_finite16(v);
+            odd |= x;
+            w[2 * dt + e][k] = v & ~((x >> 15) * 0xffffu);
+          }
+        }
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       u32x4 ph[NRB], pl[NRB];
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) {
         const float* pr = s[rb] + 8 * e;
-        uint32_t w[4], x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          w[k] = pack2(pr[2 * k], pr[2 * k + 1]);
-          x[k] = pack2(pr[2 * k] - __uint_as_float(w[k] << 16), pr[2 * k + 1] - __uint_as_float(w[k] & 0xffff0000u));
+          ph[rb][k] = pack2(pr[2 * k], pr[2 * k + 1]);
+          pl[rb][k] = pack2(pr[2 * k] - __uint_as_float(ph[rb][k] << 16), pr[2 * k + 1] - __uint_as_float(ph[rb][k] & 0xffff0000u));
         }
-        ph[rb] = u32x4{w[0], w[1], w[2], w[3]};
-        pl[rb] = u32x4{x[0], x[1], x[2], x[3]};
       }
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        u32x4 v = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
-        if (!full) {
-          uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = valid - 8 * e - 2 * k;
-            w[k] = c >= 2 ? w[k] : c == 1 ? w[k] & 0xffffu : 0u;
-            if (not_finite16(w[k])) {
-              odd = true;
-              if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
-              if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
-            }
-          }
-          v = u32x4{w[0], w[1], w[2], w[3]};
-        }
+      for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-          st.o[rb][dt] = mfma16x16x32(v, ph[rb], st.o[rb][dt]);
-          st.o[rb][dt] = mfma16x16x32(v, pl[rb], st.o[rb][dt]);
+          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], ph[rb], st.o[rb][dt]);
+          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], pl[rb], st.o[rb][dt]);
         }
-      }
     }
-    if (__any(odd)) add_odd(q, false);
+    if (__any(odd != 0)) odd_pages |= 1ull << q;
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
   }
 
@@ -623,6 +619,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       s_l[wk][wr][16 * rb + n16] = st.l[rb];
     }
   }
+  if (lane == 0) s_odd[wk][wr] = odd_pages;
   __syncthreads();
   const int nrb = gridDim.y * WR * NRB;             // row blocks of the partials
 #pragma unroll
@@ -662,6 +659,12 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
         }
       }
     if (wk == 0 && g4 == 0) a.ml[blk * 16 + n16] = make_float2(M, L);
+    if (wk == 0 && lane == 0) {
+      uint64_t w = 0;
+#pragma unroll
+      for (int k = 0; k < kKeyWaves; ++k) w |= s_odd[k][wr];
+      a.odd[blk] = w;
+    }
   }
 }
 
@@ -677,6 +680,10 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n16 = lane & 15, g4 = lane >> 4;
   const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
+  const int r = 16 * rb + n16;
+  const bool in_row = r < a.R * a.G;
+  const int j = in_row ? r / a.G : 0, hq = kvh * a.G + (in_row ? r % a.G : 0);
+  const int vis = in_row ? row_vis(a, b, j) : -1;
   const Groups gr = count_groups(a, s_tmp[wave]);
   int pages = 0, first = 0;
 #pragma unroll
@@ -692,17 +699,32 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   for (int i = wave; i < per; i += NW * U) {
     float2 ml[U];
     f32x4 v[U];
+    uint64_t odd[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const bool in = i + NW * k < per;
       const size_t blk = (size_t)(first + (in ? i + NW * k : i)) * nrb + rb;
       ml[k] = a.ml[blk * 16 + n16];
+      odd[k] = a.odd[blk];
       v[k] = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
       if (!in) {
         ml[k] = make_float2(-INFINITY, 0.f);
         v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        odd[k] = 0;
       }
     }
+    for (int k = 0; k < U; ++k)
+      for (uint64_t w = odd[k]; w; w &= w - 1) {    // values that are not finite, for the rows that see them
+        const int p = (i + NW * k) * gr.ppw + __builtin_ctzll(w);
+        const bool in8 = p < a.packed[b];
+        const size_t at = ((size_t)a.table[(size_t)b * a.stride + p] * a.nkv + kvh) * kAttnChunk * D;
+        for (int key = 0; key < kAttnChunk; ++key)
+          for (int e = 0; e < 4; ++e) {
+            const size_t c = at + (size_t)(16 * dt + 4 * g4 + e) * kAttnChunk + key;
+            const float x = in8 ? ((a.v8[c] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[c]);
+            if (!(fabsf(x) < INFINITY) && p * kAttnChunk + key < vis) o[e] += x;
+          }
+      }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const float mn = fmaxf(M, ml[k].x);
@@ -720,9 +742,6 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   }
   __syncthreads();
   if (wave != 0) return;
-  const int r = 16 * rb + n16;
-  if (r >= a.R * a.G) return;
-  const int j = r / a.G, hq = kvh * a.G + r % a.G, vis = row_vis(a, b, j);
   if (vis < 0) return;                              // no such row: left as it was
   M = -INFINITY;
 #pragma unroll

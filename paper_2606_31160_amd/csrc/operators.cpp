@@ -54,7 +54,7 @@ const char* bad_pass(const spec_kv8* c, int32_t batch, int32_t rows, int32_t q_h
 struct AttnPlan {
   int target;
   int64_t groups;
-  size_t ml, bytes;   // offset of the maxima and sums; all
+  size_t ml, odd, bytes;   // offsets of the maxima and sums and of the odd pages; all
 };
 AttnPlan attn_plan(const spec_kv8* c, int batch, int rows, int q_heads, int stride) {
   const int r = rows * (q_heads / c->kv_heads);
@@ -62,7 +62,8 @@ AttnPlan attn_plan(const spec_kv8* c, int batch, int rows, int q_heads, int stri
   p.target = kv8_target_groups(r, num_cus());
   p.groups = kv8_max_groups(batch, c->kv_heads, stride, 0, p.target);
   p.ml = align_up(kv8_part_bytes(p.groups, r, c->head_dim));
-  p.bytes = p.ml + align_up(kv8_ml_bytes(p.groups, r));
+  p.odd = p.ml + align_up(kv8_ml_bytes(p.groups, r));
+  p.bytes = p.odd + align_up(kv8_ml_bytes(p.groups, r) / 16);
   return p;
 }
 
@@ -150,6 +151,7 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   a.err = d_err;
   a.part = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml);
+  a.odd = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + p.odd);
   a.B = batch;
   a.R = rows;
   a.nq = q_heads;
