@@ -52,18 +52,11 @@ struct Kv8AttnArgs {
 
 constexpr int kKv8MinPages = 4, kKv8MaxPages = 64;   // pages of a group
 
-// Pages of a group where the lengths decide: `pages` (of all sequences and kv
-// heads) in about `target` groups.
-__host__ __device__ inline int kv8_group_pages(int64_t pages, int target) {
-  const int64_t want = (pages + target - 1) / target;
-  return (int)(want < kKv8MinPages ? kKv8MinPages : want > kKv8MaxPages ? kKv8MaxPages : want);
-}
-
 // Groups of a call at most (the grid), the partials' bytes, the groups a call without a fixed `ppw` aims at.
 int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target);
 size_t kv8_part_bytes(int64_t groups, int rows, int D);
 size_t kv8_ml_bytes(int64_t groups, int rows);     // of ml; odd takes a sixteenth of it
-int kv8_target_groups(int rows, int ncu);
+int kv8_target_groups(int rows, int ncu);   // (what runs at once)
 hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0 = nullptr,
                            hipEvent_t e1 = nullptr);
 hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0 = nullptr,

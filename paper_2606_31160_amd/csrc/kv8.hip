@@ -118,84 +118,118 @@ __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
 
 constexpr int kKeyWaves = 4;    // waves that share a group's pages: wave w takes pages w, w + 4, ..
 
-// Slots that row j of sequence b sees; negative: no such row.
-__device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, int b, int j) {
-  if (!a.st) return a.vis[b * a.R + j];
-  const SeqState& s = a.st[b];
-  return j < s.count ? s.base + (j < s.causal ? j + 1 : s.count) : -1;
+// Sums and maxima over a wave, and its running sum, by lane moves within the
+// vector unit (row shifts, then the last lane of each row of 16 to the next rows).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_max(int x) {   // x >= 0
+  return max(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
+}
+__device__ __forceinline__ int wave_max(int x) {
+  x = dpp_max<0x111, 0xf>(x);
+  x = dpp_max<0x112, 0xf>(x);
+  x = dpp_max<0x114, 0xf>(x);
+  x = dpp_max<0x118, 0xf>(x);
+  x = dpp_max<0x142, 0xa>(x);
+  return __builtin_amdgcn_readlane(dpp_max<0x143, 0xc>(x), 63);
+}
+// Over the 16 lanes of a row, in all of them.
+__device__ __forceinline__ int row_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false));
+  return max(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false));
 }
 
-// Pages of sequences lane, lane + 64 and lane + 128; tmp: LDS of SPEC_MAX_ROWS
-// words of this wave's own.
-__device__ __forceinline__ void seq_pages(const Kv8AttnArgs& a, int (&pages)[3], int* tmp) {
+// The groups of a call.  They are numbered sequence by sequence, then by pages,
+// then by kv head.  Every wave of a workgroup counts them for itself, lane l
+// sequences l, l + 64 and l + 128; vis: LDS of SPEC_MAX_ROWS words of its own.
+struct Groups {
+  int ppw;
+  int pages[3], first[3];   // of sequence lane + 64 i: pages, number of its first group
+  int total;
+  int base, count, causal;  // of sequence lane (a context's)
+};
+
+__device__ __forceinline__ Groups count_groups(const Kv8AttnArgs& a, int* vis) {
   const int lane = threadIdx.x & 63;
+  Groups g;
   int end[3] = {0, 0, 0};
   if (a.st) {
-    if (lane < a.B) {
-      const SeqState& s = a.st[lane];
-      end[0] = s.count > 0 ? s.base + s.count : 0;
-    }
+    const SeqState& s = a.st[min(lane, a.B - 1)];
+    g.base = s.base, g.count = s.count, g.causal = s.causal;
+    end[0] = lane < a.B && g.count > 0 ? g.base + g.count : 0;
   } else {
     const int n = a.B * a.R;
     int v[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) v[i] = lane + 64 * i < n ? a.vis[lane + 64 * i] : 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (lane + 64 * i < n) vis[lane + 64 * i] = v[i];
     if (a.R == 1) {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) end[i] = v[i];
+      for (int i = 0; i < 3; ++i) end[i] = max(v[i], 0);
     } else if (a.B == 1) {
-      int m = max(max(v[0], v[1]), v[2]);
-      for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o));
+      const int m = wave_max(max(max(v[0], v[1]), max(v[2], 0)));
       end[0] = lane == 0 ? m : 0;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-        if (lane + 64 * i < n) tmp[lane + 64 * i] = v[i];
+    } else {                                        // at most 80 sequences
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
+      for (int i = 0; i < 2; ++i)
         if (lane + 64 * i < a.B)
-          for (int j = 0; j < a.R; ++j) end[i] = max(end[i], tmp[(lane + 64 * i) * a.R + j]);
+          for (int j = 0; j < a.R; ++j) end[i] = max(end[i], vis[(lane + 64 * i) * a.R + j]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < 3; ++i) pages[i] = min((max(end[i], 0) + kAttnChunk - 1) / kAttnChunk, a.stride);
-}
-
-// Groups are numbered sequence by sequence, a sequence's kv head by kv head.
-// Every wave of a workgroup counts them for itself.
-struct Groups {
-  int ppw;
-  int pages[3], first[3];   // of sequence lane + 64 i: pages, number of its first group
-  int total;
-};
-
-__device__ __forceinline__ Groups count_groups(const Kv8AttnArgs& a, int* tmp) {
-  const int lane = threadIdx.x & 63;
-  Groups g;
-  seq_pages(a, g.pages, tmp);
+  for (int i = 0; i < 3; ++i)
+    g.pages[i] = min((int)(((unsigned)end[i] + kAttnChunk - 1) / kAttnChunk), a.stride);
+  auto sum = [&](int ppw) {                         // groups of ppw pages; first[] on the way
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      g.first[i] = before;
+      if (64 * i >= a.B) continue;
+      const int n = a.nkv * (int)(((unsigned)g.pages[i] + ppw - 1) / ppw), x = wave_scan(n);
+      g.first[i] = before + x - n;
+      before += __builtin_amdgcn_readlane(x, 63);
+    }
+    return before;
+  };
   g.ppw = a.ppw;
   if (g.ppw == 0) {
-    int all = g.pages[0] + g.pages[1] + g.pages[2];
-    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
-    g.ppw = kv8_group_pages((int64_t)all * a.nkv, a.target);
-  }
-  int before = 0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    g.first[i] = before;
-    if (64 * i >= a.B) continue;
-    const int n = a.nkv * ((g.pages[i] + g.ppw - 1) / g.ppw);
-    int sum = n;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(sum, o);
-      if (lane >= o) sum += x;
+    // as few pages as leave no more groups than run at once
+    g.ppw = kKv8MinPages;
+    g.total = sum(g.ppw);
+    if (g.total > a.target) {
+      g.ppw = min(max(g.total / a.target, 1) * kKv8MinPages, kKv8MaxPages);
+      while ((g.total = sum(g.ppw)) > a.target && g.ppw < kKv8MaxPages && a.B * a.nkv <= a.target) g.ppw += kKv8MinPages;
     }
-    g.first[i] = before + sum - n;
-    before += __shfl(sum, 63);
+  } else {
+    g.total = sum(g.ppw);
   }
-  g.total = before;
+  g.ppw = __builtin_amdgcn_readfirstlane(g.ppw);    // (all uniform, as the compiler cannot see)
+  g.total = __builtin_amdgcn_readfirstlane(g.total);
   return g;
+}
+
+// Slots that row j of sequence b sees; negative: no such row.
+__device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, const Groups& g, const int* vis, int b, int j) {
+  if (!a.st) return vis[b * a.R + j];
+  const int base = __builtin_amdgcn_readlane(g.base, b), count = __builtin_amdgcn_readlane(g.count, b);
+  const int causal = __builtin_amdgcn_readlane(g.causal, b);
+  return j < count ? base + (j < causal ? j + 1 : count) : -1;
 }
 
 __device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi) {
@@ -304,12 +338,12 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   __shared__ f32x4 s_o[2][WR][kKeyWaves][kKeyWaves - 1][ND4][64];
   __shared__ u32x4 s_q[WR][NRB][2 * KH][64];        // Q operands: in registers they would not leave room for two pages
   __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
-  __shared__ int s_tmp[WR * kKeyWaves][SPEC_MAX_ROWS];
+  __shared__ int s_vis[WR * kKeyWaves][SPEC_MAX_ROWS];
   __shared__ uint64_t s_odd[kKeyWaves][WR];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int n16 = lane & 15, g4 = lane >> 4;
-  const Groups gr = count_groups(a, s_tmp[wave]);
+  const Groups gr = count_groups(a, s_vis[wave]);
   const int id = blockIdx.x;
   if (id >= gr.total) return;
   int b = 0, pages = 0, first = 0;
@@ -326,9 +360,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   }
   b = __builtin_amdgcn_readfirstlane(b);
   pages = __builtin_amdgcn_readfirstlane(pages);
-  const int per = (pages + gr.ppw - 1) / gr.ppw;
-  const int kvh = __builtin_amdgcn_readfirstlane((id - first) / per);
-  const int p0 = __builtin_amdgcn_readfirstlane((id - first) % per * gr.ppw);   // first page
+  first = __builtin_amdgcn_readfirstlane(first);
+  const int grp = __builtin_amdgcn_readfirstlane((unsigned)(id - first) / (unsigned)a.nkv), kvh = id - first - grp * a.nkv;
+  const int p0 = grp * gr.ppw;                      // first page
   const int np = min(gr.ppw, pages - p0);
   const int packed = min(max(a.packed[b], 0), a.stride);
   const int n8 = min(max(packed - p0, 0), np);
@@ -346,7 +380,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const int r = r0 + 16 * rb + n16;
     const bool in = r < rows;
     const int j = in ? r / a.G : 0, hq = kvh * a.G + (in ? r % a.G : 0);
-    const int v = in ? row_vis(a, b, j) : -1;
+    const int v = in ? row_vis(a, gr, s_vis[wave], b, j) : -1;
     if (v > a.stride * kAttnChunk && a.err) *a.err = SPEC_E_INVAL;
     vis[rb] = v < 0 ? INT32_MAX : v;                // rows that nobody asked for need no mask
     vmin = min(vmin, vis[rb]);
@@ -358,12 +392,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       for (int t = 0; t < 2 * KH; ++t) s_q[wr][rb][t][lane] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
     }
   }
-  for (int o = 8; o > 0; o >>= 1) {
-    vmin = min(vmin, __shfl_xor(vmin, o));
-    vmax = max(vmax, __shfl_xor(vmax, o));
-  }
-  vmin = __builtin_amdgcn_readfirstlane(vmin);
-  vmax = __builtin_amdgcn_readfirstlane(vmax);      // slots that no row of this wave sees: from here
+  vmin = ~__builtin_amdgcn_readfirstlane(row_max(~vmin));
+  vmax = __builtin_amdgcn_readfirstlane(row_max(vmax));      // slots that no row of this wave sees: from here
 
   // pages that may be read, and those that this wave has to
   if (page < 0 || page >= (lane < n8 ? a.pages8 : a.pages16)) page = -1;
@@ -401,12 +431,12 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
   };
-  auto mask = [&](float (&s)[NRB][16], int k0) {
+  auto mask = [&](float (&s)[NRB][16], int k0, int end) {
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (k0 + 16 * g4 + i >= vis[rb]) s[rb][i] = -INFINITY;
+        if (k0 + 16 * g4 + i >= min(vis[rb], end)) s[rb][i] = -INFINITY;
   };
   auto turn_o = [&](float f) {
 #pragma unroll
@@ -434,7 +464,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     load_k(p);
     load_v(p);
   }
-  __syncthreads();                                  // s_q
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // s_q, with pages on their way
   // (the scales arrive while the first page does)
   const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
   if (lane < np && (page < 0 || !fine) && a.err) *a.err = SPEC_E_INVAL;
@@ -446,16 +476,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   while (p < 64) {
     t8 &= t8 - 1;
     const int next = t8 ? __builtin_ctzll(t8) : 64;
-    if (!(good >> p & 1)) {                         // a page without scales: not visible
-      if (next < 64) {
-        load_k(next);
-        load_v(next);
-      }
-      p = next;
-      continue;
-    }
     const int k0 = (p0 + p) * kAttnChunk;
-    const bool full = k0 + kAttnChunk <= vmin;
+    const bool sound = good >> p & 1;               // else a page without scales: not visible
+    const bool full = sound && k0 + kAttnChunk <= vmin;
     float s[NRB][16];                               // scores, then probabilities, of keys 16 g4 + i
     int ql = lane;
     asm volatile("" : "+v"(ql));                    // (Q is read again for every page)
@@ -484,8 +507,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
         for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
     }
     if (next < 64) load_k(next);
-    if (!full) mask(s, k0);
-    const float off = lane_f(lv, p), far = far_of(off);
+    if (!full) mask(s, k0, sound ? INT32_MAX : 0);
+    const float off = sound ? lane_f(lv, p) : 0.f, far = far_of(off);
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
     soft(st, s, fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f), far != 0.f ? kHead : off + kHead);
     if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
@@ -498,7 +521,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
         pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
       }
     if (!full) {
-      const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;   // of this lane's 16 keys
+      const int valid = (sound ? min(vmax - k0, kAttnChunk) : 0) - 16 * g4;   // of this lane's 16 keys
       uint32_t m[4], odd = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -563,7 +586,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) w[2 * dt + e] = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
-    if (!full) mask(s, k0);
+    if (!full) mask(s, k0, INT32_MAX);
     const float off = lane_f(lv, q), far = far_of(off);
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
     soft(st, s, a.scale_log2, far != 0.f ? kHead : off + kHead);
@@ -676,15 +699,15 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   constexpr int NDT = D / 16, U = 4;
   __shared__ f32x4 s_o[NW][64];
   __shared__ float s_m[NW][16], s_l[NW][16];
-  __shared__ int s_tmp[NW][SPEC_MAX_ROWS];
+  __shared__ int s_vis[NW][SPEC_MAX_ROWS];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n16 = lane & 15, g4 = lane >> 4;
   const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
   const int r = 16 * rb + n16;
   const bool in_row = r < a.R * a.G;
   const int j = in_row ? r / a.G : 0, hq = kvh * a.G + (in_row ? r % a.G : 0);
-  const int vis = in_row ? row_vis(a, b, j) : -1;
-  const Groups gr = count_groups(a, s_tmp[wave]);
+  const Groups gr = count_groups(a, s_vis[wave]);
+  const int vis = in_row ? row_vis(a, gr, s_vis[wave], b, j) : -1;
   int pages = 0, first = 0;
 #pragma unroll
   for (int i = 0; i < 3; ++i)
@@ -693,7 +716,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
       first = __builtin_amdgcn_readlane(gr.first[i], b & 63);
     }
   const int per = (pages + gr.ppw - 1) / gr.ppw;
-  first += kvh * per;
+  first += kvh;
   float M = -INFINITY, L = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int i = wave; i < per; i += NW * U) {
@@ -703,7 +726,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const bool in = i + NW * k < per;
-      const size_t blk = (size_t)(first + (in ? i + NW * k : i)) * nrb + rb;
+      const size_t blk = ((size_t)first + (size_t)(in ? i + NW * k : i) * a.nkv) * nrb + rb;
       ml[k] = a.ml[blk * 16 + n16];
       odd[k] = a.odd[blk];
       v[k] = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
@@ -793,13 +816,20 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
+// Workgroups that run at once: one of 8 waves or two of 4 waves a CU.
+int kv8_target_groups(int rows, int ncu) {
+  const Shape s = shape_of(rows);
+  return std::max(1, 2 * ncu / (s.wr * s.y));
+}
 
+// Where the lengths decide, count_groups stops at `target`, or at kKv8MaxPages, or
+// (with more heads of sequences than that) takes 4 floor(n / target) pages where n
+// groups of 4 were: at most 2 target and one shorter group for each of them.
 int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target) {
   const int64_t most = ppw ? ppw : kKv8MaxPages, least = ppw ? ppw : kKv8MinPages;
   const int64_t fixed = (int64_t)B * nkv * ((stride + most - 1) / most);
   if (ppw) return fixed;
-  return std::min((int64_t)B * nkv * ((stride + least - 1) / least), std::max<int64_t>(fixed, (int64_t)target + (int64_t)B * nkv));
+  return std::min((int64_t)B * nkv * ((stride + least - 1) / least), std::max<int64_t>(fixed, 2 * (int64_t)target + (int64_t)B * nkv));
 }
 
 size_t kv8_part_bytes(int64_t groups, int rows, int D) { return (size_t)groups * padded_blocks(rows) * 16 * D * sizeof(float); }

@@ -448,9 +448,12 @@ int attn_pages_per_workgroup(const spec_config* cfg, const spec_seq_init* seqs, 
 // Pages of a group of the attention over a cache in 8 bits: fixed by the prompts
 // alone, as above, and so the same for every K.
 int kv8_pages_per_group(const spec_config* cfg, const spec_seq_init* seqs, int ncu) {
-  long long pages = 0;
-  for (int b = 0; b < cfg->batch; ++b) pages += seqs[b].prefix_len / kAttnChunk + 1;
-  return kv8_group_pages(pages * cfg->target.kv_heads, ncu);
+  // a multiple of kKv8MinPages that leaves no more groups than CUs
+  for (int ppw = kKv8MinPages;; ppw += kKv8MinPages) {
+    long long groups = 0;
+    for (int b = 0; b < cfg->batch; ++b) groups += cfg->target.kv_heads * (long long)(seqs[b].prefix_len / (kAttnChunk * ppw) + 1);
+    if (groups <= ncu || ppw >= kKv8MaxPages || (long long)cfg->batch * cfg->target.kv_heads > ncu) return ppw;
+  }
 }
 
 // Carves the workspace (base == nullptr only measures).  Returns total bytes.
