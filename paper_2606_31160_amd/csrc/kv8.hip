@@ -11,6 +11,7 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "kv8.h"
@@ -19,8 +20,18 @@ namespace specdec {
 
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// e with 2^e the smallest power of two such that big <= 448 2^e (0 for big = 0); big = f
+// 2^x with f in [1/2, 1), and 448 = 7/8 2^9.
+__device__ __forceinline__ int scale_exponent(float big) {
+  int x;
+  const float f = frexpf(big, &x);
+  return big > 0.f ? max(f <= 0.875f ? x - 9 : x - 8, -126) : 0;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }   // |e| <= 126
 
 // ---------------------------------------------------------------------------
 // Packing: one workgroup of 256 threads per (page, kv head, keys / values).  Keys
@@ -70,13 +81,10 @@ __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
   __syncthreads();
   big = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  // big = f 2^e with f in [1/2, 1): 448 = 7/8 2^9
-  int e;
-  const float f = frexpf(big, &e);
-  e = big > 0.f ? max(f <= 0.875f ? e - 9 : e - 8, -126) : 0;
-  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);   // 2^-e, e in [-126, 120]
+  const int e = scale_exponent(big);                // in [-126, 120]
+  const float inv = power_of_two(-e);
   const size_t pg = (size_t)page * a.nkv + h;
-  if (threadIdx.x == 0) (val ? a.vs : a.ks)[pg] = __uint_as_float((uint32_t)(127 + e) << 23);
+  if (threadIdx.x == 0) (val ? a.vs : a.ks)[pg] = power_of_two(e);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int i = threadIdx.x + 256 * u, off = i / KC, c = i % KC;
@@ -247,7 +255,7 @@ __device__ __forceinline__ u32x4 f16_of_e4m3(uint32_t lo, uint32_t hi) {
                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
   return __builtin_bit_cast(u32x4, r);
 }
-typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), f16x2));
 }
@@ -262,6 +270,9 @@ __device__ __forceinline__ float lane_f(float x, int l) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
 }
 
+// A barrier for data in LDS that leaves loads from memory in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // The softmax state of a wave's rows (lane: row lane & 15 of each block).
 template <int NRB, int NDT>
 struct RowState {
@@ -269,31 +280,34 @@ struct RowState {
   f32x4 o[NRB][NDT];
 };
 
-constexpr float kGrow = 8.f, kHead = 7.f;
+constexpr float kHead = 7.f;    // probabilities are held 2^7 times as large
 
-// Scores s of 16 keys per lane -> probabilities 2^(s sc - m + off), and l.  The
-// maximum follows only when a row's scores pass it by 2^8, so that the sums are
-// seldom rescaled and lanes seldom compared: a probability is at most 2^(8 + off).
-template <int NRB, int NDT>
-__device__ __forceinline__ void soft(RowState<NRB, NDT>& st, float (&s)[NRB][16], float sc, float off) {
-  bool grow = false;
+// Scores s of 16 keys per lane -> probabilities 2^(s sc - m + off), handed to put, and
+// l.  The maximum m follows only when a row's scores pass it by 2^8: until then O is not
+// rescaled and lanes are not compared, and a probability is at most 2^(8 + off), which
+// fits fp16 (off <= 7 there).  A row's sums depend on no other row.  (A maximum that
+// passes NaN on, as the row's sums do anyway, takes one instruction for three.)
+template <int NRB, int NDT, class Put>
+__device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NRB][16], const float (&sc)[NRB], float off,
+                                     Put put) {
   float pm[NRB];
+  bool grow = false;
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
-    pm[rb] = s[rb][0];
+    float x = s[rb][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) pm[rb] = fmaxf(pm[rb], s[rb][i]);
-    grow |= pm[rb] * sc > st.m[rb] + kGrow;
+    for (int i = 1; i < 16; ++i) x = __builtin_elementwise_maximum(x, s[rb][i]);
+    pm[rb] = x * sc[rb];
+    grow |= pm[rb] > st.m[rb] + 8.f;
   }
   if (__any(grow)) {
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 16));
       pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 32));
-      const float mn = pm[rb] * sc;
-      if (mn > st.m[rb] + kGrow) {                  // (a row's own matter: the others' sums stay as they are)
-        const float alpha = st.m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[rb] - mn);
-        st.m[rb] = mn;
+      if (pm[rb] > st.m[rb] + 8.f) {
+        const float alpha = st.m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[rb] - pm[rb]);
+        st.m[rb] = pm[rb];
         st.l[rb] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= alpha;
@@ -304,39 +318,57 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, float (&s)[NRB][16]
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
     const float c = off - (st.m[rb] == -INFINITY ? 0.f : st.m[rb]);   // no key seen yet: all probabilities zero
-    float ls = 0.f;
+    float p[16], ls = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[rb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i], sc, c));
-      ls += s[rb][i];
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i], sc[rb], c));
+      ls += p[i];
     }
+    put(rb, p);
     st.l[rb] = __builtin_fmaf(ls, back, st.l[rb]);
   }
+}
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ i32x8 join8(u32x4 a, u32x4 b) {
+  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// 16x16x128 MFMA of e4m3 operands, lane's 32 bytes in any order that both share; the
+// second operand's numbers times 2^(EB - 127).
+template <int EB>
+__device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127, 0, EB);
 }
 
 // grid (groups, row blocks / (NRB WR)), WR x 4 waves: wave w has row blocks NRB (w %
 // WR) .. and pages w / WR, + 4, .. of the group.
 //
-// S^T = K Q^T and O^T = V^T P^T by 16x16x32 MFMA, lane (n = lane & 15, g = lane >> 4)
-// holding row n.  Row i of key tile t is key 16 (i >> 2) + 4 t + (i & 3): the 16
-// scores of a lane belong to the consecutive keys 16 g .. 16 g + 15, one 16-byte read
-// of a value row; and a lane's 16 bytes of a key row serve two steps over the head
-// dimension, whose order is the same in Q's operand.  The next page's keys are
-// loaded while this one's softmax runs, its values while the next scores are formed.
-//   Keys are read as bf16, like Q.  Values and probabilities are read as fp16: an
-// e4m3 code is exact in it, and a probability keeps 11 bits, as a rounding to bf16
-// would show in the bf16 result.  The value scale is part of the probability's
-// exponent: with u the largest one of the group, p vs / u 2^7 is in fp16's normal
-// range down to 2^-21 (a page whose scale is further below u has O turned to its
-// own unit for as long).  bf16 pages take their values as they are and each
-// probability as the sum of two bf16 numbers.
+// S^T = K Q^T and O^T = V^T P^T, lane (n = lane & 15, g = lane >> 4) holding row n.  Row
+// i of key tile t is key 16 (i >> 2) + 4 t + (i & 3): the 16 scores of a lane belong to
+// the consecutive keys 16 g .. 16 g + 15, one 16-byte read of a value row; and a
+// lane's 16 bytes of a key row serve whatever part of the head dimension, whose order
+// is the same in Q's operand.  The next page's keys are loaded while this one's
+// softmax runs, its values while the next scores are formed.
+//   Keys of head dimension 128 go to the matrix unit as they are, in 16x16x128 MFMA of
+// e4m3 numbers: Q = 2^e (hi + lo / 16) with hi = e4m3(Q / 2^e) and lo the rest, four
+// bits each, which is all of a bf16 number (but for what lies 2^-22 below the row's
+// largest).  For 64 they are read as bf16, like Q.
+//   Values and probabilities are read as fp16: an e4m3 code is exact in it, and a
+// probability keeps 11 bits, as a rounding to bf16 would show in the bf16 result.
+// The value scale is part of the probability's exponent: with u the largest one of
+// the group, p vs / u 2^7 is in fp16's normal range down to 2^-21 (a page whose scale
+// is further below u has O turned to its own unit for as long).  bf16 pages take
+// their values as they are and each probability as the sum of two bf16 numbers.
 //   Which pages share a wave depends on the group only, and a row's sums on no
 // other row, so contexts that differ in K, and so in NRB and WR, sum alike.
 template <int D, int NRB, int WR>
 __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kKeyWaves;
-  __shared__ f32x4 s_o[2][WR][kKeyWaves][kKeyWaves - 1][ND4][64];
-  __shared__ u32x4 s_q[WR][NRB][2 * KH][64];        // Q operands: in registers they would not leave room for two pages
+  constexpr bool kNative = D == 128;                // keys as e4m3 operands
+  __shared__ f32x4 s_o[WR][kKeyWaves][NDT][64];
+  // Q operands, bf16 and e4m3 (hi, lo): in registers they would not leave room for two pages
+  __shared__ u32x4 s_q[WR][NRB][2 * KH][64], s_q8[kNative ? WR : 1][kNative ? NRB : 1][2 * KH][64];
+  __shared__ float s_qs[WR][NRB * 16];              // 2^e of every row
   __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
   __shared__ int s_vis[WR * kKeyWaves][SPEC_MAX_ROWS];
   __shared__ uint64_t s_odd[kKeyWaves][WR];
@@ -367,14 +399,14 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   const int packed = min(max(a.packed[b], 0), a.stride);
   const int n8 = min(max(packed - p0, 0), np);
 
-  // lane l: the group's l-th page and its scales
+  // lane l: the group's l-th page
   int page = -1;
-  float ks = 1.f, vsc = 1.f;
   if (lane < np) page = a.table[(size_t)b * a.stride + p0 + lane];
 
   // rows of this wave
   const int rows = a.R * a.G, r0 = (blockIdx.y * WR + wr) * NRB * 16;
   int vis[NRB], vmin = INT32_MAX, vmax = 0;
+  u32x4 q[2 * KH];                                  // of row block wk
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
     const int r = r0 + 16 * rb + n16;
@@ -386,10 +418,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     vmin = min(vmin, vis[rb]);
     vmax = max(vmax, v);
     // (a row that is not there reads one that is)
-    if (rb % kKeyWaves == wk) {
+    if (rb == wk) {
       const bf16_t* qp = a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)hq * D + 16 * g4;
 #pragma unroll
-      for (int t = 0; t < 2 * KH; ++t) s_q[wr][rb][t][lane] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+      for (int t = 0; t < 2 * KH; ++t) q[t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
     }
   }
   vmin = ~__builtin_amdgcn_readfirstlane(row_max(~vmin));
@@ -397,12 +429,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 
   // pages that may be read, and those that this wave has to
   if (page < 0 || page >= (lane < n8 ? a.pages8 : a.pages16)) page = -1;
-  if (lane < n8 && page >= 0) {
-    ks = a.ks[(size_t)page * a.nkv + kvh];
-    vsc = a.vs[(size_t)page * a.nkv + kvh];
-  }
+  if (lane < np && page < 0 && a.err) *a.err = SPEC_E_INVAL;
   const int seen = vmax <= p0 * kAttnChunk ? 0 : min(np, (vmax - p0 * kAttnChunk + kAttnChunk - 1) / kAttnChunk);
-  uint64_t todo = __ballot(lane < seen && page >= 0 && lane % kKeyWaves == wk);
+  const uint64_t todo = __ballot(lane < seen && page >= 0 && lane % kKeyWaves == wk);
   const uint64_t mask8 = n8 >= 64 ? ~0ull : (1ull << n8) - 1;
 
   RowState<NRB, NDT> st;
@@ -415,19 +444,27 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   }
 
   const int krow = 16 * (n16 >> 2) + (n16 & 3);     // key of this lane in tile 0
-  u32x4 kr[4][KH], vr[NDT];
+  // a page on its way: per key tile the lane's bytes of its key (both halves of the head dimension side by side for
+  // the 128-wide operand), per 16 dimensions those of its value row
+  typedef std::conditional_t<kNative, i32x8, u32x4> KeyBytes;
+  KeyBytes kr[4];
+  u32x4 vr[NDT];
   auto at_of = [&](int p) {                         // element of the page's first key or value
     return ((size_t)__builtin_amdgcn_readlane(page, p) * a.nkv + kvh) * kAttnChunk * D;
   };
-  auto load_k = [&](int p) {
-    const uint8_t* kp = a.k8 + at_of(p) + krow * D + 16 * g4;
+  auto load_k = [&](size_t at) {
+    const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int h = 0; h < KH; ++h) kr[t][h] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * h);
+    for (int t = 0; t < 4; ++t) {
+      const u32x4* k = reinterpret_cast<const u32x4*>(kp + 4 * t * D);
+      if constexpr (kNative)
+        kr[t] = join8(k[0], k[4]);
+      else
+        kr[t] = k[0];
+    }
   };
-  auto load_v = [&](int p) {
-    const uint8_t* vp = a.v8 + at_of(p) + n16 * kAttnChunk + 16 * g4;
+  auto load_v = [&](size_t at) {
+    const uint8_t* vp = a.v8 + at + n16 * kAttnChunk + 16 * g4;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
   };
@@ -447,115 +484,184 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // A page whose unit is far from u: O is turned by 2^far while it is added, and
   // what 2^60 leaves (seen in no sound cache) is taken by the probabilities.
   auto far_of = [](float off) { return fabsf(off) > 16.f ? fminf(fmaxf(-off, -60.f), 60.f) : 0.f; };
-  auto times = [](float (&s)[NRB][16], float f) {
+  // Q's operands into LDS, by the wave that loaded them.
+  auto stage_q = [&] {
+    if (wk >= NRB) return;
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
+    for (int t = 0; t < 2 * KH; ++t) s_q[wr][wk][t][lane] = q[t];
+    if constexpr (kNative) {
+      // 2^e: the smallest power of two with max |q| <= 448 2^e, as for a page
+      float big = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[rb][i] *= f;
+      for (int t = 0; t < 2 * KH; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x = fabsf(__uint_as_float(q[t][k] << 16)), y = fabsf(__uint_as_float(q[t][k] & 0xffff0000u));
+          big = fmaxf(big, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
+        }
+      big = fmaxf(big, __shfl_xor(big, 16));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const int e = scale_exponent(big);
+      const float inv = power_of_two(-e);
+      if (g4 == 0) s_qs[wr][16 * wk + n16] = power_of_two(e);
+#pragma unroll
+      for (int h = 0; h < KH; ++h) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float y[4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w = q[2 * h + (k >> 1)][2 * (k & 1) + i];
+            const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
+            y[2 * i] = fabsf(x0) < INFINITY ? x0 * inv : NAN;
+            y[2 * i + 1] = fabsf(x1) < INFINITY ? x1 * inv : NAN;
+          }
+          int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+          c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+          const f32x2 d0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), d1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+          hi[k] = (uint32_t)c;
+          c = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - d0.x) * 16.f, (y[1] - d0.y) * 16.f, 0, false);
+          lo[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32((y[2] - d1.x) * 16.f, (y[3] - d1.y) * 16.f, c, true);
+        }
+        s_q8[wr][wk][h][lane] = u32x4{hi[0], hi[1], hi[2], hi[3]};
+        s_q8[wr][wk][KH + h][lane] = u32x4{lo[0], lo[1], lo[2], lo[3]};
+      }
+    }
   };
   // Pages that not every row sees, with values that are not finite: these are taken
   // as zero here, as zero probability times one is not zero, and the combine gives
   // them to the rows that see their slots.
   uint64_t odd_pages = 0;
+  float u = 1.f, lv = 0.f;                          // unit of O; lane l: log2 of the l-th page's value scale / u
 
-  uint64_t t8 = todo & mask8;
-  int p = t8 ? __builtin_ctzll(t8) : 64;
-  if (p < 64) {
-    load_k(p);
-    load_v(p);
-  }
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // s_q, with pages on their way
-  // (the scales arrive while the first page does)
-  const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
-  if (lane < np && (page < 0 || !fine) && a.err) *a.err = SPEC_E_INVAL;
-  const uint64_t good = __ballot(fine);
-  float u = lane < n8 && page >= 0 && fine ? vsc : 0.f;
-  for (int o = 32; o > 0; o >>= 1) u = fmaxf(u, __shfl_xor(u, o));
-  if (u == 0.f) u = 1.f;
-  const float lv = (lane < n8 ? log2f(vsc) : 0.f) - log2f(u);   // lane l: of the group's l-th page
-  while (p < 64) {
-    t8 &= t8 - 1;
-    const int next = t8 ? __builtin_ctzll(t8) : 64;
-    const int k0 = (p0 + p) * kAttnChunk;
-    const bool sound = good >> p & 1;               // else a page without scales: not visible
-    const bool full = sound && k0 + kAttnChunk <= vmin;
-    float s[NRB][16];                               // scores, then probabilities, of keys 16 g4 + i
-    int ql = lane;
-    asm volatile("" : "+v"(ql));                    // (Q is read again for every page)
-    u32x4 qf[NRB][2 * KH];
+  if (n8 > 0 && a.pages8 > 0) {                     // workgroup-uniform
+    uint64_t t8 = todo & mask8;
+    int p = t8 ? __builtin_ctzll(t8) : 64;
+    const size_t sl = (size_t)max(lane < n8 ? page : 0, 0) * a.nkv + kvh;
+    const float ks = a.ks[sl], vsc = a.vs[sl];
+    // (without a page to do, the pool's first: loads outside a branch can be awaited one by one)
+    const size_t at0 = p < 64 ? at_of(p) : (size_t)kvh * kAttnChunk * D;
+    load_k(at0);
+    load_v(at0);
+    stage_q();
+    lds_barrier();                                  // Q in LDS, with pages on their way
+    const bool own = lane < n8 && page >= 0, fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
+    if (own && !fine && a.err) *a.err = SPEC_E_INVAL;
+    const uint64_t good = __ballot(own && fine);
+    const int um = wave_max(own && fine ? (int)__float_as_uint(vsc) : 0);   // (positive floats order as integers)
+    if (um != 0) u = __uint_as_float((uint32_t)um);
+    const float lu = log2f(u);
+    lv = (own ? log2f(vsc) : 0.f) - lu;
+    float qs[NRB];
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-      for (int t = 0; t < 2 * KH; ++t) qf[rb][t] = s_q[wr][rb][t][ql];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f32x4 acc[NRB];
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int h = 0; h < KH; ++h) {
-        const u32x4 lo = bf16_of_e4m3(kr[t][h].x, kr[t][h].y), hi = bf16_of_e4m3(kr[t][h].z, kr[t][h].w);
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-          acc[rb] = mfma16x16x32(lo, qf[rb][2 * h], acc[rb]);
-          acc[rb] = mfma16x16x32(hi, qf[rb][2 * h + 1], acc[rb]);
-        }
-      }
+    for (int rb = 0; rb < NRB; ++rb) qs[rb] = a.scale_log2 * (kNative ? s_qs[wr][16 * rb + n16] : 1.f);
+    while (p < 64) {
+      t8 &= t8 - 1;
+      const int next = t8 ? __builtin_ctzll(t8) : 64;
+      const int k0 = (p0 + p) * kAttnChunk;
+      const bool sound = good >> p & 1;             // else a page without scales: not visible
+      const bool full = sound && k0 + kAttnChunk <= vmin;
+      float s[NRB][16];                             // scores of keys 16 g4 + i
+      int ql = lane;
+      asm volatile("" : "+v"(ql));                  // (Q is read again for every page)
+      KeyBytes qf[NRB][2];
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
-    }
-    if (next < 64) load_k(next);
-    if (!full) mask(s, k0, sound ? INT32_MAX : 0);
-    const float off = sound ? lane_f(lv, p) : 0.f, far = far_of(off);
-    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
-    soft(st, s, fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f), far != 0.f ? kHead : off + kHead);
-    if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
-    u32x4 pb[NRB][2];
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (kNative)
+            qf[rb][t] = join8(s_q8[wr][rb][2 * t][ql], s_q8[wr][rb][2 * t + 1][ql]);
+          else
+            qf[rb][t] = s_q[wr][rb][t][ql];
+        }
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
+      for (int t = 0; t < 4; ++t) {
+        f32x4 acc[NRB];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float* q = s[rb] + 8 * e;
-        pb[rb][e] = u32x4{pack_f16(q[0], q[1]), pack_f16(q[2], q[3]), pack_f16(q[4], q[5]), pack_f16(q[6], q[7])};
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (kNative) {
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) {
+            acc[rb] = mfma_e4m3<127>(kr[t], qf[rb][0], acc[rb]);
+            acc[rb] = mfma_e4m3<123>(kr[t], qf[rb][1], acc[rb]);
+          }
+        } else {
+          const u32x4 lo = bf16_of_e4m3(kr[t].x, kr[t].y), hi = bf16_of_e4m3(kr[t].z, kr[t].w);
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) {
+            acc[rb] = mfma16x16x32(lo, qf[rb][0], acc[rb]);
+            acc[rb] = mfma16x16x32(hi, qf[rb][1], acc[rb]);
+          }
+        }
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
       }
-    if (!full) {
-      const int valid = (sound ? min(vmax - k0, kAttnChunk) : 0) - 16 * g4;   // of this lane's 16 keys
-      uint32_t m[4], odd = 0;
+      // (the last page loads itself again, out of the caches: under a branch the loads were moved ahead of the products
+      // above and took registers of their own)
+      const size_t nat = at_of(next < 64 ? next : p);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(nat);
+      if (!full) mask(s, k0, sound ? INT32_MAX : 0);
+      const float off = sound ? lane_f(lv, p) : 0.f, far = far_of(off);
+      if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
+      const float rest = far != 0.f ? __builtin_amdgcn_exp2f(off + far) : 1.f;
+      float sc[NRB];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = min(max(valid - 4 * k, 0), 4);
-        m[k] = (uint32_t)((1ull << (8 * c)) - 1);
-      }
+      for (int rb = 0; rb < NRB; ++rb) sc[rb] = fmaxf(qs[rb] * lane_f(ks, p), 1e-37f);
+      u32x4 pb[NRB][2];
+      soft(st, s, sc, far != 0.f ? kHead : off + kHead, [&](int rb, float (&x)[16]) {
+        if (rest != 1.f)
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+          for (int i = 0; i < 16; ++i) x[i] *= rest;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) pb[rb][e][k] = pack_f16(x[8 * e + 2 * k], x[8 * e + 2 * k + 1]);
+      });
+      if (!full) {
+        const int valid = (sound ? min(vmax - k0, kAttnChunk) : 0) - 16 * g4;   // of this lane's 16 keys
+        uint32_t m[4], odd = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t w = vr[dt][k] & m[k], x = nan8(w);
-          odd |= x;
-          vr[dt][k] = w & ~((x >> 7) * 0xffu);
+          const int c = min(max(valid - 4 * k, 0), 4);
+          m[k] = (uint32_t)((1ull << (8 * c)) - 1);
         }
-      if (__any(odd != 0)) odd_pages |= 1ull << p;
-    }
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) {
-      const u32x4 lo = f16_of_e4m3(vr[dt].x, vr[dt].y), hi = f16_of_e4m3(vr[dt].z, vr[dt].w);
+        for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) {
-        st.o[rb][dt] = mfma_f16(lo, pb[rb][0], st.o[rb][dt]);
-        st.o[rb][dt] = mfma_f16(hi, pb[rb][1], st.o[rb][dt]);
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t w = vr[dt][k] & m[k], x = nan8(w);
+            odd |= x;
+            vr[dt][k] = w & ~((x >> 7) * 0xffu);
+          }
+        if (__any(odd != 0)) odd_pages |= 1ull << p;
       }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const u32x4 lo = f16_of_e4m3(vr[dt].x, vr[dt].y), hi = f16_of_e4m3(vr[dt].z, vr[dt].w);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+          st.o[rb][dt] = mfma_f16(lo, pb[rb][0], st.o[rb][dt]);
+          st.o[rb][dt] = mfma_f16(hi, pb[rb][1], st.o[rb][dt]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(nat);
+      if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
+      p = next;
     }
-    if (next < 64) load_v(next);
-    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
-    p = next;
+  } else {
+    stage_q();
+    lds_barrier();
   }
 
   for (uint64_t t16 = todo & ~mask8; t16; t16 &= t16 - 1) {
-    const int q = __builtin_ctzll(t16);
-    const size_t at = at_of(q);
-    const int k0 = (p0 + q) * kAttnChunk;
+    const int p = __builtin_ctzll(t16);
+    const size_t at = at_of(p);
+    const int k0 = (p0 + p) * kAttnChunk;
     const bool full = k0 + kAttnChunk <= vmin;
     float s[NRB][16];
     int ql = lane;
@@ -587,13 +693,30 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
       for (int e = 0; e < 2; ++e) w[2 * dt + e] = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
     if (!full) mask(s, k0, INT32_MAX);
-    const float off = lane_f(lv, q), far = far_of(off);
+    const float off = lane_f(lv, p), far = far_of(off);
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
-    soft(st, s, a.scale_log2, far != 0.f ? kHead : off + kHead);
-    if (far != 0.f) times(s, __builtin_amdgcn_exp2f(off + far));
-    uint32_t odd = 0;
+    const float rest = far != 0.f ? __builtin_amdgcn_exp2f(off + far) : 1.f;
+    float sc[NRB];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) sc[rb] = a.scale_log2;
+    u32x4 ph[NRB][2], pl[NRB][2];
+    soft(st, s, sc, far != 0.f ? kHead : off + kHead, [&](int rb, float (&x)[16]) {
+      if (rest != 1.f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= rest;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x0 = x[8 * e + 2 * k], x1 = x[8 * e + 2 * k + 1];
+          const uint32_t h = pack2(x0, x1);
+          ph[rb][e][k] = h;
+          pl[rb][e][k] = pack2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xffff0000u));
+        }
+    });
     if (!full) {
       const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;
+      uint32_t odd = 0;
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -606,28 +729,17 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
             w[2 * dt + e][k] = v & ~((x >> 15) * 0xffffu);
           }
         }
+      if (__any(odd != 0)) odd_pages |= 1ull << p;
     }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      u32x4 ph[NRB], pl[NRB];
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) {
-        const float* pr = s[rb] + 8 * e;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          ph[rb][k] = pack2(pr[2 * k], pr[2 * k + 1]);
-          pl[rb][k] = pack2(pr[2 * k] - __uint_as_float(ph[rb][k] << 16), pr[2 * k + 1] - __uint_as_float(ph[rb][k] & 0xffff0000u));
-        }
-      }
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], ph[rb], st.o[rb][dt]);
-          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], pl[rb], st.o[rb][dt]);
+          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], ph[rb][e], st.o[rb][dt]);
+          st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], pl[rb][e], st.o[rb][dt]);
         }
-    }
-    if (__any(odd != 0)) odd_pages |= 1ull << q;
     if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
   }
 
@@ -643,7 +755,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     }
   }
   if (lane == 0) s_odd[wk][wr] = odd_pages;
-  __syncthreads();
+  lds_barrier();
   const int nrb = gridDim.y * WR * NRB;             // row blocks of the partials
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
@@ -659,28 +771,19 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       L = __builtin_fmaf(f, s_l[w][wr][16 * rb + n16], L);
     }
     const float f = (st.m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[rb] - M)) * u;
+    if (rb) lds_barrier();                          // the last block's tiles have been read
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= f;
-#pragma unroll
-    for (int w = 0; w < kKeyWaves; ++w)
-      if (w != wk)
-#pragma unroll
-        for (int d = 0; d < ND4; ++d)
-          s_o[rb & 1][wr][w][(wk - w + kKeyWaves) % kKeyWaves - 1][d][lane] = st.o[rb][w * ND4 + d];
-    __syncthreads();
-    // (the buffer is written again two blocks on, behind the next barrier)
+    for (int dt = 0; dt < NDT; ++dt) s_o[wr][wk][dt][lane] = st.o[rb][dt] * f;
+    lds_barrier();
     const size_t blk = (size_t)id * nrb + (blockIdx.y * WR + wr) * NRB + rb;
 #pragma unroll
-    for (int w = 0; w < kKeyWaves; ++w)
-      if (w == wk) {
+    for (int d = 0; d < ND4; ++d) {
+      const int dt = wk * ND4 + d;
+      f32x4 v = s_o[wr][0][dt][lane];
 #pragma unroll
-        for (int d = 0; d < ND4; ++d) {
-          f32x4 v = st.o[rb][w * ND4 + d];
-#pragma unroll
-          for (int k = 0; k < kKeyWaves - 1; ++k) v += s_o[rb & 1][wr][w][k][d][lane];
-          *reinterpret_cast<f32x4*>(a.part + ((blk * NDT + w * ND4 + d) * 64 + lane) * 4) = v;
-        }
-      }
+      for (int k = 1; k < kKeyWaves; ++k) v += s_o[wr][k][dt][lane];
+      *reinterpret_cast<f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4) = v;
+    }
     if (wk == 0 && g4 == 0) a.ml[blk * 16 + n16] = make_float2(M, L);
     if (wk == 0 && lane == 0) {
       uint64_t w = 0;
