@@ -1837,15 +1837,13 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
     p.out = c.o;
     p.q_stride = p.out_stride = (int64_t)nq * D;
     p.opk = wide_o(c) ? c.Mpad / 16 : 0;
-    p.part = c.kv8_part;
-    p.ml = c.kv8_ml;
-    p.odd = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(c.kv8_ml) + c.kv8_ml_bytes);
     p.B = c.B;
     p.R = c.R;
     p.nq = nq;
     p.nkv = nkv;
     p.G = G;
     p.ppw = c.kv8_ppw;
+    kv8_set_parts(p, c.kv8_part, c.kv8_ml, c.kv8_groups);
     p.scale_log2 = kLog2e / sqrtf((float)D);
     {
       Timed t(c, SPEC_KERNEL_ATTN, 0);

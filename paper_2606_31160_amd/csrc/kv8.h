@@ -43,6 +43,7 @@ struct Kv8AttnArgs {
   int32_t* err;            // or null
   float* part;             // [groups][row blocks][D/16][64] unnormalised partial outputs
   float2* ml;              // [groups][row blocks * 16] (maximum in log2 units, sum)
+  int4* seq;               // [B] first group, groups of a kv head, pages of a group (sequences with pages)
   uint64_t* odd;           // [groups][row blocks] pages with values that the combine adds
   int B, R, nq, nkv, G;
   int ppw;                 // pages of a group; 0: as many as leave about `target` groups
@@ -55,7 +56,8 @@ constexpr int kKv8MinPages = 4, kKv8MaxPages = 64;   // pages of a group
 // Groups of a call at most (the grid), the partials' bytes, the groups a call without a fixed `ppw` aims at.
 int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target);
 size_t kv8_part_bytes(int64_t groups, int rows, int D);
-size_t kv8_ml_bytes(int64_t groups, int rows);     // of ml; odd takes a sixteenth of it
+size_t kv8_ml_bytes(int64_t groups, int rows);     // of ml, odd behind it and seq behind that
+void kv8_set_parts(Kv8AttnArgs& a, void* part, void* ml, int64_t groups);
 int kv8_target_groups(int rows, int ncu);   // (what runs at once)
 hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0 = nullptr,
                            hipEvent_t e1 = nullptr);

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float v = x[u][4 * q + k];
-        y[k] = fabsf(v) < INFINITY ? v * inv : NAN;
+        y[k] = v * inv;                             // (infinities become NaN: e4m3 has none)
       }
       int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
       code[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
@@ -270,6 +270,11 @@ __device__ __forceinline__ float lane_f(float x, int l) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
 }
 
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // A barrier for data in LDS that leaves loads from memory in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -347,12 +352,14 @@ __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
 // i of key tile t is key 16 (i >> 2) + 4 t + (i & 3): the 16 scores of a lane belong to
 // the consecutive keys 16 g .. 16 g + 15, one 16-byte read of a value row; and a
 // lane's 16 bytes of a key row serve whatever part of the head dimension, whose order
-// is the same in Q's operand.  The next page's keys are loaded while this one's
-// softmax runs, its values while the next scores are formed.
+// is the same in Q's operand.
+//   The next page's keys are loaded while this one's softmax runs, its values while
+// the next scores are formed.  (Pages by way of LDS, for the two waves of WR = 2 at
+// once, took longer: 33 us where this takes 29.5, the waves in step at its barriers.)
 //   Keys of head dimension 128 go to the matrix unit as they are, in 16x16x128 MFMA of
 // e4m3 numbers: Q = 2^e (hi + lo / 16) with hi = e4m3(Q / 2^e) and lo the rest, four
-// bits each, which is all of a bf16 number (but for what lies 2^-22 below the row's
-// largest).  For 64 they are read as bf16, like Q.
+// bits each, which is all of a bf16 number (an element below 2^-15 of the row's
+// largest is held to 2^-21 of that).  For 64 they are read as bf16, like Q.
 //   Values and probabilities are read as fp16: an e4m3 code is exact in it, and a
 // probability keeps 11 bits, as a rounding to bf16 would show in the bf16 result.
 // The value scale is part of the probability's exponent: with u the largest one of
@@ -365,13 +372,16 @@ template <int D, int NRB, int WR>
 __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kKeyWaves;
   constexpr bool kNative = D == 128;                // keys as e4m3 operands
+  constexpr int kOp = kAttnChunk * D;               // bytes of a page's keys (or values)
+  typedef std::conditional_t<kNative, i32x8, u32x4> KeyBytes;   // a lane's part of a key operand
   __shared__ f32x4 s_o[WR][kKeyWaves][NDT][64];
-  // Q operands, bf16 and e4m3 (hi, lo): in registers they would not leave room for two pages
-  __shared__ u32x4 s_q[WR][NRB][2 * KH][64], s_q8[kNative ? WR : 1][kNative ? NRB : 1][2 * KH][64];
-  __shared__ float s_qs[WR][NRB * 16];              // 2^e of every row
   __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
   __shared__ int s_vis[WR * kKeyWaves][SPEC_MAX_ROWS];
   __shared__ uint64_t s_odd[kKeyWaves][WR];
+  // Q's e4m3 operands (hi, lo) and their 2^e, made by one wave for all: they are much work, and in registers they would not leave
+  // room for two pages
+  __shared__ u32x4 s_q[kNative ? WR : 1][kNative ? NRB : 1][2][2][64];
+  __shared__ float s_qs[WR][NRB * 16];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int n16 = lane & 15, g4 = lane >> 4;
@@ -397,7 +407,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   const int p0 = grp * gr.ppw;                      // first page
   const int np = min(gr.ppw, pages - p0);
   const int packed = min(max(a.packed[b], 0), a.stride);
-  const int n8 = min(max(packed - p0, 0), np);
+  const int n8 = a.pages8 > 0 ? min(max(packed - p0, 0), np) : 0;
+  const int n16p = max(packed - p0, 0);             // the first bf16 page
+  if (id == first && threadIdx.x == 0 && blockIdx.y == 0) a.seq[b] = make_int4(first, (pages + gr.ppw - 1) / gr.ppw, gr.ppw, 0);
 
   // lane l: the group's l-th page
   int page = -1;
@@ -406,33 +418,40 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // rows of this wave
   const int rows = a.R * a.G, r0 = (blockIdx.y * WR + wr) * NRB * 16;
   int vis[NRB], vmin = INT32_MAX, vmax = 0;
-  u32x4 q[2 * KH];                                  // of row block wk
+  u32x4 q[2 * KH], qb[NRB][kNative ? 1 : 2];        // of row block wk / of all (what the 8-bit pages are read against)
+  // (a row that is not there reads one that is)
+  auto q_at = [&](int rb, int& j) {
+    const int r = r0 + 16 * rb + n16;
+    j = r < rows ? (unsigned)r / (unsigned)a.G : 0;
+    const int g = r < rows ? r - j * a.G : 0;
+    return a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)(kvh * a.G + g) * D + 16 * g4;
+  };
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
-    const int r = r0 + 16 * rb + n16;
-    const bool in = r < rows;
-    const int j = in ? r / a.G : 0, hq = kvh * a.G + (in ? r % a.G : 0);
-    const int v = in ? row_vis(a, gr, s_vis[wave], b, j) : -1;
+    int j;
+    const bf16_t* const qp = q_at(rb, j);
+    const int v = r0 + 16 * rb + n16 < rows ? row_vis(a, gr, s_vis[wave], b, j) : -1;
     if (v > a.stride * kAttnChunk && a.err) *a.err = SPEC_E_INVAL;
     vis[rb] = v < 0 ? INT32_MAX : v;                // rows that nobody asked for need no mask
     vmin = min(vmin, vis[rb]);
     vmax = max(vmax, v);
-    // (a row that is not there reads one that is)
-    if (rb == wk) {
-      const bf16_t* qp = a.q + (int64_t)(b * a.R + j) * a.q_stride + (int64_t)hq * D + 16 * g4;
+    if constexpr (kNative) {
+      if (rb == wk)
 #pragma unroll
-      for (int t = 0; t < 2 * KH; ++t) q[t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+        for (int t = 0; t < 2 * KH; ++t) q[t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) qb[rb][t] = ld16(qp + 8 * t);
     }
   }
   vmin = ~__builtin_amdgcn_readfirstlane(row_max(~vmin));
   vmax = __builtin_amdgcn_readfirstlane(row_max(vmax));      // slots that no row of this wave sees: from here
 
   // pages that may be read, and those that this wave has to
-  if (page < 0 || page >= (lane < n8 ? a.pages8 : a.pages16)) page = -1;
+  if (page < 0 || page >= (lane < n16p ? a.pages8 : a.pages16)) page = -1;
   if (lane < np && page < 0 && a.err) *a.err = SPEC_E_INVAL;
   const int seen = vmax <= p0 * kAttnChunk ? 0 : min(np, (vmax - p0 * kAttnChunk + kAttnChunk - 1) / kAttnChunk);
   const uint64_t todo = __ballot(lane < seen && page >= 0 && lane % kKeyWaves == wk);
-  const uint64_t mask8 = n8 >= 64 ? ~0ull : (1ull << n8) - 1;
 
   RowState<NRB, NDT> st;
 #pragma unroll
@@ -444,29 +463,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   }
 
   const int krow = 16 * (n16 >> 2) + (n16 & 3);     // key of this lane in tile 0
-  // a page on its way: per key tile the lane's bytes of its key (both halves of the head dimension side by side for
-  // the 128-wide operand), per 16 dimensions those of its value row
-  typedef std::conditional_t<kNative, i32x8, u32x4> KeyBytes;
-  KeyBytes kr[4];
-  u32x4 vr[NDT];
   auto at_of = [&](int p) {                         // element of the page's first key or value
-    return ((size_t)__builtin_amdgcn_readlane(page, p) * a.nkv + kvh) * kAttnChunk * D;
-  };
-  auto load_k = [&](size_t at) {
-    const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const u32x4* k = reinterpret_cast<const u32x4*>(kp + 4 * t * D);
-      if constexpr (kNative)
-        kr[t] = join8(k[0], k[4]);
-      else
-        kr[t] = k[0];
-    }
-  };
-  auto load_v = [&](size_t at) {
-    const uint8_t* vp = a.v8 + at + n16 * kAttnChunk + 16 * g4;
-#pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
+    return ((size_t)max(__builtin_amdgcn_readlane(page, p), 0) * a.nkv + kvh) * kOp;
   };
   auto mask = [&](float (&s)[NRB][16], int k0, int end) {
 #pragma unroll
@@ -484,96 +482,117 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // A page whose unit is far from u: O is turned by 2^far while it is added, and
   // what 2^60 leaves (seen in no sound cache) is taken by the probabilities.
   auto far_of = [](float off) { return fabsf(off) > 16.f ? fminf(fmaxf(-off, -60.f), 60.f) : 0.f; };
-  // Q's operands into LDS, by the wave that loaded them.
-  auto stage_q = [&] {
-    if (wk >= NRB) return;
-#pragma unroll
-    for (int t = 0; t < 2 * KH; ++t) s_q[wr][wk][t][lane] = q[t];
-    if constexpr (kNative) {
-      // 2^e: the smallest power of two with max |q| <= 448 2^e, as for a page
-      float big = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2 * KH; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float x = fabsf(__uint_as_float(q[t][k] << 16)), y = fabsf(__uint_as_float(q[t][k] & 0xffff0000u));
-          big = fmaxf(big, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
-        }
-      big = fmaxf(big, __shfl_xor(big, 16));
-      big = fmaxf(big, __shfl_xor(big, 32));
-      const int e = scale_exponent(big);
-      const float inv = power_of_two(-e);
-      if (g4 == 0) s_qs[wr][16 * wk + n16] = power_of_two(e);
-#pragma unroll
-      for (int h = 0; h < KH; ++h) {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float y[4];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t w = q[2 * h + (k >> 1)][2 * (k & 1) + i];
-            const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
-            y[2 * i] = fabsf(x0) < INFINITY ? x0 * inv : NAN;
-            y[2 * i + 1] = fabsf(x1) < INFINITY ? x1 * inv : NAN;
-          }
-          int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-          c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
-          const f32x2 d0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), d1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-          hi[k] = (uint32_t)c;
-          c = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - d0.x) * 16.f, (y[1] - d0.y) * 16.f, 0, false);
-          lo[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32((y[2] - d1.x) * 16.f, (y[3] - d1.y) * 16.f, c, true);
-        }
-        s_q8[wr][wk][h][lane] = u32x4{hi[0], hi[1], hi[2], hi[3]};
-        s_q8[wr][wk][KH + h][lane] = u32x4{lo[0], lo[1], lo[2], lo[3]};
-      }
-    }
-  };
   // Pages that not every row sees, with values that are not finite: these are taken
   // as zero here, as zero probability times one is not zero, and the combine gives
   // them to the rows that see their slots.
   uint64_t odd_pages = 0;
   float u = 1.f, lv = 0.f;                          // unit of O; lane l: log2 of the l-th page's value scale / u
 
-  if (n8 > 0 && a.pages8 > 0) {                     // workgroup-uniform
-    uint64_t t8 = todo & mask8;
-    int p = t8 ? __builtin_ctzll(t8) : 64;
-    const size_t sl = (size_t)max(lane < n8 ? page : 0, 0) * a.nkv + kvh;
+  if (n8 > 0) {                                     // workgroup-uniform
+    const bool own = lane < n8 && page >= 0;
+    const size_t sl = (size_t)(own ? page : 0) * a.nkv + kvh;
     const float ks = a.ks[sl], vsc = a.vs[sl];
-    // (without a page to do, the pool's first: loads outside a branch can be awaited one by one)
-    const size_t at0 = p < 64 ? at_of(p) : (size_t)kvh * kAttnChunk * D;
-    load_k(at0);
-    load_v(at0);
-    stage_q();
-    lds_barrier();                                  // Q in LDS, with pages on their way
-    const bool own = lane < n8 && page >= 0, fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
+    uint64_t t8 = todo & (n8 >= 64 ? ~0ull : (1ull << n8) - 1);
+
+    // a page on its way
+    KeyBytes kr[4];
+    u32x4 vr[NDT];
+    auto load_k = [&](size_t at) {
+      const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const u32x4* k = reinterpret_cast<const u32x4*>(kp + 4 * t * D);
+        if constexpr (kNative)
+          kr[t] = join8(k[0], k[4]);
+        else
+          kr[t] = k[0];
+      }
+    };
+    auto load_v = [&](size_t at) {
+      const uint8_t* vp = a.v8 + at + n16 * kAttnChunk + 16 * g4;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(vp + 16 * dt * kAttnChunk);
+    };
+    int p = t8 ? __builtin_ctzll(t8) : 64;
+    {
+      // (without a page to do, the group's first: loads outside a branch can be awaited one by one)
+      const size_t at = at_of(p < 64 ? p : 0);
+      load_k(at);
+      load_v(at);
+    }
+    if constexpr (kNative) {
+      if (wk < NRB) {
+        // 2^e: the smallest power of two with max |q| <= 448 2^e, as for a page, from the largest of the lane's 32 bf16
+        // magnitudes and its row's other three lanes (one that is not finite makes the row NaN whatever e is)
+        uint32_t big = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) big = pk_max_u16(big, q[t][k] & 0x7fff7fffu);
+        big = max(big & 0xffffu, big >> 16);
+        big = max(big, (uint32_t)__shfl_xor((int)big, 16));
+        big = max(big, (uint32_t)__shfl_xor((int)big, 32));
+        const int e = min(max((int)(big >> 7) - ((big & 127) <= 96 ? 135 : 134), -120), 120);
+        const float inv = power_of_two(-e), inv16 = inv * 16.f;
+        if (g4 == 0) s_qs[wr][16 * wk + n16] = a.scale_log2 * power_of_two(e);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 hi, lo;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            int c = 0, r = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t w = q[2 * h + (k >> 1)][2 * (k & 1) + i];
+              const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
+              const int y = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * inv, x1 * inv, 0, false);
+              const f32x2 d = __builtin_amdgcn_cvt_pk_f32_fp8(y, false);
+              const float z0 = __builtin_fmaf(x0, inv16, -16.f * d.x), z1 = __builtin_fmaf(x1, inv16, -16.f * d.y);
+              const int z = __builtin_amdgcn_cvt_pk_fp8_f32(z0, z1, 0, false);
+              c |= (y & 0xffff) << (16 * i);
+              r |= (z & 0xffff) << (16 * i);
+            }
+            hi[k] = (uint32_t)c;
+            lo[k] = (uint32_t)r;
+          }
+          s_q[wr][wk][0][h][lane] = hi;
+          s_q[wr][wk][1][h][lane] = lo;
+        }
+      }
+      lds_barrier();                                // with pages on their way
+    }
+    // (the scales arrive before the pages)
+    const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
     if (own && !fine && a.err) *a.err = SPEC_E_INVAL;
     const uint64_t good = __ballot(own && fine);
     const int um = wave_max(own && fine ? (int)__float_as_uint(vsc) : 0);   // (positive floats order as integers)
     if (um != 0) u = __uint_as_float((uint32_t)um);
-    const float lu = log2f(u);
-    lv = (own ? log2f(vsc) : 0.f) - lu;
+    lv = (lane < n8 ? __builtin_amdgcn_logf(vsc) : 0.f) - __builtin_amdgcn_logf(u);
     float qs[NRB];
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) qs[rb] = a.scale_log2 * (kNative ? s_qs[wr][16 * rb + n16] : 1.f);
+    for (int rb = 0; rb < NRB; ++rb) qs[rb] = kNative ? s_qs[wr][16 * rb + n16] : a.scale_log2;
+
     while (p < 64) {
       t8 &= t8 - 1;
       const int next = t8 ? __builtin_ctzll(t8) : 64;
+      // (the last page loads itself again, out of the caches: under a branch the loads were moved ahead of the
+      // products and took registers of their own)
+      const size_t nat = at_of(next < 64 ? next : p);
       const int k0 = (p0 + p) * kAttnChunk;
-      const bool sound = good >> p & 1;             // else a page without scales: not visible
+      const bool sound = good >> p & 1;           // else a page without scales: not visible
       const bool full = sound && k0 + kAttnChunk <= vmin;
-      float s[NRB][16];                             // scores of keys 16 g4 + i
-      int ql = lane;
-      asm volatile("" : "+v"(ql));                  // (Q is read again for every page)
+      float s[NRB][16];                           // scores of keys 16 g4 + i
       KeyBytes qf[NRB][2];
+      int ql = lane;
+      asm volatile("" : "+v"(ql));                // (read again for every page)
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int h = 0; h < 2; ++h) {
           if constexpr (kNative)
-            qf[rb][t] = join8(s_q8[wr][rb][2 * t][ql], s_q8[wr][rb][2 * t + 1][ql]);
+            qf[rb][h] = join8(s_q[wr][rb][h][0][ql], s_q[wr][rb][h][1][ql]);
           else
-            qf[rb][t] = s_q[wr][rb][t][ql];
+            qf[rb][h] = qb[rb][h];
         }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -599,9 +618,6 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
       }
-      // (the last page loads itself again, out of the caches: under a branch the loads were moved ahead of the products
-      // above and took registers of their own)
-      const size_t nat = at_of(next < 64 ? next : p);
       __builtin_amdgcn_sched_barrier(0);
       load_k(nat);
       if (!full) mask(s, k0, sound ? INT32_MAX : 0);
@@ -653,22 +669,24 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
       p = next;
     }
-  } else {
-    stage_q();
-    lds_barrier();
   }
 
-  for (uint64_t t16 = todo & ~mask8; t16; t16 &= t16 - 1) {
+  for (uint64_t t16 = n16p >= 64 ? 0 : todo & ~((1ull << n16p) - 1); t16; t16 &= t16 - 1) {
     const int p = __builtin_ctzll(t16);
     const size_t at = at_of(p);
     const int k0 = (p0 + p) * kAttnChunk;
     const bool full = k0 + kAttnChunk <= vmin;
     float s[NRB][16];
-    int ql = lane;
-    asm volatile("" : "+v"(ql));
-    // all of the page's keys, then all of its values, in flight at once
-    u32x4 w[16 * KH];
+    // Q again and all of the page's keys, then all of its values, in flight at once
+    u32x4 w[16 * KH], qw[NRB][2 * KH];
     const bf16_t* kp = a.k16 + at + krow * D + 16 * g4;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      int j;
+      const bf16_t* const qp = q_at(rb, j);
+#pragma unroll
+      for (int t = 0; t < 2 * KH; ++t) qw[rb][t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
+    }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -681,7 +699,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
       for (int h = 0; h < 2 * KH; ++h)
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(w[2 * KH * t + h], s_q[wr][rb][h][ql], acc[rb]);
+        for (int rb = 0; rb < NRB; ++rb) acc[rb] = mfma16x16x32(w[2 * KH * t + h], qw[rb][h], acc[rb]);
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
@@ -802,24 +820,23 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   constexpr int NDT = D / 16, U = 4;
   __shared__ f32x4 s_o[NW][64];
   __shared__ float s_m[NW][16], s_l[NW][16];
-  __shared__ int s_vis[NW][SPEC_MAX_ROWS];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n16 = lane & 15, g4 = lane >> 4;
   const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
   const int r = 16 * rb + n16;
   const bool in_row = r < a.R * a.G;
   const int j = in_row ? r / a.G : 0, hq = kvh * a.G + (in_row ? r % a.G : 0);
-  const Groups gr = count_groups(a, s_vis[wave]);
-  const int vis = in_row ? row_vis(a, gr, s_vis[wave], b, j) : -1;
-  int pages = 0, first = 0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-    if (b >> 6 == i) {
-      pages = __builtin_amdgcn_readlane(gr.pages[i], b & 63);
-      first = __builtin_amdgcn_readlane(gr.first[i], b & 63);
-    }
-  const int per = (pages + gr.ppw - 1) / gr.ppw;
-  first += kvh;
+  const int4 seq = a.seq[b];                        // (of no meaning if no row of the sequence sees anything)
+  int vis;
+  if (a.st) {
+    const SeqState& s = a.st[b];
+    vis = j < s.count ? s.base + (j < s.causal ? j + 1 : s.count) : -1;
+  } else {
+    vis = a.vis[b * a.R + j];
+  }
+  if (!in_row) vis = -1;
+  const int per = __any(vis > 0) ? seq.y : 0, ppw = seq.z;
+  const int first = seq.x + kvh;
   float M = -INFINITY, L = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int i = wave; i < per; i += NW * U) {
@@ -841,7 +858,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
     }
     for (int k = 0; k < U; ++k)
       for (uint64_t w = odd[k]; w; w &= w - 1) {    // values that are not finite, for the rows that see them
-        const int p = (i + NW * k) * gr.ppw + __builtin_ctzll(w);
+        const int p = (i + NW * k) * ppw + __builtin_ctzll(w);
         const bool in8 = p < a.packed[b];
         const size_t at = ((size_t)a.table[(size_t)b * a.stride + p] * a.nkv + kvh) * kAttnChunk * D;
         for (int key = 0; key < kAttnChunk; ++key)
@@ -936,7 +953,16 @@ int64_t kv8_max_groups(int B, int nkv, int stride, int ppw, int target) {
 }
 
 size_t kv8_part_bytes(int64_t groups, int rows, int D) { return (size_t)groups * padded_blocks(rows) * 16 * D * sizeof(float); }
-size_t kv8_ml_bytes(int64_t groups, int rows) { return (size_t)groups * padded_blocks(rows) * 16 * sizeof(float2); }
+size_t kv8_ml_bytes(int64_t groups, int rows) {
+  return (size_t)groups * padded_blocks(rows) * (16 * sizeof(float2) + sizeof(uint64_t)) + SPEC_MAX_ROWS * sizeof(int4) + 16;
+}
+void kv8_set_parts(Kv8AttnArgs& a, void* part, void* ml, int64_t groups) {
+  const size_t n = (size_t)groups * padded_blocks(a.R * a.G);
+  a.part = static_cast<float*>(part);
+  a.ml = static_cast<float2*>(ml);
+  a.odd = reinterpret_cast<uint64_t*>(a.ml + 16 * n);
+  a.seq = reinterpret_cast<int4*>(a.odd + (n + 1) / 2 * 2);
+}
 
 hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const Shape h = shape_of(a.R * a.G);

@@ -54,7 +54,7 @@ const char* bad_pass(const spec_kv8* c, int32_t batch, int32_t rows, int32_t q_h
 struct AttnPlan {
   int target;
   int64_t groups;
-  size_t ml, odd, bytes;   // offsets of the maxima and sums and of the odd pages; all
+  size_t ml, bytes;   // offset of the maxima and sums; all
 };
 AttnPlan attn_plan(const spec_kv8* c, int batch, int rows, int q_heads, int stride) {
   const int r = rows * (q_heads / c->kv_heads);
@@ -62,8 +62,7 @@ AttnPlan attn_plan(const spec_kv8* c, int batch, int rows, int q_heads, int stri
   p.target = kv8_target_groups(r, num_cus());
   p.groups = kv8_max_groups(batch, c->kv_heads, stride, 0, p.target);
   p.ml = align_up(kv8_part_bytes(p.groups, r, c->head_dim));
-  p.odd = p.ml + align_up(kv8_ml_bytes(p.groups, r));
-  p.bytes = p.odd + align_up(kv8_ml_bytes(p.groups, r) / 16);
+  p.bytes = p.ml + align_up(kv8_ml_bytes(p.groups, r));
   return p;
 }
 
@@ -149,14 +148,12 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   a.out_stride = out_stride;
   a.lse = d_lse;
   a.err = d_err;
-  a.part = static_cast<float*>(workspace);
-  a.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml);
-  a.odd = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + p.odd);
   a.B = batch;
   a.R = rows;
   a.nq = q_heads;
   a.nkv = c->kv_heads;
   a.G = q_heads / c->kv_heads;
+  kv8_set_parts(a, workspace, static_cast<char*>(workspace) + p.ml, p.groups);
   a.target = p.target;
   a.scale_log2 = scale * 1.4426950408889634f;
   const spec_status s = launched(launch_kv8_attn(a, c->head_dim, p.groups, stream), f);

@@ -564,7 +564,7 @@ size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has
     c.kv8_part_bytes = kv8_part_bytes(c.kv8_groups, rows, D);
     c.kv8_ml_bytes = kv8_ml_bytes(c.kv8_groups, rows);
     c.kv8_part = reinterpret_cast<float*>(cv.take<char>(c.kv8_part_bytes));
-    c.kv8_ml = reinterpret_cast<float2*>(cv.take<char>(c.kv8_ml_bytes + c.kv8_ml_bytes / 16));   // and the odd pages
+    c.kv8_ml = reinterpret_cast<float2*>(cv.take<char>(c.kv8_ml_bytes));
   }
   if (has_draft) {
     c.drf.kv_layer = (size_t)L.pool * cfg->draft.kv_heads * kAttnChunk * D;
@@ -821,7 +821,7 @@ ScratchPlan scratch_plan(const Ctx& c) {
   p.lp = take(attn_rows * sizeof(float));
   p.rp = take(attn_rows * 4 * sizeof(float));
   p.kv8_part = take(c.kv8_part_bytes);
-  p.kv8_ml = take(c.kv8_ml_bytes + c.kv8_ml_bytes / 16);
+  p.kv8_ml = take(c.kv8_ml_bytes);
   p.part = take(c.part_elems * sizeof(float));
   p.sg_part = take(c.sg ? c.sg_part_floats * sizeof(float) : 0);
   p.cnt_bytes = c.sg ? align_up((size_t)(c.sg_units + 1) * sizeof(unsigned), 16) : 0;

@@ -239,6 +239,13 @@ class Case:
                         # score, the normalisation), by half a step of fp16, 2^-11 or at most 2^-25 where it is that
                         # small, and the result by half a step of bf16, 2^-8; 2^-14 A for what is summed in 32 bits.
                         ds = (self.D + 8) * 2.0 ** -24 * S
+                        if self.D == 128 and n > 0:
+                            # Against keys of 128 dimensions a query is 2^e (hi + lo / 16) of e4m3 numbers, with 448 2^e the
+                            # first of its kind not below max |q|, so max |q| > 224 2^e.  Where four bits each do not hold
+                            # an element to its last bit, half of e4m3's smallest step, 2^-9, is lost of lo: 2^-14 2^e <
+                            # 2^-14 / 224 max |q| < 2^-21 max |q| an element.
+                            with np.errstate(invalid="ignore"):
+                                ds += 2.0 ** -21 * np.abs(q).max() * np.nanmax(np.abs(k[:n]).sum(1)) * self.scale
                         tol = 2.0 ** -8 * np.abs(want) + A * (2.0 ** -11 + 2 * ds + 2.0 ** -14) + n * 2.0 ** -25 * vm / l
                         bad = ~(np.isclose(o, want, rtol=0, atol=0, equal_nan=True) | (np.abs(o - want) <= tol))
                         assert not bad.any(), (b, j, hq, np.flatnonzero(bad)[:4], o[bad][:4], want[bad][:4])
@@ -423,3 +430,18 @@ def test_pack_then_attention(torch):
                 # e^(2 * 2^-4 S) - 1 of the weights
                 ds = 2.0 ** -4 * S
                 assert (np.abs(out[j, hq * D:(hq + 1) * D] - want) <= A * (2.0 ** -4 * math.exp(2 * ds) + math.expm1(2 * ds) + 2.0 ** -7)).all()
+
+
+def test_attention_queries_that_are_not_finite_or_tiny(torch):
+    """NaN and infinities in a query make its own row NaN; queries of any magnitude keep their digits."""
+    for D in (64, 128):
+        c = Case(torch, 20, 4, 2, D, [200], [2], _causal([200], 5))
+        c.q[1, 3], c.q[2, D + 7], c.q[2, 2 * D] = 0x7FC0, 0x7F80, 0xFF80
+        c.check()
+        for amp in (1e-38, 1e-30, 1e-3, 1e4):
+            c = Case(torch, 21, 4, 2, D, [200], [2], _causal([200], 5))
+            c.q = ref.bf16(ref.bf16_value(c.q) * amp)
+            c.check()
+        c = Case(torch, 22, 4, 2, D, [200], [2], _causal([200], 5))   # elements of one query far apart
+        c.q = ref.bf16(ref.bf16_value(c.q) * np.exp2(np.random.default_rng(1).integers(-30, 4, c.q.shape)))
+        c.check()
