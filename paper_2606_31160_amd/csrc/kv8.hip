@@ -594,30 +594,28 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
           else
             qf[rb][h] = qb[rb][h];
         }
+      // (products on one accumulator stand apart, or the second waits for the first)
+      f32x4 acc[4][NRB];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f32x4 acc[NRB];
+      for (int t = 0; t < 4; t += 2)
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) acc[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (kNative) {
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) {
-            acc[rb] = mfma_e4m3<127>(kr[t], qf[rb][0], acc[rb]);
-            acc[rb] = mfma_e4m3<123>(kr[t], qf[rb][1], acc[rb]);
-          }
-        } else {
-          const u32x4 lo = bf16_of_e4m3(kr[t].x, kr[t].y), hi = bf16_of_e4m3(kr[t].z, kr[t].w);
+          for (int k = t; k < t + 2; ++k)
 #pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) {
-            acc[rb] = mfma16x16x32(lo, qf[rb][0], acc[rb]);
-            acc[rb] = mfma16x16x32(hi, qf[rb][1], acc[rb]);
-          }
-        }
+            for (int rb = 0; rb < NRB; ++rb) {
+              const f32x4 c = e ? acc[k][rb] : f32x4{0.f, 0.f, 0.f, 0.f};
+              if constexpr (kNative)
+                acc[k][rb] = e ? mfma_e4m3<123>(kr[k], qf[rb][1], c) : mfma_e4m3<127>(kr[k], qf[rb][0], c);
+              else
+                acc[k][rb] = mfma16x16x32(e ? bf16_of_e4m3(kr[k].z, kr[k].w) : bf16_of_e4m3(kr[k].x, kr[k].y), qf[rb][e], c);
+            }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[rb][i];
-      }
+          for (int i = 0; i < 4; ++i) s[rb][4 * t + i] = acc[t][rb][i];
       __builtin_amdgcn_sched_barrier(0);
       load_k(nat);
       if (!full) mask(s, k0, sound ? INT32_MAX : 0);
@@ -656,14 +654,15 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
         if (__any(odd != 0)) odd_pages |= 1ull << p;
       }
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        const u32x4 lo = f16_of_e4m3(vr[dt].x, vr[dt].y), hi = f16_of_e4m3(vr[dt].z, vr[dt].w);
+      for (int dt = 0; dt < NDT; dt += 2)
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-          st.o[rb][dt] = mfma_f16(lo, pb[rb][0], st.o[rb][dt]);
-          st.o[rb][dt] = mfma_f16(hi, pb[rb][1], st.o[rb][dt]);
-        }
-      }
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int k = dt; k < dt + 2; ++k) {
+            const u32x4 v = e ? f16_of_e4m3(vr[k].z, vr[k].w) : f16_of_e4m3(vr[k].x, vr[k].y);
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) st.o[rb][k] = mfma_f16(v, pb[rb][e], st.o[rb][k]);
+          }
       __builtin_amdgcn_sched_barrier(0);
       load_v(nat);
       if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
@@ -936,11 +935,12 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroups that run at once: one of 8 waves or two of 4 waves a CU.
-int kv8_target_groups(int rows, int ncu) {
-  const Shape s = shape_of(rows);
-  return std::max(1, 2 * ncu / (s.wr * s.y));
-}
+// One workgroup per CU: fewer pages each, in two workgroups of 4 waves per CU or in
+// further rounds, cost their prologues (about 5 us before the first product).  Per
+// call, groups aimed at 256 / 512 / 1024: 16 scenes of 2 to 8 thousand tokens, one row
+// each, 21.8 / 23.7 / 25.4 us, 9 rows 35.3 / 43.8 / 51.0; one of 131 thousand tokens 27.7 /
+// 40.1 / 40.0.
+int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
 
 // Where the lengths decide, count_groups stops at `target`, or at kKv8MaxPages, or
 // (with more heads of sequences than that) takes 4 floor(n / target) pages where n
