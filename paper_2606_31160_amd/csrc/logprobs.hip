@@ -37,13 +37,42 @@ __device__ __forceinline__ float load_one(const void* p, int64_t i) {
 
 // The largest T with at least n lanes' keys >= T, of keys below 2^bits: the n-th
 // largest key if all differ.
-__device__ __forceinline__ uint64_t nth_largest(uint64_t key, int n, int bits) {
-  uint64_t t = 0;
+template <class K>
+__device__ __forceinline__ K nth_largest(K key, int n, int bits) {
+  K t = 0;
   for (int b = bits - 1; b >= 0; --b) {
-    const uint64_t c = t | (1ull << b);
+    const K c = t | ((K)1 << b);
     if (__popcll(__ballot(key >= c)) >= n) t = c;
   }
   return t;
+}
+
+// Sum and maximum over a wave, in every lane, by lane moves within the vector unit.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float x, float other) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(other), (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+__device__ __forceinline__ float wave_add(float x) {
+  x += dpp<0x111, 0xf>(x, 0.f);
+  x += dpp<0x112, 0xf>(x, 0.f);
+  x += dpp<0x114, 0xf>(x, 0.f);
+  x += dpp<0x118, 0xf>(x, 0.f);
+  x += dpp<0x142, 0xa>(x, 0.f);
+  x += dpp<0x143, 0xc>(x, 0.f);
+  return last_lane(x);
+}
+// NaN if a lane holds one.
+__device__ __forceinline__ float wave_max(float x) {
+  x = __builtin_elementwise_maximum(x, dpp<0x111, 0xf>(x, -INFINITY));
+  x = __builtin_elementwise_maximum(x, dpp<0x112, 0xf>(x, -INFINITY));
+  x = __builtin_elementwise_maximum(x, dpp<0x114, 0xf>(x, -INFINITY));
+  x = __builtin_elementwise_maximum(x, dpp<0x118, 0xf>(x, -INFINITY));
+  x = __builtin_elementwise_maximum(x, dpp<0x142, 0xa>(x, -INFINITY));
+  x = __builtin_elementwise_maximum(x, dpp<0x143, 0xc>(x, -INFINITY));
+  return last_lane(x);
 }
 
 // Sorts the n largest of c distinct keys in LDS: the key of rank r goes to put(r, key).
@@ -92,12 +121,17 @@ __device__ __forceinline__ Scores scores(float M, float S, float N, float T) {
   return r;
 }
 
+// The logits of the given tokens, on their way while the row is summed: thread g
+// has token g (further ones are loaded when they are written).
 template <int DT>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, const Scores& z) {
-  for (int g = threadIdx.x; g < a.ng; g += kThreads) {
-    const int t = a.given[(size_t)row * a.ng + g];
-    a.lp[(size_t)row * a.ng + g] = t >= 0 && t < a.V ? (load_one<DT>(a.x, (int64_t)row * a.stride + t) - z.M) - z.Z : NAN;
-  }
+__device__ __forceinline__ float given_logit(const LogprobArgs& a, int row, int g) {
+  const int t = a.given[(size_t)row * a.ng + g];
+  return t >= 0 && t < a.V ? load_one<DT>(a.x, (int64_t)row * a.stride + t) : NAN;
+}
+template <int DT>
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, const Scores& z, float first) {
+  for (int g = threadIdx.x; g < a.ng; g += kThreads)
+    a.lp[(size_t)row * a.ng + g] = ((g < kThreads ? first : given_logit<DT>(a, row, g)) - z.M) - z.Z;
   if (a.entropy && threadIdx.x == 0) a.entropy[row] = z.entropy;
 }
 __device__ __forceinline__ void write_top(const LogprobArgs& a, int row, int r, uint64_t key, const Scores& z) {
@@ -110,7 +144,12 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int row, int r, 
 // that equal logits go to the lowest index) for k_logprobs_join, or with one chunk
 // a row the results themselves.
 //   Candidates: n of a wave's 64 lane maxima are at least as large as the n-th
-// largest of them, so what is smaller is none of the n largest.
+// largest of them, so what is smaller is none of the n largest.  That takes one
+// comparison a logit; only the few that pass are put in order.  Where too many pass
+// (equal or masked logits) or too few (NaN), the same is done with whole keys, which
+// all differ.
+//   Bound by the arithmetic of a logit, about ten instructions with one exponential:
+// 144 rows of 152064 bf16 logits (44 MB).
 template <int DT, int E>
 __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   constexpr int NP = E / kPiece, NW = kThreads / 64;
@@ -122,6 +161,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   __shared__ int count;
   const int row = blockIdx.y, split = blockIdx.x, wave = threadIdx.x >> 6;
   const int base = split * kThreads * E;
+  const bool one = gridDim.x == 1;
   const char* const p = static_cast<const char*>(a.x) + (int64_t)row * a.stride * (DT == SPEC_F32 ? 4 : 2);
   const bool aligned = (reinterpret_cast<uintptr_t>(p) & 15) == 0;   // whole pieces in one or two loads
   float x[E];
@@ -147,37 +187,79 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
       for (int k = 0; k < kPiece; ++k) x[8 * i + k] = at + k < a.V ? load_one<DT>(p, at + k) : -INFINITY;
     }
   }
+  const float given = one && (int)threadIdx.x < a.ng ? given_logit<DT>(a, row, threadIdx.x) : 0.f;
   if (threadIdx.x == 0) count = 0;
-  float m = x[0];
+  float lm = x[0];                                  // the lane's maximum; NaN if there is one
 #pragma unroll
-  for (int i = 1; i < E; ++i) m = fmaxf(m, x[i]);
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  for (int i = 1; i < E; ++i) lm = __builtin_elementwise_maximum(lm, x[i]);
+  float m = wave_max(lm);
   if ((threadIdx.x & 63) == 0) red[wave][0] = m;
+  if (a.top) {
+    const uint32_t w = nth_largest(order_of(lm) >> kLow, a.top, 32 - kLow);
+    if ((threadIdx.x & 63) == 0) thr[wave] = w;
+  }
   __syncthreads();
-  m = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+  m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(red[0][0], red[1][0]),
+                                    __builtin_elementwise_maximum(red[2][0], red[3][0]));
+  const bool nan = m != m;                          // workgroup-uniform
   const float mm = m == -INFINITY ? 0.f : m;
   float s = 0.f, n = 0.f, t = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float d = x[i] - mm;
-    const float e = x[i] == mm ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
-    n += x[i] == mm ? 1.f : 0.f;
+    const float d = fmaxf(x[i] - mm, -200.f);       // (e is zero there, no matter how far below)
+    const float e = __builtin_amdgcn_exp2f(d * kLog2e);
     s += e;
-    t = __builtin_fmaf(e, fmaxf(d, -200.f), t);     // (where e is zero, no matter how far below)
+    t = __builtin_fmaf(e, d, t);
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    s += __shfl_xor(s, o);
-    n += __shfl_xor(n, o);
-    t += __shfl_xor(t, o);
+  if (lm == m) {                                    // S without the maximum itself
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const bool is = x[i] == m;
+      n += is ? 1.f : 0.f;
+      s += is ? 0.f : __builtin_amdgcn_exp2f((x[i] - mm) * kLog2e);
+    }
   }
+  s = wave_add(s);
+  n = wave_add(n);
+  t = wave_add(t);
   if ((threadIdx.x & 63) == 0) red[wave][1] = s, red[wave][2] = n, red[wave][3] = t;
 
   // keys of this thread's logits within the chunk; 0: none
+  auto local_of = [&](int i) { return ((i / kPiece) * kThreads + (int)threadIdx.x) * kPiece + i % kPiece; };
   auto key_of = [&](int i) -> uint64_t {
-    const int local = ((i / kPiece) * kThreads + (int)threadIdx.x) * kPiece + i % kPiece;
-    return base + local < a.V ? ((uint64_t)(order_of(x[i]) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - local) : 0ull;
+    const int l = local_of(i);
+    return base + l < a.V ? ((uint64_t)(order_of(x[i]) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
   };
   if (a.top) {
+    uint32_t w = (uint32_t)thr[0];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) w = max(w, (uint32_t)thr[k]);
+    // (-0 and 0 are equal in floating point; below the lowest number all pass)
+    const float least = w > 0 ? value_of(w << kLow | (kLow && !(w >> 15) ? 0xffffu : 0u)) : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (x[i] >= least && base + local_of(i) < a.V) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kThreads) list[at] = ((uint64_t)order_of(x[i]) << 32) | (uint32_t)~(base + local_of(i));
+      }
+  }
+  __syncthreads();
+  s = red[0][1] + red[1][1] + red[2][1] + red[3][1];
+  n = red[0][2] + red[1][2] + red[2][2] + red[3][2];
+  t = red[0][3] + red[1][3] + red[2][3] + red[3][3];
+  const size_t at = (size_t)row * a.splits + split;
+  Scores z{};
+  if (one) {
+    z = scores(m, s, n, t);
+    write_row<DT>(a, row, z, given);
+  } else if (threadIdx.x == 0) {
+    a.stats[at] = make_float4(m, s, n, t);
+  }
+  if (!a.top) return;
+  int c = count;
+  const int have = min(a.V - base, kThreads * E);   // logits of the chunk
+  if (nan || c > kThreads || c < min(a.top, have)) {
     uint64_t big = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -185,35 +267,19 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
       big = k > big ? k : big;
     }
     const uint64_t w = nth_largest(big, a.top, 32 - kLow + kLocalBits);
+    __syncthreads();
     if ((threadIdx.x & 63) == 0) thr[wave] = w;
-  }
-  __syncthreads();
-  s = red[0][1] + red[1][1] + red[2][1] + red[3][1];
-  n = red[0][2] + red[1][2] + red[2][2] + red[3][2];
-  t = red[0][3] + red[1][3] + red[2][3] + red[3][3];
-  const bool one = gridDim.x == 1;
-  const size_t at = (size_t)row * a.splits + split;
-  Scores z{};
-  if (one) {
-    z = scores(m, s, n, t);
-    write_row<DT>(a, row, z);
-  } else if (threadIdx.x == 0) {
-    a.stats[at] = make_float4(m, s, n, t);
-  }
-  if (!a.top) return;
-  uint64_t least = 1;                               // (0 is no logit)
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    uint64_t least = 1;                             // (0 is no logit)
 #pragma unroll
-  for (int w = 0; w < NW; ++w) least = thr[w] > least ? thr[w] : least;
+    for (int k = 0; k < NW; ++k) least = thr[k] > least ? thr[k] : least;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const uint64_t k = key_of(i);
-    if (k >= least) {
-      const uint32_t local = (1u << kLocalBits) - 1 - (uint32_t)(k & ((1u << kLocalBits) - 1));
-      list[atomicAdd(&count, 1)] = ((uint64_t)order_of(x[i]) << 32) | (uint32_t)~(base + local);
-    }
+    for (int i = 0; i < E; ++i)
+      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = ((uint64_t)order_of(x[i]) << 32) | (uint32_t)~(base + local_of(i));
+    __syncthreads();
+    c = count;
   }
-  __syncthreads();
-  const int c = count;
   // a chunk at the end of the row may hold fewer logits than `top`
   if (!one && (int)threadIdx.x < a.top && (int)threadIdx.x >= c) a.keys[at * a.top + threadIdx.x] = 0;
   rank_keys(list, c, min(a.top, c), best, [&](int r, uint64_t k) {
@@ -227,58 +293,54 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
 // Joins the chunks of a row: grid (rows).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a) {
+  constexpr int kLow = DT == SPEC_BF16 ? 16 : 0;
   __shared__ uint64_t list[kMaxSplits * SPEC_MAX_TOP], few[kThreads], best[kThreads / 64];
   __shared__ int count;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const float4* st = a.stats + (size_t)row * a.splits;
-  if (threadIdx.x == 0) count = 0;
-  // every wave sums the statistics for itself
-  float M = -INFINITY;
-  for (int i = lane; i < a.splits; i += 64) M = fmaxf(M, st[i].x);
-  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-  float S = 0.f, N = 0.f, T = 0.f;
-  for (int i = lane; i < a.splits; i += 64) {
-    const float4 c = st[i];
-    if (c.x == M) {
-      S += c.y, N += c.z, T += c.w;
-    } else if (c.x > -INFINITY) {
-      const float d = c.x - M, e = expf(d), k = c.y + c.z;
-      S += e * k;
-      T += e * (c.w + fmaxf(d, -200.f) * k);
-    } else {
-      S += c.y;                                     // zero, or NaN
-    }
-  }
-  for (int o = 32; o > 0; o >>= 1) {
-    S += __shfl_xor(S, o);
-    N += __shfl_xor(N, o);
-    T += __shfl_xor(T, o);
-  }
-  const Scores z = scores(M, S, N, T);
-  write_row<DT>(a, row, z);
-  if (!a.top) return;
   const int c = a.splits * a.top;
+  const float given = (int)threadIdx.x < a.ng ? given_logit<DT>(a, row, threadIdx.x) : 0.f;
+  if (threadIdx.x == 0) count = 0;
+  // every wave sums the statistics for itself: at most 128 chunks
+  float4 ch[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) ch[i] = lane + 64 * i < a.splits ? st[lane + 64 * i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
   for (int i = threadIdx.x; i < c; i += kThreads) list[i] = a.keys[(size_t)row * c + i];
+  const float M = wave_max(__builtin_elementwise_maximum(ch[0].x, ch[1].x));
+  float S = 0.f, N = 0.f, T = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (ch[i].x > -INFINITY) {
+      const float d = ch[i].x - M, e = d == 0.f ? 1.f : expf(d), k = ch[i].y + (d == 0.f ? 0.f : ch[i].z);
+      S += e * k;
+      N += d == 0.f ? ch[i].z : 0.f;
+      T += e * (ch[i].w + (d == 0.f ? 0.f : fmaxf(d, -200.f) * k));
+    }
+  S = wave_add(S);
+  N = wave_add(N);
+  T = wave_add(T);
+  const Scores z = scores(M, S, N, T);
+  write_row<DT>(a, row, z, given);
+  if (!a.top) return;
   __syncthreads();
-  // as in a chunk, with all keys spread over every wave's lanes
-  uint64_t big = 0;
-  for (int i = lane; i < c; i += 64) big = list[i] > big ? list[i] : big;
-  uint64_t least = nth_largest(big, a.top, 64);
-  if (least == 0) least = 1;
+  // as in a chunk, by the order alone, with all keys spread over every wave's lanes
+  uint32_t big = 0;
+  for (int i = lane; i < c; i += 64) big = max(big, (uint32_t)(list[i] >> (32 + kLow)));
+  const uint32_t least = max(nth_largest(big, a.top, 32 - kLow), 1u);
   for (int i = threadIdx.x; i < c; i += kThreads)
-    if (list[i] >= least) {
+    if ((uint32_t)(list[i] >> (32 + kLow)) >= least) {
       const int k = atomicAdd(&count, 1);
       if (k < kThreads) few[k] = list[i];
     }
   __syncthreads();
-  const bool fits = count <= kThreads;
+  const bool fits = count <= kThreads && count >= a.top;
   rank_keys(fits ? few : list, fits ? count : c, a.top, best, [&](int r, uint64_t k) { write_top(a, row, r, k, z); });
 }
 
-// Logits of a thread: as many as leave two chunks per CU, 8 to 32.
+// Logits of a thread: as many as leave a chunk per CU, 8 to 32.
 int per_thread(int rows, int V, int ncu) {
   for (int e = 32; e > kPiece; e /= 2)
-    if ((int64_t)rows * ((V + kThreads * e - 1) / (kThreads * e)) >= 2 * ncu || V > kMaxSplits * kThreads * (e / 2)) return e;
+    if ((int64_t)rows * ((V + kThreads * e - 1) / (kThreads * e)) >= ncu || V > kMaxSplits * kThreads * (e / 2)) return e;
   return kPiece;
 }
 
