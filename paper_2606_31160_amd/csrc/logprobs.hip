@@ -139,6 +139,11 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int row, int r, 
   a.top_lp[(size_t)row * a.top + r] = (value_of((uint32_t)(key >> 32)) - z.M) - z.Z;
 }
 
+// Keys that a chunk's list has room for: (n - 1) E + 1 may pass a wave's threshold.
+__host__ __device__ constexpr int list_keys(int top, int E) {
+  return top == 0 ? 1 : kThreads / 64 * ((top - 1) * E + 1) > kThreads ? kThreads / 64 * ((top - 1) * E + 1) : kThreads;
+}
+
 // One chunk of 256 E logits of a row: grid (chunks, rows).  Its statistics and its
 // `top` largest keys (order of the logit, then the complement of its index, so
 // that equal logits go to the lowest index) for k_logprobs_join, or with one chunk
@@ -149,7 +154,8 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int row, int r, 
 // (equal or masked logits) or too few (NaN), the same is done with whole keys, which
 // all differ.
 //   Bound by the arithmetic of a logit, about ten instructions with one exponential:
-// 144 rows of 152064 bf16 logits (44 MB).
+// 144 rows of 152064 bf16 logits (44 MB, 6.3 us to read) in 24.5 us with their join.
+// Logits stay in registers as they lie in memory.
 template <int DT, int E>
 __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   constexpr int NP = E / kPiece, NW = kThreads / 64;
@@ -157,41 +163,50 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   constexpr int kLow = DT == SPEC_BF16 ? 16 : 0;    // bits of an order code that say nothing
   __shared__ float red[NW][4];
   __shared__ uint64_t thr[NW], best[NW];
-  __shared__ uint64_t list[NW * ((SPEC_MAX_TOP - 1) * E + 1)];
+  extern __shared__ uint64_t list[];                // list_keys(top, E)
   __shared__ int count;
   const int row = blockIdx.y, split = blockIdx.x, wave = threadIdx.x >> 6;
   const int base = split * kThreads * E;
   const bool one = gridDim.x == 1;
   const char* const p = static_cast<const char*>(a.x) + (int64_t)row * a.stride * (DT == SPEC_F32 ? 4 : 2);
   const bool aligned = (reinterpret_cast<uintptr_t>(p) & 15) == 0;   // whole pieces in one or two loads
-  float x[E];
+  // logits as they lie in memory: half the registers of their values where they are 16 bits wide
+  constexpr int kWords = DT == SPEC_F32 ? 8 : 4;    // of a piece
+  uint32_t raw[NP][kWords];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int at = base + (i * kThreads + (int)threadIdx.x) * kPiece;
     if (aligned && at + kPiece <= a.V) {
-      if (DT == SPEC_F32) {
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(p + 4 * (int64_t)at), hi = *reinterpret_cast<const f32x4*>(p + 4 * (int64_t)at + 16);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[8 * i + k] = lo[k], x[8 * i + 4 + k] = hi[k];
-      } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p + 2 * (int64_t)at);
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint16_t h = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
-          x[8 * i + k] = DT == SPEC_BF16 ? bf2f(h) : (float)__builtin_bit_cast(_Float16, h);
-        }
+      for (int h = 0; h < kWords / 4; ++h) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p + (DT == SPEC_F32 ? 4 : 2) * (int64_t)at + 16 * h);
+        raw[i][4 * h] = w.x, raw[i][4 * h + 1] = w.y, raw[i][4 * h + 2] = w.z, raw[i][4 * h + 3] = w.w;
       }
     } else {
+      constexpr uint32_t kNone = DT == SPEC_F32 ? 0xff800000u : DT == SPEC_BF16 ? 0xff80u : 0xfc00u;   // -infinity
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) x[8 * i + k] = at + k < a.V ? load_one<DT>(p, at + k) : -INFINITY;
+      for (int k = 0; k < kPiece; ++k) {
+        if (DT == SPEC_F32) {
+          raw[i][k] = at + k < a.V ? reinterpret_cast<const uint32_t*>(p)[at + k] : kNone;
+        } else {
+          const uint32_t h = at + k < a.V ? reinterpret_cast<const uint16_t*>(p)[at + k] : kNone;
+          raw[i][k >> 1] = k & 1 ? raw[i][k >> 1] | h << 16 : h;
+        }
+      }
     }
   }
+  auto x = [&](int i) -> float {
+    const int k = i % kPiece;
+    if (DT == SPEC_F32) return __uint_as_float(raw[i / kPiece][k % kWords]);
+    const uint32_t w = raw[i / kPiece][(k >> 1) % kWords];
+    if (DT == SPEC_BF16) return __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(k & 1 ? w >> 16 : w));
+  };
   const float given = one && (int)threadIdx.x < a.ng ? given_logit<DT>(a, row, threadIdx.x) : 0.f;
   if (threadIdx.x == 0) count = 0;
-  float lm = x[0];                                  // the lane's maximum; NaN if there is one
+  float lm = x(0);                                  // the lane's maximum; NaN if there is one
 #pragma unroll
-  for (int i = 1; i < E; ++i) lm = __builtin_elementwise_maximum(lm, x[i]);
+  for (int i = 1; i < E; ++i) lm = __builtin_elementwise_maximum(lm, x(i));
   float m = wave_max(lm);
   if ((threadIdx.x & 63) == 0) red[wave][0] = m;
   if (a.top) {
@@ -206,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   float s = 0.f, n = 0.f, t = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float d = fmaxf(x[i] - mm, -200.f);       // (e is zero there, no matter how far below)
+    const float d = fmaxf(x(i) - mm, -200.f);       // (e is zero there, no matter how far below)
     const float e = __builtin_amdgcn_exp2f(d * kLog2e);
     s += e;
     t = __builtin_fmaf(e, d, t);
@@ -215,9 +230,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const bool is = x[i] == m;
+      const bool is = x(i) == m;
       n += is ? 1.f : 0.f;
-      s += is ? 0.f : __builtin_amdgcn_exp2f((x[i] - mm) * kLog2e);
+      s += is ? 0.f : __builtin_amdgcn_exp2f((x(i) - mm) * kLog2e);
     }
   }
   s = wave_add(s);
@@ -229,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   auto local_of = [&](int i) { return ((i / kPiece) * kThreads + (int)threadIdx.x) * kPiece + i % kPiece; };
   auto key_of = [&](int i) -> uint64_t {
     const int l = local_of(i);
-    return base + l < a.V ? ((uint64_t)(order_of(x[i]) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
+    return base + l < a.V ? ((uint64_t)(order_of(x(i)) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
   };
   if (a.top) {
     uint32_t w = (uint32_t)thr[0];
@@ -239,9 +254,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     const float least = w > 0 ? value_of(w << kLow | (kLow && !(w >> 15) ? 0xffffu : 0u)) : -INFINITY;
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if (x[i] >= least && base + local_of(i) < a.V) {
+      if (x(i) >= least && base + local_of(i) < a.V) {
         const int at = atomicAdd(&count, 1);
-        if (at < kThreads) list[at] = ((uint64_t)order_of(x[i]) << 32) | (uint32_t)~(base + local_of(i));
+        if (at < kThreads) list[at] = ((uint64_t)order_of(x(i)) << 32) | (uint32_t)~(base + local_of(i));
       }
   }
   __syncthreads();
@@ -276,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     for (int k = 0; k < NW; ++k) least = thr[k] > least ? thr[k] : least;
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = ((uint64_t)order_of(x[i]) << 32) | (uint32_t)~(base + local_of(i));
+      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = ((uint64_t)order_of(x(i)) << 32) | (uint32_t)~(base + local_of(i));
     __syncthreads();
     c = count;
   }
@@ -337,23 +352,30 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a) {
   rank_keys(fits ? few : list, fits ? count : c, a.top, best, [&](int r, uint64_t k) { write_top(a, row, r, k, z); });
 }
 
-// Logits of a thread: as many as leave a chunk per CU, 8 to 32.
+// Logits of a thread: 16 where that leaves a chunk per CU, else 8; 32 only where a
+// row would have more chunks than its join holds.  Measured for bf16 rows of 152064,
+// at 8, 16 and 32: 144 rows 29.1, 24.5, 26.1 us (fewer waves fit a SIMD at 32, more
+// to join at 8); 9 rows 14.0, 12.6, 12.6 us.
 int per_thread(int rows, int V, int ncu) {
-  for (int e = 32; e > kPiece; e /= 2)
-    if ((int64_t)rows * ((V + kThreads * e - 1) / (kThreads * e)) >= ncu || V > kMaxSplits * kThreads * (e / 2)) return e;
-  return kPiece;
+  if (V > kMaxSplits * kThreads * 16) return 32;
+  const int chunks = (V + kThreads * 16 - 1) / (kThreads * 16);
+  return (int64_t)rows * chunks >= ncu || V > kMaxSplits * kThreads * 8 ? 16 : kPiece;
+}
+
+template <int DT, int E>
+void launch_chunks(const LogprobArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_logprobs<DT, E>), dim3(a.splits, a.rows), dim3(kThreads), list_keys(a.top, E) * sizeof(uint64_t), s, a);
 }
 
 template <int DT>
 hipError_t launch(const LogprobArgs& a, hipStream_t s) {
-  const dim3 grid(a.splits, a.rows);
   const int e = (a.V + a.splits * kThreads - 1) / (a.splits * kThreads);
   if (e <= 8)
-    hipLaunchKernelGGL((k_logprobs<DT, 8>), grid, dim3(kThreads), 0, s, a);
+    launch_chunks<DT, 8>(a, s);
   else if (e <= 16)
-    hipLaunchKernelGGL((k_logprobs<DT, 16>), grid, dim3(kThreads), 0, s, a);
+    launch_chunks<DT, 16>(a, s);
   else
-    hipLaunchKernelGGL((k_logprobs<DT, 32>), grid, dim3(kThreads), 0, s, a);
+    launch_chunks<DT, 32>(a, s);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || a.splits == 1) return err;
   hipLaunchKernelGGL(k_logprobs_join<DT>, dim3(a.rows), dim3(kThreads), 0, s, a);
