@@ -270,11 +270,6 @@ __device__ __forceinline__ float lane_f(float x, int l) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
 }
 
-__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-
 // A barrier for data in LDS that leaves loads from memory in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -334,17 +329,6 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
   }
 }
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ i32x8 join8(u32x4 a, u32x4 b) {
-  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-// 16x16x128 MFMA of e4m3 operands, lane's 32 bytes in any order that both share; the
-// second operand's numbers times 2^(EB - 127).
-template <int EB>
-__device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127, 0, EB);
-}
-
 // grid (groups, row blocks / (NRB WR)), WR x 4 waves: wave w has row blocks NRB (w %
 // WR) .. and pages w / WR, + 4, .. of the group.
 //
@@ -356,10 +340,9 @@ __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
 //   The next page's keys are loaded while this one's softmax runs, its values while
 // the next scores are formed.  (Pages by way of LDS, for the two waves of WR = 2 at
 // once, took longer: 33 us where this takes 29.5, the waves in step at its barriers.)
-//   Keys of head dimension 128 go to the matrix unit as they are, in 16x16x128 MFMA of
-// e4m3 numbers: Q = 2^e (hi + lo / 16) with hi = e4m3(Q / 2^e) and lo the rest, four
-// bits each, which is all of a bf16 number (an element below 2^-15 of the row's
-// largest is held to 2^-21 of that).  For 64 they are read as bf16, like Q.
+//   Keys are read as bf16, like Q: an e4m3 code is exact in it.  (16x16x128 MFMA
+// of e4m3 numbers, against Q in two parts of four bits each, took as long, and their
+// sums drop what is some 2^-16 of the largest product: scores 1e-5 off, not 1e-7.)
 //   Values and probabilities are read as fp16: an e4m3 code is exact in it, and a
 // probability keeps 11 bits, as a rounding to bf16 would show in the bf16 result.
 // The value scale is part of the probability's exponent: with u the largest one of
@@ -371,17 +354,12 @@ __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c) {
 template <int D, int NRB, int WR>
 __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int NDT = D / 16, KH = D / 64, ND4 = NDT / kKeyWaves;
-  constexpr bool kNative = D == 128;                // keys as e4m3 operands
   constexpr int kOp = kAttnChunk * D;               // bytes of a page's keys (or values)
-  typedef std::conditional_t<kNative, i32x8, u32x4> KeyBytes;   // a lane's part of a key operand
   __shared__ f32x4 s_o[WR][kKeyWaves][NDT][64];
   __shared__ float s_m[kKeyWaves][WR][NRB * 16], s_l[kKeyWaves][WR][NRB * 16];
   __shared__ int s_vis[WR * kKeyWaves][SPEC_MAX_ROWS];
   __shared__ uint64_t s_odd[kKeyWaves][WR];
-  // Q's e4m3 operands (hi, lo) and their 2^e, made by one wave for all: they are much work, and in registers they would not leave
-  // room for two pages
-  __shared__ u32x4 s_q[kNative ? WR : 1][kNative ? NRB : 1][2][2][64];
-  __shared__ float s_qs[WR][NRB * 16];
+  __shared__ u32x4 s_q[WR][NRB][2 * KH][64];        // Q's operands: in registers they would not leave room for two pages
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int n16 = lane & 15, g4 = lane >> 4;
@@ -418,7 +396,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // rows of this wave
   const int rows = a.R * a.G, r0 = (blockIdx.y * WR + wr) * NRB * 16;
   int vis[NRB], vmin = INT32_MAX, vmax = 0;
-  u32x4 q[2 * KH], qb[NRB][kNative ? 1 : 2];        // of row block wk / of all (what the 8-bit pages are read against)
+  u32x4 q[2 * KH];                                  // of row block wk
   // (a row that is not there reads one that is)
   auto q_at = [&](int rb, int& j) {
     const int r = r0 + 16 * rb + n16;
@@ -435,14 +413,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     vis[rb] = v < 0 ? INT32_MAX : v;                // rows that nobody asked for need no mask
     vmin = min(vmin, vis[rb]);
     vmax = max(vmax, v);
-    if constexpr (kNative) {
-      if (rb == wk)
+    if (rb == wk)
 #pragma unroll
-        for (int t = 0; t < 2 * KH; ++t) q[t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) qb[rb][t] = ld16(qp + 8 * t);
-    }
+      for (int t = 0; t < 2 * KH; ++t) q[t] = ld16(qp + 64 * (t >> 1) + 8 * (t & 1));
   }
   vmin = ~__builtin_amdgcn_readfirstlane(row_max(~vmin));
   vmax = __builtin_amdgcn_readfirstlane(row_max(vmax));      // slots that no row of this wave sees: from here
@@ -495,17 +468,14 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     uint64_t t8 = todo & (n8 >= 64 ? ~0ull : (1ull << n8) - 1);
 
     // a page on its way
-    KeyBytes kr[4];
+    u32x4 kr[4][KH];
     u32x4 vr[NDT];
     auto load_k = [&](size_t at) {
       const uint8_t* kp = a.k8 + at + krow * D + 16 * g4;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const u32x4* k = reinterpret_cast<const u32x4*>(kp + 4 * t * D);
-        if constexpr (kNative)
-          kr[t] = join8(k[0], k[4]);
-        else
-          kr[t] = k[0];
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kr[t][h] = *reinterpret_cast<const u32x4*>(kp + 4 * t * D + 64 * h);
       }
     };
     auto load_v = [&](size_t at) {
@@ -520,47 +490,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       load_k(at);
       load_v(at);
     }
-    if constexpr (kNative) {
-      if (wk < NRB) {
-        // 2^e: the smallest power of two with max |q| <= 448 2^e, as for a page, from the largest of the lane's 32 bf16
-        // magnitudes and its row's other three lanes (one that is not finite makes the row NaN whatever e is)
-        uint32_t big = 0;
+    if (wk < NRB)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) big = pk_max_u16(big, q[t][k] & 0x7fff7fffu);
-        big = max(big & 0xffffu, big >> 16);
-        big = max(big, (uint32_t)__shfl_xor((int)big, 16));
-        big = max(big, (uint32_t)__shfl_xor((int)big, 32));
-        const int e = min(max((int)(big >> 7) - ((big & 127) <= 96 ? 135 : 134), -120), 120);
-        const float inv = power_of_two(-e), inv16 = inv * 16.f;
-        if (g4 == 0) s_qs[wr][16 * wk + n16] = a.scale_log2 * power_of_two(e);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          u32x4 hi, lo;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            int c = 0, r = 0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t w = q[2 * h + (k >> 1)][2 * (k & 1) + i];
-              const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
-              const int y = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * inv, x1 * inv, 0, false);
-              const f32x2 d = __builtin_amdgcn_cvt_pk_f32_fp8(y, false);
-              const float z0 = __builtin_fmaf(x0, inv16, -16.f * d.x), z1 = __builtin_fmaf(x1, inv16, -16.f * d.y);
-              const int z = __builtin_amdgcn_cvt_pk_fp8_f32(z0, z1, 0, false);
-              c |= (y & 0xffff) << (16 * i);
-              r |= (z & 0xffff) << (16 * i);
-            }
-            hi[k] = (uint32_t)c;
-            lo[k] = (uint32_t)r;
-          }
-          s_q[wr][wk][0][h][lane] = hi;
-          s_q[wr][wk][1][h][lane] = lo;
-        }
-      }
-      lds_barrier();                                // with pages on their way
-    }
+      for (int t = 0; t < 2 * KH; ++t) s_q[wr][wk][t][lane] = q[t];
+    lds_barrier();                                  // with pages on their way
     // (the scales arrive before the pages)
     const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
     if (own && !fine && a.err) *a.err = SPEC_E_INVAL;
@@ -568,9 +501,6 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const int um = wave_max(own && fine ? (int)__float_as_uint(vsc) : 0);   // (positive floats order as integers)
     if (um != 0) u = __uint_as_float((uint32_t)um);
     lv = (lane < n8 ? __builtin_amdgcn_logf(vsc) : 0.f) - __builtin_amdgcn_logf(u);
-    float qs[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) qs[rb] = kNative ? s_qs[wr][16 * rb + n16] : a.scale_log2;
 
     while (p < 64) {
       t8 &= t8 - 1;
@@ -582,34 +512,26 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       const bool sound = good >> p & 1;           // else a page without scales: not visible
       const bool full = sound && k0 + kAttnChunk <= vmin;
       float s[NRB][16];                           // scores of keys 16 g4 + i
-      KeyBytes qf[NRB][2];
+      u32x4 qf[NRB][2 * KH];
       int ql = lane;
       asm volatile("" : "+v"(ql));                // (read again for every page)
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if constexpr (kNative)
-            qf[rb][h] = join8(s_q[wr][rb][h][0][ql], s_q[wr][rb][h][1][ql]);
-          else
-            qf[rb][h] = qb[rb][h];
-        }
+        for (int h = 0; h < 2 * KH; ++h) qf[rb][h] = s_q[wr][rb][h][ql];
       // (products on one accumulator stand apart, or the second waits for the first)
       f32x4 acc[4][NRB];
 #pragma unroll
       for (int t = 0; t < 4; t += 2)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int h = 0; h < 2 * KH; ++h)
 #pragma unroll
-          for (int k = t; k < t + 2; ++k)
+          for (int k = t; k < t + 2; ++k) {
+            const u32x4 w = kr[k][h >> 1];
+            const u32x4 x = h & 1 ? bf16_of_e4m3(w.z, w.w) : bf16_of_e4m3(w.x, w.y);
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) {
-              const f32x4 c = e ? acc[k][rb] : f32x4{0.f, 0.f, 0.f, 0.f};
-              if constexpr (kNative)
-                acc[k][rb] = e ? mfma_e4m3<123>(kr[k], qf[rb][1], c) : mfma_e4m3<127>(kr[k], qf[rb][0], c);
-              else
-                acc[k][rb] = mfma16x16x32(e ? bf16_of_e4m3(kr[k].z, kr[k].w) : bf16_of_e4m3(kr[k].x, kr[k].y), qf[rb][e], c);
-            }
+            for (int rb = 0; rb < NRB; ++rb) acc[k][rb] = mfma16x16x32(x, qf[rb][h], h ? acc[k][rb] : f32x4{0.f, 0.f, 0.f, 0.f});
+          }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -624,7 +546,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       const float rest = far != 0.f ? __builtin_amdgcn_exp2f(off + far) : 1.f;
       float sc[NRB];
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) sc[rb] = fmaxf(qs[rb] * lane_f(ks, p), 1e-37f);
+      for (int rb = 0; rb < NRB; ++rb) sc[rb] = fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f);
       u32x4 pb[NRB][2];
       soft(st, s, sc, far != 0.f ? kHead : off + kHead, [&](int rb, float (&x)[16]) {
         if (rest != 1.f)

@@ -239,13 +239,6 @@ class Case:
                         # score, the normalisation), by half a step of fp16, 2^-11 or at most 2^-25 where it is that
                         # small, and the result by half a step of bf16, 2^-8; 2^-14 A for what is summed in 32 bits.
                         ds = (self.D + 8) * 2.0 ** -24 * S
-                        if self.D == 128 and n > 0:
-                            # Against keys of 128 dimensions a query is 2^e (hi + lo / 16) of e4m3 numbers, with 448 2^e the
-                            # first of its kind not below max |q|, so max |q| > 224 2^e.  Where four bits each do not hold
-                            # an element to its last bit, half of e4m3's smallest step, 2^-9, is lost of lo: 2^-14 2^e <
-                            # 2^-14 / 224 max |q| < 2^-21 max |q| an element.
-                            with np.errstate(invalid="ignore"):
-                                ds += 2.0 ** -21 * np.abs(q).max() * np.nanmax(np.abs(k[:n]).sum(1)) * self.scale
                         tol = 2.0 ** -8 * np.abs(want) + A * (2.0 ** -11 + 2 * ds + 2.0 ** -14) + n * 2.0 ** -25 * vm / l
                         bad = ~(np.isclose(o, want, rtol=0, atol=0, equal_nan=True) | (np.abs(o - want) <= tol))
                         assert not bad.any(), (b, j, hq, np.flatnonzero(bad)[:4], o[bad][:4], want[bad][:4])
@@ -339,6 +332,35 @@ def test_attention_far_scales(torch):
 def test_attention_sharp_rows(torch):
     """Scores of a wide range: most probabilities underflow."""
     Case(torch, 12, 4, 1, 128, [400], [5], _causal([400], 9), amp=6.0).check()
+
+
+@pytest.mark.parametrize("D,packed", [(64, 1), (128, 1), (64, 0), (128, 0)])
+def test_attention_scores_are_summed_in_32_bits(torch, D, packed):
+    """Queries are whole numbers up to 255, a quarter of a key's numbers 32 to 448, the rest 2 to 7.5 in steps of 1/4
+    and more: any sum of products is a whole number of 1/4 and at most 32 448 255 + 96 7.5 255 < 2^22, exact in 32
+    bits in any order.  One key is visible, so lse is its score: off by the roundings of its factor, of itself, of its
+    difference from itself and of the change of logarithm's base (two), half a step each, of at most its magnitude
+    and 1."""
+    c = Case(torch, 16, 28, 4, D, [PAGE], [packed], np.ones((1, 5), np.int32))
+    rng = np.random.default_rng(17)
+    c.q = ref.bf16(rng.integers(128, 256, c.q.shape) * rng.choice([-1, 1], c.q.shape))
+
+    def codes(shape):                             # [..., D]
+        large = np.arange(D) % 4 == 0
+        return (np.where(large, rng.integers(0x60, 0x7F, shape), rng.integers(0x40, 0x50, shape)) |
+                rng.choice([0, 0x80], shape)).astype(np.uint8)
+
+    c.k8, c.k16 = codes(c.k8.shape), ref.bf16(ref.e4m3_value(codes(c.k16.shape)))
+    c.ks[:] = 1.0
+    c.scale = 2.0 ** -14
+    _, lse = c.run()
+    for h in range(4):
+        k, _ = c.keys_values(0, h)
+        for j in range(5):
+            for g in range(7):
+                q = ref.bf16_value(c.q[j, (7 * h + g) * D:(7 * h + g + 1) * D])
+                want = float(q @ k[0]) * c.scale
+                assert abs(lse[j, 7 * h + g] - want) <= 5 * 2.0 ** -24 * (abs(want) + 1), (j, h, g, lse[j, 7 * h + g], want)
 
 
 def test_attention_bad_pages_and_lengths(torch):
