@@ -153,9 +153,11 @@ __host__ __device__ constexpr int list_keys(int top, int E) {
 // comparison a logit; only the few that pass are put in order.  Where too many pass
 // (equal or masked logits) or too few (NaN), the same is done with whole keys, which
 // all differ.
-//   Bound by the arithmetic of a logit, about ten instructions with one exponential:
-// 144 rows of 152064 bf16 logits (44 MB, 6.3 us to read) in 24.5 us with their join.
-// Logits stay in registers as they lie in memory.
+//   Bound by its vector instructions (some 20 a logit with a chunk's fixed part, one of
+// them an exponential): 144 rows of 152064 bf16 logits, 44 MB that take 6.3 us to read,
+// take 21.0 us with their join.
+//   Logits stay in registers as they lie in memory; the paths that few chunks take
+// read them again, and so cost no registers.
 template <int DT, int E>
 __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   constexpr int NP = E / kPiece, NW = kThreads / 64;
@@ -221,10 +223,17 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   float s = 0.f, n = 0.f, t = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float d = fmaxf(x(i) - mm, -200.f);       // (e is zero there, no matter how far below)
-    const float e = __builtin_amdgcn_exp2f(d * kLog2e);
+    const float d = x(i) - mm, e = __builtin_amdgcn_exp2f(d * kLog2e);
     s += e;
     t = __builtin_fmaf(e, d, t);
+  }
+  if (t != t) {                                     // 0 times -infinity, of logits that are it
+    t = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float d = x(i) - mm, e = __builtin_amdgcn_exp2f(d * kLog2e);
+      t = __builtin_fmaf(e, fmaxf(d, -200.f), t);   // (e is zero there, no matter how far below)
+    }
   }
   if (lm == m) {                                    // S without the maximum itself
     s = 0.f;
@@ -240,24 +249,29 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   t = wave_add(t);
   if ((threadIdx.x & 63) == 0) red[wave][1] = s, red[wave][2] = n, red[wave][3] = t;
 
-  // keys of this thread's logits within the chunk; 0: none
+  // the i-th logit's place within the chunk, and its key there, from memory; 0: none
   auto local_of = [&](int i) { return ((i / kPiece) * kThreads + (int)threadIdx.x) * kPiece + i % kPiece; };
   auto key_of = [&](int i) -> uint64_t {
     const int l = local_of(i);
-    return base + l < a.V ? ((uint64_t)(order_of(x(i)) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
+    return base + l < a.V ? ((uint64_t)(order_of(load_one<DT>(p, base + l)) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
   };
+  auto listed = [&](float v, int i) { return ((uint64_t)order_of(v) << 32) | (uint32_t)~(base + local_of(i)); };
+  bool plain = false;                               // candidates by value; uniform
   if (a.top) {
     uint32_t w = (uint32_t)thr[0];
 #pragma unroll
     for (int k = 1; k < NW; ++k) w = max(w, (uint32_t)thr[k]);
     // (-0 and 0 are equal in floating point; below the lowest number all pass)
     const float least = w > 0 ? value_of(w << kLow | (kLow && !(w >> 15) ? 0xffffu : 0u)) : -INFINITY;
+    plain = !nan && least > -INFINITY;
+    if (plain && __any(lm >= least)) {
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (x(i) >= least && base + local_of(i) < a.V) {
-        const int at = atomicAdd(&count, 1);
-        if (at < kThreads) list[at] = ((uint64_t)order_of(x(i)) << 32) | (uint32_t)~(base + local_of(i));
-      }
+      for (int i = 0; i < E; ++i)
+        if (x(i) >= least) {
+          const int at = atomicAdd(&count, 1);
+          if (at < kThreads) list[at] = listed(x(i), i);
+        }
+    }
   }
   __syncthreads();
   s = red[0][1] + red[1][1] + red[2][1] + red[3][1];
@@ -274,13 +288,10 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   if (!a.top) return;
   int c = count;
   const int have = min(a.V - base, kThreads * E);   // logits of the chunk
-  if (nan || c > kThreads || c < min(a.top, have)) {
+  if (!plain || c > kThreads || c < min(a.top, have)) {
     uint64_t big = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const uint64_t k = key_of(i);
-      big = k > big ? k : big;
-    }
+#pragma unroll 1
+    for (int i = 0; i < E; ++i) big = max(big, key_of(i));
     const uint64_t w = nth_largest(big, a.top, 32 - kLow + kLocalBits);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) thr[wave] = w;
@@ -289,9 +300,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     uint64_t least = 1;                             // (0 is no logit)
 #pragma unroll
     for (int k = 0; k < NW; ++k) least = thr[k] > least ? thr[k] : least;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < E; ++i)
-      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = ((uint64_t)order_of(x(i)) << 32) | (uint32_t)~(base + local_of(i));
+      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = listed(load_one<DT>(p, base + local_of(i)), i);
     __syncthreads();
     c = count;
   }
@@ -354,8 +365,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a) {
 
 // Logits of a thread: 16 where that leaves a chunk per CU, else 8; 32 only where a
 // row would have more chunks than its join holds.  Measured for bf16 rows of 152064,
-// at 8, 16 and 32: 144 rows 29.1, 24.5, 26.1 us (fewer waves fit a SIMD at 32, more
-// to join at 8); 9 rows 14.0, 12.6, 12.6 us.
+// at 16 and 32: 144 rows 21.0, 22.0 us, 9 rows 12.6, 12.9 us (fewer waves fit a SIMD);
+// at 8, of an earlier form, 144 rows took 29.1 where 16 took 25.4, 9 rows 14.0 and
+// 12.9 (more to join).
 int per_thread(int rows, int V, int ncu) {
   if (V > kMaxSplits * kThreads * 16) return 32;
   const int chunks = (V + kThreads * 16 - 1) / (kThreads * 16);
