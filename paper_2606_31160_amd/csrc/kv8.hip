@@ -738,7 +738,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 // of one row, as the partials do.
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
-  constexpr int NDT = D / 16, U = 4;
+  // groups of a wave loaded at once: of many, many; of few, no more than there are, as
+  // what is beyond is loaded all the same (4 for both: 36.5 and 27.9 us a call for 16
+  // scenes of 9 rows and one of 131 thousand tokens, not 34.2 and 26.4)
+  constexpr int NDT = D / 16, U = NW == 16 ? 8 : 2;
   __shared__ f32x4 s_o[NW][64];
   __shared__ float s_m[NW][16], s_l[NW][16];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
