@@ -341,8 +341,7 @@ spec_status spec_debug_feature(spec_ctx* ctx, int32_t b, int32_t slot0, int32_t 
 spec_status spec_debug_path(const spec_ctx* ctx, int32_t* path);
 
 /* Cache pages one attention workgroup takes in every pass (with SPEC_FLAG_KV8,
- * every target pass) of a context opened
- * with these arguments, into *pages (a pass with an armed readout takes one).
+ * every target pass) of a context opened with these arguments, into *pages (a pass with an armed readout takes one).
  * Does not synchronise; needs no context. */
 spec_status spec_debug_attn_pages(const spec_config* cfg, const spec_seq_init* seqs /* [batch] */, int32_t* pages);
 
@@ -407,15 +406,16 @@ typedef struct spec_kv8 {
 } spec_kv8;
 
 /* Packs the keys (as the cache holds them, after rotation) and values of `rows`
- * >= 1 tokens into 8-bit pages: rows [64 i, 64 i + 64) into pool page d_pages[i]
+ * (1..2^28) tokens into 8-bit pages: rows [64 i, 64 i + 64) into pool page d_pages[i]
  * (device int32, ceil(rows / 64) entries, no page twice).  k, v: bf16 rows of
  * [kv_heads][head_dim], 16-byte aligned, row_stride elements apart (a multiple of
  * 8; the rows may lie in a fused projection).  A page and head's scale is the
  * smallest power of two s, at least 2^-126, with max |x| <= 448 s over its finite
  * values (1 if all are zero); codes are x / s to nearest even.  NaN and infinities
  * become NaN.  Slots past the rows are set to zero.  What a page stands for is
- * exact in bf16 (but for magnitudes from 248 * 2^120, which round to 2^128).  An entry of d_pages outside the pool is skipped and sets *d_err
- * (device int32, may be NULL; otherwise left alone) to SPEC_E_INVAL. */
+ * exact in bf16 (but for magnitudes from 248 * 2^120, which round to 2^128).  An
+ * entry of d_pages outside the pool is skipped and sets *d_err (device int32, may be
+ * NULL; otherwise left alone) to SPEC_E_INVAL. */
 spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, int64_t row_stride, int32_t rows,
                           const int32_t* d_pages, int32_t* d_err, hipStream_t stream);
 
@@ -425,7 +425,8 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  *   out = sum_s p_s v_s,  p = softmax(scale * q . k_s),  lse = ln sum_s e^(scale * q . k_s).
  * n = 0: out = 0 and lse = -infinity.  n < 0: no such row; its out and lse are left
  * as they were.  Slots that a row does not see have no influence on it, whatever
- * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS.
+ * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS; rows*q_heads/kv_heads < 2^20;
+ * batch*kv_heads*table_stride <= 2^27.
  *   scale        positive and finite
  *   d_table      [batch][table_stride] device int32; entries past a sequence's
  *                visible pages are not read
@@ -436,8 +437,9 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  *   d_lse        [batch*rows][q_heads] device float, or NULL
  *   d_err        device int32 or NULL: set to SPEC_E_INVAL, else left alone, if a
  *                table entry lay outside its pool or a scale was not positive and
- *                finite (the page is then taken as not visible), or a row wanted
- *                more slots than the table has
+ *                finite (the page is then taken as not visible; a row that sees no
+ *                other has NaN in out and -infinity in lse), or a row wanted more
+ *                slots than the table has
  * Sums are formed in 32 bits, in an order fixed by the arguments and lengths. */
 spec_status spec_kv8_attn(const spec_kv8* cache, int32_t batch, int32_t rows, int32_t q_heads, const int32_t* d_table,
                           int32_t table_stride, const int32_t* d_packed, const int32_t* d_visible, const void* q,

@@ -14,6 +14,7 @@ using namespace specdec;
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int64_t kMaxRowsPerHead = 16 * 65535, kMaxPageHeads = 1 << 27, kMaxPackRows = 1 << 28;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned(const void* p, uintptr_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -47,7 +48,10 @@ const char* bad_pass(const spec_kv8* c, int32_t batch, int32_t rows, int32_t q_h
   if (batch < 1 || rows < 1 || (int64_t)batch * rows > SPEC_MAX_ROWS) return "batch and rows must be at least 1, batch*rows at most SPEC_MAX_ROWS";
   if (q_heads < 1 || q_heads % c->kv_heads) return "q_heads must be a multiple of kv_heads";
   if ((int64_t)q_heads * c->head_dim > (1 << 20)) return "q_heads*head_dim too large";
+  // (row blocks are a grid's second dimension; threads of all groups fit 32 bits)
+  if (rows * (int64_t)(q_heads / c->kv_heads) > kMaxRowsPerHead) return "rows*q_heads/kv_heads too large";
   if (table_stride < 1 || table_stride > INT32_MAX / SPEC_KV_PAGE) return "table_stride out of range";
+  if ((int64_t)batch * c->kv_heads * table_stride > kMaxPageHeads) return "batch*kv_heads*table_stride too large";
   return nullptr;
 }
 
@@ -83,7 +87,7 @@ spec_status spec_kv8_pack(const spec_kv8* c, const void* k, const void* v, int64
   if (const char* w = bad_cache(c, false)) return fail(SPEC_E_INVAL, f, w);
   if (c->pages8 < 1) return fail(SPEC_E_INVAL, f, "no 8-bit pages");
   if (c->kv_heads > 65535) return fail(SPEC_E_INVAL, f, "too many kv heads");
-  if (rows < 1) return fail(SPEC_E_INVAL, f, "rows must be at least 1");
+  if (rows < 1 || rows > kMaxPackRows) return fail(SPEC_E_INVAL, f, "rows must be 1..2^28");
   if (row_stride < (int64_t)c->kv_heads * c->head_dim || row_stride % 8)
     return fail(SPEC_E_INVAL, f, "row_stride must be a multiple of 8 and at least kv_heads*head_dim");
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(d_pages, 4) || (d_err && !aligned(d_err, 4)))

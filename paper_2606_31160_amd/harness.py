@@ -206,15 +206,16 @@ class Session:
         """Scores of the last verify's logits (of verify(logits=True)) after its commit: the log probability of every
         committed token under the target, each row's entropy and its `top` most probable tokens.  Returns the device
         tensors logprob [B, K+1] (row j: committed token j; valid where the commit's are), entropy [B, K+1],
-        top_token and top_logprob [B, K+1, top]."""
+        top_token and top_logprob [B, K+1, top], filled on the session's stream."""
         torch, n = self.torch, self.B * (self.K + 1)
-        out = {"logprob": torch.empty((self.B, self.K + 1), device=self.dev),
-               "entropy": torch.empty((self.B, self.K + 1), device=self.dev),
-               "top_token": torch.empty((self.B, self.K + 1, top), dtype=torch.int32, device=self.dev),
-               "top_logprob": torch.empty((self.B, self.K + 1, top), device=self.dev)}
         need = B.spec_logprobs_workspace_bytes(n, self.V, top)
-        if getattr(self, "_score_ws", None) is None or self._score_ws.numel() < need:
-            self._score_ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+        with torch.cuda.stream(self.stream):     # (memory that this stream has done with)
+            out = {"logprob": torch.empty((self.B, self.K + 1), device=self.dev),
+                   "entropy": torch.empty((self.B, self.K + 1), device=self.dev),
+                   "top_token": torch.empty((self.B, self.K + 1, top), dtype=torch.int32, device=self.dev),
+                   "top_logprob": torch.empty((self.B, self.K + 1, top), device=self.dev)}
+            if getattr(self, "_score_ws", None) is None or self._score_ws.numel() < need:
+                self._score_ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
         B.spec_logprobs(self.logits.data_ptr(), B.SPEC_BF16, n, self.V, self.V, self.com.data_ptr(), 1, top,
                         *(out[k].data_ptr() for k in ("logprob", "entropy", "top_token", "top_logprob")),
                         self._score_ws.data_ptr(), need, self.stream.cuda_stream)

@@ -429,6 +429,95 @@ def test_attention_is_the_same_every_time_and_in_a_graph(torch):
         c.d["vis"].copy_(vis)
 
 
+def test_attention_shared_pages_and_odd_page_counts(torch):
+    """Sequences on the same pages, as a shared prompt's; counts of 8-bit pages past the table and below zero."""
+    R = 2
+    c = Case(torch, 23, 4, 2, 64, [300, 300, 300], [5, 5, 5], _causal([300, 300, 300], R))
+    c.table[1] = c.table[0]
+    c.packed = [5, 2 ** 31 - 1, 5]
+    c.q[R:2 * R] = c.q[:R]
+    out, lse = c.run()
+    assert int(c.err) == 0 and (out[:R] == out[R:2 * R]).all() and (lse[:R] == lse[R:2 * R]).all()
+    c = Case(torch, 24, 4, 2, 64, [130], [0], _causal([130], R))
+    c.check()
+    want = c.out.clone()
+    c.packed = [-7]
+    c.run()
+    assert torch.equal(c.out, want)
+    lens = [(53 * i) % 190 + 2 for i in range(80)]   # the most sequences of two rows
+    Case(torch, 25, 2, 1, 64, lens, [n // PAGE for n in lens], _causal(lens, R)).check()
+
+
+def test_attention_rows_that_see_refused_pages_only(torch):
+    c = Case(torch, 26, 4, 2, 64, [PAGE, PAGE], [1, 1], _causal([PAGE, PAGE], 2))
+    c.table[0, 0] = -1
+    out, lse = c.run()
+    assert int(c.err) == 1 and np.isnan(out[:2]).all() and (lse[:2] == -math.inf).all()
+    assert np.isfinite(out[2:]).all() and np.isfinite(lse[2:]).all()
+
+
+def test_attention_two_at_once(torch):
+    """Two streams, a workspace each."""
+    cs = [Case(torch, 27 + i, 28, 4, 128, [2000 + 700 * i], [30], _causal([2000 + 700 * i], 9)) for i in range(2)]
+    for c in cs:
+        c.check()
+    want = [c.out.clone() for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    for c in cs:
+        c.out.fill_(3)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s in zip(cs, streams):
+            c.call(s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(c.out, w) for c, w in zip(cs, want))
+
+
+def test_attention_pages_far_into_their_pools(torch):
+    """Pages whose first byte is past 2^32 in every pool."""
+    c = Case(torch, 29, 8, 4, 128, [300], [3], _causal([300], 3), extra=0)
+    c.check()
+    want = c.out.clone()
+    for pool, far in (("k8", 2 ** 17), ("v8", 2 ** 17), ("k16", 2 ** 16), ("v16", 2 ** 16)):
+        x = c.d[pool]
+        big = torch.empty((far + 9,) + x.shape[1:], dtype=x.dtype, device="cuda")
+        assert big[far:].data_ptr() - big.data_ptr() >= 2 ** 32
+        big[far + 1:far + 1 + x.shape[0]] = x
+        c.d[pool] = big
+    for n in ("ks", "vs"):
+        x = c.d[n]
+        c.d[n] = torch.ones((2 ** 17 + 9,) + x.shape[1:], device="cuda")
+        c.d[n][2 ** 17 + 1:2 ** 17 + 1 + x.shape[0]] = x
+    c.d["table"][0, :3] += 2 ** 17 + 1
+    c.d["table"][0, 3:] += 2 ** 16 + 1
+    from paper_2606_31160_amd import binding as B
+    c.cache = B.kv8(4, 128, 2 ** 17 + 9, c.d["k8"].data_ptr(), c.d["v8"].data_ptr(), c.d["ks"].data_ptr(),
+                    c.d["vs"].data_ptr(), 2 ** 16 + 9, c.d["k16"].data_ptr(), c.d["v16"].data_ptr())
+    c.out.fill_(3)
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err) == 0 and torch.equal(c.out, want)
+
+
+def test_pack_rows_far_apart(torch):
+    """Rows whose offset passes 2^32 bytes."""
+    D, nkv, rows, stride = 64, 2, 130, 2 ** 24 + 8
+    rng = np.random.default_rng(30)
+    k, v = (ref.bf16(rng.standard_normal((rows, nkv * D))) for _ in range(2))
+    from paper_2606_31160_amd import binding as B
+    far = torch.empty((rows, stride), dtype=torch.int16, device="cuda")
+    far[:, :nkv * D], far[:, nkv * D:2 * nkv * D] = _dev(torch, k), _dev(torch, v)
+    k8 = torch.full((3, nkv, PAGE, D), 0xAB, dtype=torch.uint8, device="cuda")
+    v8 = torch.full((3, nkv, D, PAGE), 0xAB, dtype=torch.uint8, device="cuda")
+    ks, vs = torch.full((2, 3, nkv), -7.0, device="cuda")
+    to = torch.tensor([1, 2, 0], dtype=torch.int32, device="cuda")
+    c = B.kv8(nkv, D, 3, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr())
+    B.spec_kv8_pack(c, far.data_ptr(), far.data_ptr() + 2 * nkv * D, stride, rows, to.data_ptr(), 0,
+                    torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    _check_pages(k, v, nkv, D, [1, 2, 0], 3, (k8.cpu().numpy(), v8.cpu().numpy(), ks.cpu().numpy(), vs.cpu().numpy(), 0))
+
+
 def test_pack_then_attention(torch):
     """A prompt's rows packed and attended to, against the rows themselves: what 8 bits cost stays within their step."""
     nq, nkv, D, n = 8, 2, 128, 5 * PAGE

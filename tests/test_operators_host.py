@@ -54,6 +54,13 @@ def test_attention_refuses_bad_arguments(kw, text):
     refused(lambda: attn(cache(), **kw), INVAL, text)
 
 
+@pytest.mark.parametrize("cache_kw,kw,text", [
+    (dict(kv_heads=1), dict(batch=1, rows=70, q_heads=16384), "rows*q_heads/kv_heads"),
+    (dict(kv_heads=64), dict(batch=2, rows=1, q_heads=64, table_stride=2 ** 20 + 1), "batch*kv_heads*table_stride")])
+def test_attention_refuses_what_no_grid_holds(cache_kw, kw, text):
+    refused(lambda: attn(cache(**cache_kw), q_stride=1 << 20, out_stride=1 << 20, **kw), INVAL, text)
+
+
 def test_attention_refuses_a_small_workspace():
     n = B.spec_kv8_attn_workspace_bytes(cache(), 2, 3, 4, 5)
     assert n > 0
@@ -71,7 +78,7 @@ def test_attention_workspace_grows_with_the_pass_only():
 
 @pytest.mark.parametrize("kw,text", [
     (dict(k=0), "null"), (dict(v=P + 8), "misaligned"), (dict(row_stride=120), "row_stride"), (dict(row_stride=132), "row_stride"),
-    (dict(rows=0), "rows"), (dict(rows=-5), "rows"), (dict(d_pages=0), "null"), (dict(d_err=P + 1), "misaligned")])
+    (dict(rows=0), "rows"), (dict(rows=-5), "rows"), (dict(rows=2 ** 28 + 1), "rows"), (dict(d_pages=0), "null"), (dict(d_err=P + 1), "misaligned")])
 def test_pack_refuses_bad_arguments(kw, text):
     d = dict(k=P, v=P, row_stride=128, rows=64, d_pages=P, d_err=0, stream=0)
     d.update(kw)
