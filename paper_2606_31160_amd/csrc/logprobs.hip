@@ -153,11 +153,12 @@ __host__ __device__ constexpr int list_keys(int top, int E) {
 // comparison a logit; only the few that pass are put in order.  Where too many pass
 // (equal or masked logits) or too few (NaN), the same is done with whole keys, which
 // all differ.
-//   Bound by its vector instructions (some 20 a logit with a chunk's fixed part, one of
-// them an exponential): 144 rows of 152064 bf16 logits, 44 MB that take 6.3 us to read,
-// take 21.0 us with their join.
-//   Logits stay in registers as they lie in memory; the paths that few chunks take
-// read them again, and so cost no registers.
+//   Bound by its vector instructions (about eight a logit, one of them an exponential,
+// and a chunk's fixed part: maxima compared, sums joined, candidates): 144 rows of
+// 152064 bf16 logits, 44 MB that take 6.3 us to read, take 17.9 us with their join.
+//   Logits stay in registers as they lie in memory.  What only the few lanes with the
+// maximum or with candidates do is done for one such lane's logits by as many lanes,
+// read again: it takes few registers, so that 32 a thread leave 8 waves a SIMD.
 template <int DT, int E>
 __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   constexpr int NP = E / kPiece, NW = kThreads / 64;
@@ -204,6 +205,23 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     if (DT == SPEC_BF16) return __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
     return (float)__builtin_bit_cast(_Float16, (uint16_t)(k & 1 ? w >> 16 : w));
   };
+  // the place of thread t's i-th logit within the chunk
+  auto place_of = [](int i, int t) { return ((i / kPiece) * kThreads + t) * kPiece + i % kPiece; };
+  // f(place) for every logit of the given lanes of this wave, a lane each
+  auto each_of = [&](uint64_t lanes, auto f) {
+    const int lane = threadIdx.x & 63;
+    while (lanes) {
+      int from = -1;
+#pragma unroll
+      for (int k = 0; k < 64 / E; ++k)
+        if (lanes) {
+          if (lane / E == k) from = __builtin_ctzll(lanes);
+          lanes &= lanes - 1;
+        }
+      const int l = place_of(lane % E, 64 * wave + from);
+      if (from >= 0 && base + l < a.V) f(l);
+    }
+  };
   const float given = one && (int)threadIdx.x < a.ng ? given_logit<DT>(a, row, threadIdx.x) : 0.f;
   if (threadIdx.x == 0) count = 0;
   float lm = x(0);                                  // the lane's maximum; NaN if there is one
@@ -228,6 +246,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     t = __builtin_fmaf(e, d, t);
   }
   if (t != t) {                                     // 0 times -infinity, of logits that are it
+#pragma unroll
+    for (int i = 0; i < NP * kWords; ++i) asm volatile("" : "+v"(raw[i / kWords][i % kWords]));   // (formed again, not kept)
     t = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -235,27 +255,24 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
       t = __builtin_fmaf(e, fmaxf(d, -200.f), t);   // (e is zero there, no matter how far below)
     }
   }
-  if (lm == m) {                                    // S without the maximum itself
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const bool is = x(i) == m;
-      n += is ? 1.f : 0.f;
-      s += is ? 0.f : __builtin_amdgcn_exp2f((x(i) - mm) * kLog2e);
-    }
-  }
+  // S without the maximum itself, and how often it occurs: the few lanes that hold it, again
+  const bool has_max = lm == m;
+  if (has_max) s = 0.f;
+  each_of(__ballot(has_max), [&](int l) {
+    const float v = load_one<DT>(p, base + l);
+    n += v == m ? 1.f : 0.f;
+    s += v == m ? 0.f : __builtin_amdgcn_exp2f((v - mm) * kLog2e);
+  });
   s = wave_add(s);
   n = wave_add(n);
   t = wave_add(t);
   if ((threadIdx.x & 63) == 0) red[wave][1] = s, red[wave][2] = n, red[wave][3] = t;
 
-  // the i-th logit's place within the chunk, and its key there, from memory; 0: none
-  auto local_of = [&](int i) { return ((i / kPiece) * kThreads + (int)threadIdx.x) * kPiece + i % kPiece; };
-  auto key_of = [&](int i) -> uint64_t {
-    const int l = local_of(i);
+  // the key of a place within the chunk, from memory; 0: none
+  auto key_of = [&](int l) -> uint64_t {
     return base + l < a.V ? ((uint64_t)(order_of(load_one<DT>(p, base + l)) >> kLow) << kLocalBits) | (uint32_t)((1 << kLocalBits) - 1 - l) : 0ull;
   };
-  auto listed = [&](float v, int i) { return ((uint64_t)order_of(v) << 32) | (uint32_t)~(base + local_of(i)); };
+  auto listed = [&](float v, int l) { return ((uint64_t)order_of(v) << 32) | (uint32_t)~(base + l); };
   bool plain = false;                               // candidates by value; uniform
   if (a.top) {
     uint32_t w = (uint32_t)thr[0];
@@ -264,14 +281,14 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
     // (-0 and 0 are equal in floating point; below the lowest number all pass)
     const float least = w > 0 ? value_of(w << kLow | (kLow && !(w >> 15) ? 0xffffu : 0u)) : -INFINITY;
     plain = !nan && least > -INFINITY;
-    if (plain && __any(lm >= least)) {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (x(i) >= least) {
+    if (plain)
+      each_of(__ballot(lm >= least), [&](int l) {
+        const float v = load_one<DT>(p, base + l);
+        if (v >= least) {
           const int at = atomicAdd(&count, 1);
-          if (at < kThreads) list[at] = listed(x(i), i);
+          if (at < kThreads) list[at] = listed(v, l);
         }
-    }
+      });
   }
   __syncthreads();
   s = red[0][1] + red[1][1] + red[2][1] + red[3][1];
@@ -291,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
   if (!plain || c > kThreads || c < min(a.top, have)) {
     uint64_t big = 0;
 #pragma unroll 1
-    for (int i = 0; i < E; ++i) big = max(big, key_of(i));
+    for (int i = 0; i < E; ++i) big = max(big, key_of(place_of(i, threadIdx.x)));
     const uint64_t w = nth_largest(big, a.top, 32 - kLow + kLocalBits);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) thr[wave] = w;
@@ -301,8 +318,10 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a) {
 #pragma unroll
     for (int k = 0; k < NW; ++k) least = thr[k] > least ? thr[k] : least;
 #pragma unroll 1
-    for (int i = 0; i < E; ++i)
-      if (key_of(i) >= least) list[atomicAdd(&count, 1)] = listed(load_one<DT>(p, base + local_of(i)), i);
+    for (int i = 0; i < E; ++i) {
+      const int l = place_of(i, threadIdx.x);
+      if (key_of(l) >= least) list[atomicAdd(&count, 1)] = listed(load_one<DT>(p, base + l), l);
+    }
     __syncthreads();
     c = count;
   }
@@ -363,15 +382,16 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a) {
   rank_keys(fits ? few : list, fits ? count : c, a.top, best, [&](int r, uint64_t k) { write_top(a, row, r, k, z); });
 }
 
-// Logits of a thread: 16 where that leaves a chunk per CU, else 8; 32 only where a
-// row would have more chunks than its join holds.  Measured for bf16 rows of 152064,
-// at 16 and 32: 144 rows 21.0, 22.0 us, 9 rows 12.6, 12.9 us (fewer waves fit a SIMD);
-// at 8, of an earlier form, 144 rows took 29.1 where 16 took 25.4, 9 rows 14.0 and
-// 12.9 (more to join).
+// Logits of a thread: 32, half the fixed parts of 16, where that leaves four chunks a
+// CU (or a row has more logits than a join holds chunks of 16), else 16 where that
+// leaves one a CU, else 8.  Measured for bf16 rows of 152064, five alternatives, at
+// 16 and 32: 9 rows (0.7 chunks of 32 a CU) 8.7, 9.2 us, 36 rows (2.7) 10.9, 10.8, 72
+// rows (5.3) 14.1, 13.1, 144 rows 20.3, 17.9; at 8, of an earlier form, 9 rows took 14.0
+// where 16 took 12.9.
 int per_thread(int rows, int V, int ncu) {
-  if (V > kMaxSplits * kThreads * 16) return 32;
-  const int chunks = (V + kThreads * 16 - 1) / (kThreads * 16);
-  return (int64_t)rows * chunks >= ncu || V > kMaxSplits * kThreads * 8 ? 16 : kPiece;
+  auto chunks = [&](int e) { return (int64_t)rows * ((V + kThreads * e - 1) / (kThreads * e)); };
+  if (chunks(32) >= 4 * ncu || V > kMaxSplits * kThreads * 16) return 32;
+  return chunks(16) >= ncu || V > kMaxSplits * kThreads * 8 ? 16 : kPiece;
 }
 
 template <int DT, int E>

@@ -74,7 +74,7 @@ def _logits(torch, rng, n, V, dtype, pad=0, scale=2.5):
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("n,V,top,pad", [(1, 1, 1, 0), (1, 2, 2, 0), (3, 7, 3, 1), (2, 32, 32, 0), (5, 2047, 5, 0), (4, 2048, 20, 8),
                                          (4, 2049, 32, 3), (2, 8193, 1, 0), (3, 50257, 8, 7), (9, 152064, 20, 0),
-                                         (2, 1 << 20, 32, 0), (130, 4099, 4, 5), (2000, 300, 3, 0)])
+                                         (2, 1 << 20, 32, 0), (130, 4099, 4, 5), (2000, 300, 3, 0), (1100, 8201, 6, 1)])
 def test_scores(torch, dtype, n, V, top, pad):
     rng = np.random.default_rng(V + n)
     x = _logits(torch, rng, n, V, dtype, pad)
@@ -93,7 +93,7 @@ def test_sure_tokens_keep_their_digits(torch, V):
     _check(torch, x, V, given, 3, _call(torch, x, V, given, 3))
 
 
-@pytest.mark.parametrize("V", [64, 3000, 40000])
+@pytest.mark.parametrize("V", [64, 3000, 40000, 700001])
 @pytest.mark.parametrize("kind", ["all equal", "few values", "mostly masked", "one left", "sorted up", "sorted down", "lowest", "signed zeros"])
 def test_ties_masks_and_orders(torch, V, kind):
     rng = np.random.default_rng(V)
@@ -124,7 +124,7 @@ def test_ties_masks_and_orders(torch, V, kind):
         _check(torch, x, V, given, top, _call(torch, x, V, given, top))
 
 
-@pytest.mark.parametrize("V", [100, 20000])
+@pytest.mark.parametrize("V", [100, 20000, 700001])
 def test_rows_without_a_distribution(torch, V):
     rng = np.random.default_rng(V)
     a = rng.standard_normal((6, V)).astype(np.float32)
