@@ -37,7 +37,8 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 // Packing: one workgroup of 256 threads per (page, kv head, keys / values).  Keys
 // may be rotated on the way (a context's prompt), rounded to bf16 as the bf16
 // cache would hold them.  Infinities become NaN and count for no scale.  Slots
-// past the rows are zero.
+// past the rows are zero.  Bound by memory: 4096 tokens of 8 heads of 128, 17 MB read
+// and 8 MB written, 6.4 us a call in graphs (3.9 TB/s; a copy of 4 GiB reaches 4.7).
 // ---------------------------------------------------------------------------
 template <int D, bool ROT>
 __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
@@ -349,6 +350,11 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
 // the group, p vs / u 2^7 is in fp16's normal range down to 2^-21 (a page whose scale
 // is further below u has O turned to its own unit for as long).  bf16 pages take
 // their values as they are and each probability as the sum of two bf16 numbers.
+//   Bound by a wave's own chain, scores to softmax to value product, with two waves a
+// SIMD (of 16 scenes of 2 to 8 thousand tokens, 80 MB: 9 rows each 29.6 us, vector
+// unit 35% busy, matrix unit 14%; one row each 18.1 us, 4.4 TB/s), and where a wave has
+// a page or two by the loads before the first product, each waiting for the last:
+// about 5 us of 11.6 for 9 rows of one sequence of 4096.
 //   Which pages share a wave depends on the group only, and a row's sums on no
 // other row, so contexts that differ in K, and so in NRB and WR, sum alike.
 template <int D, int NRB, int WR>
@@ -735,7 +741,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 
 // Joins the groups of a (sequence, kv head): grid (sequences x kv heads, row
 // blocks, D / 16), NW waves, wave w groups w, w + NW, ..  A lane holds four columns
-// of one row, as the partials do.
+// of one row, as the partials do.  Bound by latency: 144 rows of 16 scenes, 19 MB of
+// partials, 4.9 us; 256 groups of 63 rows, 8.4 MB, 7.7 us.
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
   // groups of a wave loaded at once: of many, many; of few, no more than there are, as
