@@ -160,11 +160,12 @@ def test_speculation_keeps_the_greedy_output(extra):
     assert spec == greedy
 
 
-def test_speculation_keeps_the_greedy_output_at_7b_heads():
-    """63 rows of a kv head against 7: another form of the attention, the same sums."""
-    w = W.scaled(W.get("C3"), layers=2, vocab=2048, prefix_scale=0.3).with_(max_new_tokens=40)
+@pytest.mark.parametrize("name,scale,Ks", [("C3", 0.3, (8, 0, 3)), ("C6", 1.0, (16, 0, 4))])
+def test_speculation_keeps_the_greedy_output_at_full_heads(name, scale, Ks):
+    """63 (68) rows of a kv head against 7 (4): another form of the attention, the same sums."""
+    w = W.scaled(W.get(name), layers=2, vocab=2048, prefix_scale=scale).with_(max_new_tokens=40)
     runs = []
-    for K in (8, 0, 3):
+    for K in Ks:
         s = _session(w, source="device", K=K, with_draft=False)
         out = []
         greedy = runs[0] if runs else None
