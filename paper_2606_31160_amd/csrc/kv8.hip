@@ -741,7 +741,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 
 // Joins the groups of a (sequence, kv head): grid (sequences x kv heads, row
 // blocks, D / 16), NW waves, wave w groups w, w + NW, ..  A lane holds four columns
-// of one row, as the partials do.  Bound by latency: 144 rows of 16 scenes, 19 MB of
+// of one row, as the partials do.  Bound by latency: 144 rows of 16 scenes, 8 MB of
 // partials, 4.9 us; 256 groups of 63 rows, 8.4 MB, 7.7 us.
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
