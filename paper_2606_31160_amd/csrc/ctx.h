@@ -173,6 +173,7 @@ struct Ctx {
   size_t kv8_layer = 0;              // bytes of one layer's keys (or values) in 8 bits
   int kv8_ppw = 1;                   // pages of a group
   int64_t kv8_groups = 0;
+  bool kv8_many = false;             // whether the prompts make many groups (kv8.h)
   size_t kv8_part_bytes = 0, kv8_ml_bytes = 0;
   float* kv8_part = nullptr;
   float2* kv8_ml = nullptr;

@@ -1843,6 +1843,7 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
     p.nkv = nkv;
     p.G = G;
     p.ppw = c.kv8_ppw;
+    p.many = c.kv8_many;
     kv8_set_parts(p, c.kv8_part, c.kv8_ml, c.kv8_groups);
     p.scale_log2 = kLog2e / sqrtf((float)D);
     {
@@ -1850,7 +1851,7 @@ hipError_t launch_attention(Ctx& c, Model& m, int li) {
       CK(launch_kv8_attn(p, D, c.kv8_groups, c.stream, t.e0, t.e1));
     }
     Timed t2(c, SPEC_KERNEL_OTHER, 0);
-    return launch_kv8_combine(p, D, c.kv8_groups, c.stream, t2.e0, t2.e1);
+    return launch_kv8_combine(p, D, c.stream, t2.e0, t2.e1);
   }
   const bool ro = c.ro_out && c.ro_m == &m && c.ro_layer == li;
   const int cross = (c.cross && &m == &c.drf && li == 0) ? 1 : 0;

@@ -48,6 +48,7 @@ struct Kv8AttnArgs {
   int B, R, nq, nkv, G;
   int ppw;                 // pages of a group; 0: as many as leave about `target` groups
   int target;
+  bool many;               // kv8_many(): how the combine sums
   float scale_log2;
 };
 
@@ -59,9 +60,9 @@ size_t kv8_part_bytes(int64_t groups, int rows, int D);
 size_t kv8_ml_bytes(int64_t groups, int rows);     // of ml, odd behind it and seq behind that
 void kv8_set_parts(Kv8AttnArgs& a, void* part, void* ml, int64_t groups);
 int kv8_target_groups(int rows, int ncu);   // (what runs at once)
+bool kv8_many(int64_t groups, int B, int nkv);
 hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0 = nullptr,
                            hipEvent_t e1 = nullptr);
-hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0 = nullptr,
-                              hipEvent_t e1 = nullptr);
+hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, hipStream_t s, hipEvent_t e0 = nullptr, hipEvent_t e1 = nullptr);
 
 }  // namespace specdec

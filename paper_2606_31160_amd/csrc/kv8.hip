@@ -874,6 +874,10 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
 // 40.1 / 40.0.
 int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
 
+// Few (sequence, kv head) pairs have many groups each: 16 waves join them, not 4.  A
+// context asks this of its prompts alone, as the order of its sums depends on it.
+bool kv8_many(int64_t groups, int B, int nkv) { return groups >= (int64_t)32 * B * nkv; }
+
 // Where the lengths decide, count_groups stops at `target`, or at kKv8MaxPages, or
 // (with more heads of sequences than that) takes 4 floor(n / target) pages where n
 // groups of 4 were: at most 2 target and one shorter group for each of them.
@@ -907,17 +911,15 @@ hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStrea
   return hipGetLastError();
 }
 
-hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, int64_t groups, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const int rows = a.R * a.G;
   const dim3 grid(a.B * a.nkv, row_blocks(rows), D / 16);
-  // few (sequence, kv head) pairs have many groups each
-  const bool many = groups >= (int64_t)32 * a.B * a.nkv;
   void (*f)(Kv8AttnArgs, int) = nullptr;
   if (D == 128)
-    f = many ? k_kv8_combine<128, 16> : k_kv8_combine<128, 4>;
+    f = a.many ? k_kv8_combine<128, 16> : k_kv8_combine<128, 4>;
   else
-    f = many ? k_kv8_combine<64, 16> : k_kv8_combine<64, 4>;
-  hipExtLaunchKernelGGL(f, grid, dim3(many ? 1024 : 256), 0, s, e0, e1, 0, a, padded_blocks(rows));
+    f = a.many ? k_kv8_combine<64, 16> : k_kv8_combine<64, 4>;
+  hipExtLaunchKernelGGL(f, grid, dim3(a.many ? 1024 : 256), 0, s, e0, e1, 0, a, padded_blocks(rows));
   return hipGetLastError();
 }
 

@@ -159,9 +159,10 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   a.G = q_heads / c->kv_heads;
   kv8_set_parts(a, workspace, static_cast<char*>(workspace) + p.ml, p.groups);
   a.target = p.target;
+  a.many = kv8_many(p.groups, batch, c->kv_heads);
   a.scale_log2 = scale * 1.4426950408889634f;
   const spec_status s = launched(launch_kv8_attn(a, c->head_dim, p.groups, stream), f);
-  return s != SPEC_OK ? s : launched(launch_kv8_combine(a, c->head_dim, p.groups, stream), f);
+  return s != SPEC_OK ? s : launched(launch_kv8_combine(a, c->head_dim, stream), f);
 }
 
 spec_status spec_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top, size_t* bytes) {

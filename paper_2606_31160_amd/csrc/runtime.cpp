@@ -565,6 +565,9 @@ size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has
     c.kv8_groups = 0;
     for (int b = 0; b < L.B; ++b) c.kv8_groups += (seq_pages(cfg, seqs[b]) + c.kv8_ppw - 1) / c.kv8_ppw;
     c.kv8_groups *= t.kv_heads;
+    int64_t prompts = 0;             // groups of the prompts: the same for every K
+    for (int b = 0; b < L.B; ++b) prompts += t.kv_heads * (int64_t)(seqs[b].prefix_len / (kAttnChunk * c.kv8_ppw) + 1);
+    c.kv8_many = kv8_many(prompts, L.B, t.kv_heads);
     const int rows = L.R * (t.q_heads / t.kv_heads);
     c.kv8_part_bytes = kv8_part_bytes(c.kv8_groups, rows, D);
     c.kv8_ml_bytes = kv8_ml_bytes(c.kv8_groups, rows);

@@ -189,6 +189,19 @@ def test_speculation_keeps_the_greedy_output_at_full_heads(name, scale, Ks):
     assert runs[0] == runs[1] == runs[2]
 
 
+def test_the_first_row_is_the_same_for_every_K():
+    """Capacities of 124 and 125 pages, on both sides of a group's end: bit for bit."""
+    w = W.scaled(W.get("C3"), layers=8, vocab=2048).with_(seqs=(W.c5_layout(7914),), max_new_tokens=20)
+    rows = []
+    for K in (0, 4, 7):
+        s = _session(w, source="device", K=K, with_draft=False)
+        s.verify(np.zeros((1, K), np.int32) if K else None, logits=True)
+        rows.append(s.logits[0, 0].clone())
+        s.sync()
+        s.close()
+    assert rows[0].equal(rows[1]) and rows[0].equal(rows[2])
+
+
 def test_scratch_verify_and_repeated_opening():
     """spec_verify_scratch gives the same logits; so does the context opened again on the same workspace."""
     from paper_2606_31160_amd import binding as B
