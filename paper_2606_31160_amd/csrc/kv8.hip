@@ -740,20 +740,21 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 }
 
 // Joins the groups of a (sequence, kv head): grid (sequences x kv heads, row
-// blocks, D / 16), NW waves, wave w groups w, w + NW, ..  A lane holds four columns
-// of one row, as the partials do.  Bound by latency: 144 rows of 16 scenes, 8 MB of
-// partials, 4.9 us; 256 groups of 63 rows, 8.4 MB, 7.7 us.
+// blocks, D / 16 tiles x T), NW waves.  A lane holds four columns of one row, as the
+// partials do.  T = 1: a wave has a tile's 16 columns, waves take groups w, w + NW, ..
+// T = 4, for many groups: a wave has four columns of four groups at once, groups 4 w ..
+// 4 w + 3, then 4 NW on, so that few (sequence, kv head) pairs reach four times as many
+// CUs.  Bound by latency: 144 rows of 16 scenes, 8 MB of partials, 4.9 us.
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
-  // groups of a wave loaded at once: of many, many; of few, no more than there are, as
-  // what is beyond is loaded all the same (4 for both: 36.5 and 27.9 us a call for 16
-  // scenes of 9 rows and one of 131 thousand tokens, not 34.2 and 26.4)
-  constexpr int NDT = D / 16, U = NW == 16 ? 8 : 2;
+  // groups of a wave loaded at once: no more than there are of few, as what is beyond is
+  // loaded all the same (4: 36.5 us a call for 16 scenes of 9 rows, not 34.2)
+  constexpr int NDT = D / 16, U = NW == 16 ? 4 : 2, T = NW == 16 ? 4 : 1;
   __shared__ f32x4 s_o[NW][64];
   __shared__ float s_m[NW][16], s_l[NW][16];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n16 = lane & 15, g4 = lane >> 4;
-  const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z;
+  const int n16 = lane & 15, g4 = T == 1 ? lane >> 4 : blockIdx.z % 4, sub = T == 1 ? 0 : lane >> 4;
+  const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z / T;
   const int r = 16 * rb + n16;
   const bool in_row = r < a.R * a.G;
   const int j = in_row ? r / a.G : 0, hq = kvh * a.G + (in_row ? r % a.G : 0);
@@ -770,17 +771,18 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   const int first = seq.x + kvh;
   float M = -INFINITY, L = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = wave; i < per; i += NW * U) {
+  for (int i0 = T * wave; i0 < per; i0 += T * NW * U) {
+    const int i = i0 + sub;
     float2 ml[U];
     f32x4 v[U];
     uint64_t odd[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const bool in = i + NW * k < per;
-      const size_t blk = ((size_t)first + (size_t)(in ? i + NW * k : i) * a.nkv) * nrb + rb;
+      const bool in = i + T * NW * k < per;
+      const size_t blk = ((size_t)first + (size_t)(in ? i + T * NW * k : i0) * a.nkv) * nrb + rb;
       ml[k] = a.ml[blk * 16 + n16];
       odd[k] = a.odd[blk];
-      v[k] = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + lane) * 4);
+      v[k] = *reinterpret_cast<const f32x4*>(a.part + ((blk * NDT + dt) * 64 + 16 * g4 + n16) * 4);
       if (!in) {
         ml[k] = make_float2(-INFINITY, 0.f);
         v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -789,7 +791,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
     }
     for (int k = 0; k < U; ++k)
       for (uint64_t w = odd[k]; w; w &= w - 1) {    // values that are not finite, for the rows that see them
-        const int p = (i + NW * k) * ppw + __builtin_ctzll(w);
+        const int p = (i + T * NW * k) * ppw + __builtin_ctzll(w);
         const bool in8 = p < a.packed[b];
         const size_t at = ((size_t)a.table[(size_t)b * a.stride + p] * a.nkv + kvh) * kAttnChunk * D;
         for (int key = 0; key < kAttnChunk; ++key)
@@ -809,13 +811,23 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
       M = mn;
     }
   }
+#pragma unroll
+  for (int d = 16; T == 4 && d < 64; d *= 2) {      // the wave's four groups
+    const float m = __shfl_xor(M, d), l = __shfl_xor(L, d), mn = fmaxf(M, m);
+    const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - mn);
+    const float f1 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + __shfl_xor(o[e], d) * f1;
+    L = L * f0 + l * f1;
+    M = mn;
+  }
   s_o[wave][lane] = o;
-  if (g4 == 0) {
+  if (lane < 16) {
     s_m[wave][n16] = M;
     s_l[wave][n16] = L;
   }
   __syncthreads();
-  if (wave != 0) return;
+  if (wave != 0 || sub != 0) return;
   if (vis < 0) return;                              // no such row: left as it was
   M = -INFINITY;
 #pragma unroll
@@ -913,7 +925,7 @@ hipError_t launch_kv8_attn(const Kv8AttnArgs& a, int D, int64_t groups, hipStrea
 
 hipError_t launch_kv8_combine(const Kv8AttnArgs& a, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
   const int rows = a.R * a.G;
-  const dim3 grid(a.B * a.nkv, row_blocks(rows), D / 16);
+  const dim3 grid(a.B * a.nkv, row_blocks(rows), a.many ? D / 4 : D / 16);
   void (*f)(Kv8AttnArgs, int) = nullptr;
   if (D == 128)
     f = a.many ? k_kv8_combine<128, 16> : k_kv8_combine<128, 4>;

@@ -287,6 +287,23 @@ def test_attention_many_sequences(torch):
     c.check()
 
 
+@pytest.mark.parametrize("nq,nkv,D,R", [(2, 1, 64, 3), (7, 1, 128, 9), (4, 2, 128, 1)])
+def test_attention_many_groups(torch, nq, nkv, D, R):
+    """So many pages of few heads that the combine takes four groups a wave; rows of all lengths."""
+    n = 9000 * nkv + 77
+    vis = _causal([n], R)
+    for c, v in (((R - 1) // 2, 5000), (R - 1, 0 if R > 1 else n), (0, 64 if R > 3 else n)):
+        vis[0, c] = v
+    if R > 5:
+        vis[0, 4] = -1
+    c = Case(torch, 31 + R, nq, nkv, D, [n], [n // PAGE - 3], vis)
+    c.check()
+    if R > 1:                                     # values that are not finite in a late page that not every row sees
+        last = c.table[0, n // PAGE]
+        c.v16[last, 0, 3, 5], c.v16[last, 0, 4, 6] = 0x7F80, 0x7FC0
+        c.check()
+
+
 def test_attention_rows_without_slots_and_without_a_row(torch):
     """Rows that see nothing, rows that are not there, whole sequences of both, rows in any order."""
     lens = [200, 0, 100, 90, 64]

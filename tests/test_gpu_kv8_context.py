@@ -67,7 +67,7 @@ def test_prompt_caches_bit_for_bit(prompts, page_seed):
 
 
 @pytest.mark.parametrize("flags", [0, 1, 8])      # replayed graphs, direct launches, row-major weights
-@pytest.mark.parametrize("prompts", [(320,), (63,), (100, 320, 65)])
+@pytest.mark.parametrize("prompts", [(320,), (63,), (100, 320, 65), (8500,)])
 def test_verify_against_the_oracle(flags, prompts):
     w = _tiny(prompts)
     T, D = S.oracle_decoders(w, W.HostWeights(w))
