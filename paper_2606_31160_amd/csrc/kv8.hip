@@ -744,7 +744,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 // partials do.  T = 1: a wave has a tile's 16 columns, waves take groups w, w + NW, ..
 // T = 4, for many groups: a wave has four columns of four groups at once, groups 4 w ..
 // 4 w + 3, then 4 NW on, so that few (sequence, kv head) pairs reach four times as many
-// CUs.  Bound by latency: 144 rows of 16 scenes, 8 MB of partials, 4.9 us.
+// CUs.  Bound by latency: 144 rows of 16 scenes, 8 MB of partials, 4.9 us; 63 rows of one
+// scene of 131 thousand tokens, 256 groups, 8.4 MB, 5.4 us (7.7 with T = 1).
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb) {
   // groups of a wave loaded at once: no more than there are of few, as what is beyond is
@@ -881,7 +882,7 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
 
 // One workgroup per CU: fewer pages each, in two workgroups of 4 waves per CU or in
 // further rounds, cost their prologues (about 5 us before the first product).  Per
-// call, groups aimed at 256 / 512 / 1024: 16 scenes of 2 to 8 thousand tokens, one row
+// call with an earlier combine, groups aimed at 256 / 512 / 1024: 16 scenes of 2 to 8 thousand tokens, one row
 // each, 21.8 / 23.7 / 25.4 us, 9 rows 35.3 / 43.8 / 51.0; one of 131 thousand tokens 27.7 /
 // 40.1 / 40.0.
 int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
