@@ -11,7 +11,6 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "device.h"
 #include "kv8.h"
@@ -880,11 +879,11 @@ hipError_t launch_kv8_pack(const Kv8PackArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-// One workgroup per CU: fewer pages each, in two workgroups of 4 waves per CU or in
-// further rounds, cost their prologues (about 5 us before the first product).  Per
-// call with an earlier combine, groups aimed at 256 / 512 / 1024: 16 scenes of 2 to 8 thousand tokens, one row
-// each, 21.8 / 23.7 / 25.4 us, 9 rows 35.3 / 43.8 / 51.0; one of 131 thousand tokens 27.7 /
-// 40.1 / 40.0.
+// One workgroup per CU: fewer pages each, in two workgroups of 4 waves per CU or one
+// after another, cost their prologues (about 5 us before the first product).  Per call
+// (with an earlier combine), groups aimed at 256 / 512 / 1024: 16 scenes of 2 to 8
+// thousand tokens, one row each, 21.8 / 23.7 / 25.4 us, 9 rows 35.3 / 43.8 / 51.0; one of
+// 131 thousand tokens 27.7 / 40.1 / 40.0.
 int kv8_target_groups(int rows, int ncu) { return std::max(1, ncu / shape_of(rows).y); }
 
 // Few (sequence, kv head) pairs have many groups each: 16 waves join them, not 4.  A
