@@ -459,8 +459,8 @@ spec_status spec_kv8_attn_workspace_bytes(const spec_kv8* cache, int32_t batch, 
  *   d_logprob      [rows][n_tokens] float: ln p of the tokens d_tokens
  *                  [rows][n_tokens] (int32); NaN for an id outside [0, vocab)
  *   d_entropy      [rows] float: -sum p ln p, or NULL
- *   d_top_token    [rows][top] int32: the `top` (0..SPEC_MAX_TOP) most probable
- *                  tokens, most probable first, the lowest index on ties, NaN as
+ *   d_top_token    [rows][top] int32: the `top` (0..SPEC_MAX_TOP, at most vocab) most
+ *                  probable tokens, most probable first, the lowest index on ties, NaN as
  *                  -infinity (spec_verify's rule); d_top_logprob [rows][top]: their ln p
  * Logits of -infinity have p = 0 and ln p = -infinity.  A row with a NaN or
  * +infinity, or with nothing above -infinity, has no distribution: its log
