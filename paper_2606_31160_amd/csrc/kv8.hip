@@ -20,6 +20,7 @@ namespace specdec {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -460,9 +461,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   // A page whose unit is far from u: O is turned by 2^far while it is added, and
   // what 2^60 leaves (seen in no sound cache) is taken by the probabilities.
   auto far_of = [](float off) { return fabsf(off) > 16.f ? fminf(fmaxf(-off, -60.f), 60.f) : 0.f; };
-  // Pages that not every row sees, with values that are not finite: these are taken
-  // as zero here, as zero probability times one is not zero, and the combine gives
-  // them to the rows that see their slots.
+  // Pages with values that are not finite: these are taken as zero here, as zero
+  // probability times one is not zero, and the combine gives them to the rows that see
+  // their slots.  (8-bit pages that every row sees keep theirs, which are all NaN.)
   uint64_t odd_pages = 0;
   float u = 1.f, lv = 0.f;                          // unit of O; lane l: log2 of the l-th page's value scale / u
 
@@ -660,20 +661,27 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     });
     if (!full) {
       const int valid = min(vmax - k0, kAttnChunk) - 16 * g4;
-      uint32_t odd = 0;
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t m = (uint32_t)((1ull << (16 * min(max(valid - 8 * e - 2 * k, 0), 2))) - 1);
 #pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) {
-            const uint32_t v = w[2 * dt + e][k] & m, x = not_finite16(v);
-            odd |= x;
-            w[2 * dt + e][k] = v & ~((x >> 15) * 0xffffu);
-          }
+          for (int dt = 0; dt < NDT; ++dt) w[2 * dt + e][k] &= m;
         }
-      if (__any(odd != 0)) odd_pages |= 1ull << p;
+    }
+    // an infinity times both parts of a probability would be NaN: left to the combine even if all rows see it
+    u16x2 most = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2 * NDT; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[i][k] & 0x7fff7fffu));
+    if (__any(most.x >= 0x7f80 || most.y >= 0x7f80)) {
+      odd_pages |= 1ull << p;
+#pragma unroll
+      for (int i = 0; i < 2 * NDT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[i][k] &= ~((not_finite16(w[i][k]) >> 15) * 0xffffu);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e)

@@ -1,0 +1,62 @@
+"""Attention over 8-bit cache pages at the edges of its types: values that are not finite, scales and lengths far out."""
+import numpy as np
+import pytest
+
+from tests import _operators as ref
+from tests.test_gpu_kv8 import PAGE, Case, _causal, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _compare(c, out, lse, floor=0.0):
+    """Every row against the definition in 64 bits; NaN and infinities exactly.
+
+    A score is a sum of D products in 32 bits and a few roundings: off by (D + 8) 2^-24 of the sum of its magnitudes, and
+    a probability by twice that of itself.  It is held as two bf16 numbers: the first is off by half a step, 2^-8 of
+    itself, the second by 2^-8 of that, so 2^-16 on the whole.  2^-14 of the sum of magnitudes is for what is summed in
+    32 bits and for its exponent (two roundings of numbers up to 2^9, 2^-14 at most), 2^-8 of the result half a step of bf16."""
+    D, G = c.D, c.nq // c.nkv
+    for b in range(c.B):
+        for h in range(c.nkv):
+            k, v = c.keys_values(b, h)
+            for j in range(c.R):
+                r, n = b * c.R + j, min(int(c.vis[b, j]), c.stride * PAGE)
+                for hq in range(h * G, h * G + G):
+                    o, z = out[r, hq * D:(hq + 1) * D], lse[r, hq]
+                    if n < 0:
+                        assert (o == 77).all() and z == 55
+                        continue
+                    with np.errstate(invalid="ignore"):
+                        want, wz, A, S, _, _ = ref.attention(ref.bf16_value(c.q[r, hq * D:(hq + 1) * D]), k, v, n, c.scale)
+                        ds = (D + 8) * 2.0 ** -24 * S
+                        tol = 2.0 ** -8 * np.abs(want) + A * (2.0 ** -16 + 2 * ds + 2.0 ** -14) + floor
+                        ok = (np.isnan(o) & np.isnan(want)) | (o == want) | (np.isfinite(want) & (np.abs(o - want) <= tol))
+                    assert ok.all(), (b, j, hq, np.flatnonzero(~ok)[:4], o[~ok][:4], want[~ok][:4])
+                    assert z == wz or abs(z - wz) <= ds + 2.0 ** -20 + 2.0 ** -22 * abs(wz), (b, j, hq, z, wz)
+
+
+def _check(c, err=0, floor=0.0):
+    out, lse = c.run()
+    assert int(c.err) == err
+    _compare(c, out, lse, floor)
+    return out, lse
+
+
+# -- values that are not finite ----------------------------------------------------
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("R", [1, 3, 13])
+def test_infinities_in_pages_that_every_row_sees(torch, D, R):  # noqa: F811
+    """An infinite value in a bf16 page is infinite in every row, and NaN only against the other infinity."""
+    c = Case(torch, 40 + R, 6, 2, D, [200], [0], np.full((1, R), 200, np.int32))
+    for p, at, dim, bits in ((0, 3, 5, 0x7F80), (1, 60, 6, 0xFF80), (1, 7, 8, 0x7F80), (2, 9, 8, 0xFF80), (0, 1, 9, 0x7FC0),
+                             (3, 2, 10, 0xFF80), (0, 2, 11, 0x7F80), (3, 1, 11, 0x7F80)):
+        c.v16[c.table[0, p], 1, dim, at] = bits
+    out, _ = _check(c)
+    assert np.isposinf(out[:, 3 * D + 5]).all() and np.isneginf(out[:, 3 * D + 6]).all()
+    # ... whatever the other rows of the pass see
+    first = out[0]
+    if R > 1:
+        c.vis[0, 1:] = np.arange(1, R) * 13 % 150
+        out, _ = _check(c)
+        np.testing.assert_array_equal(out[0], first)
