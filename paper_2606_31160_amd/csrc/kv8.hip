@@ -759,7 +759,9 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   // loaded all the same (4: 36.5 us a call for 16 scenes of 9 rows, not 34.2)
   constexpr int NDT = D / 16, U = NW == 16 ? 4 : 2, T = NW == 16 ? 4 : 1;
   __shared__ f32x4 s_o[NW][64];
+  __shared__ f32x4 s_x[NW][64];
   __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ int s_has[NW];                         // waves that have an s_x
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n16 = lane & 15, g4 = T == 1 ? lane >> 4 : blockIdx.z % 4, sub = T == 1 ? 0 : lane >> 4;
   const int b = blockIdx.x / a.nkv, kvh = blockIdx.x % a.nkv, rb = blockIdx.y, dt = blockIdx.z / T;
@@ -779,6 +781,9 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   const int first = seq.x + kvh;
   float M = -INFINITY, L = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  // values that are not finite: apart from o, whose factors can round to zero
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+  bool has = false;
   for (int i0 = T * wave; i0 < per; i0 += T * NW * U) {
     const int i = i0 + sub;
     float2 ml[U];
@@ -798,15 +803,16 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
       }
     }
     for (int k = 0; k < U; ++k)
-      for (uint64_t w = odd[k]; w; w &= w - 1) {    // values that are not finite, for the rows that see them
+      for (uint64_t w = odd[k]; w; w &= w - 1) {    // for the rows that see them
+        has = true;
         const int p = (i + T * NW * k) * ppw + __builtin_ctzll(w);
         const bool in8 = p < a.packed[b];
         const size_t at = ((size_t)a.table[(size_t)b * a.stride + p] * a.nkv + kvh) * kAttnChunk * D;
         for (int key = 0; key < kAttnChunk; ++key)
           for (int e = 0; e < 4; ++e) {
             const size_t c = at + (size_t)(16 * dt + 4 * g4 + e) * kAttnChunk + key;
-            const float x = in8 ? ((a.v8[c] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[c]);
-            if (!(fabsf(x) < INFINITY) && p * kAttnChunk + key < vis) o[e] += x;
+            const float v = in8 ? ((a.v8[c] & 0x7f) == 0x7f ? NAN : 0.f) : bf2f(a.v16[c]);
+            if (!(fabsf(v) < INFINITY) && p * kAttnChunk + key < vis) x[e] += v;
           }
       }
 #pragma unroll
@@ -829,6 +835,15 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
     L = L * f0 + l * f1;
     M = mn;
   }
+  has = __any(has);
+  if (has) {
+#pragma unroll
+    for (int d = 16; T == 4 && d < 64; d *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], d);
+    s_x[wave][lane] = x;
+  }
+  if (lane == 0) s_has[wave] = has;
   s_o[wave][lane] = o;
   if (lane < 16) {
     s_m[wave][n16] = M;
@@ -840,10 +855,11 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   M = -INFINITY;
 #pragma unroll
   for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][n16]);
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  o = x = f32x4{0.f, 0.f, 0.f, 0.f};
   L = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
+    if (s_has[w]) x += s_x[w][lane];
     const float m = s_m[w][n16], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
     o += s_o[w][lane] * f;
     L += s_l[w][n16] * f;
@@ -851,7 +867,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   if (vis == 0) {
     o = f32x4{0.f, 0.f, 0.f, 0.f};
   } else {
-    o *= 1.f / L;
+    o = o * (1.f / L) + x;
   }
   const int row = b * a.R + j, d = hq * D + 16 * dt + 4 * g4;
   bf16_t* out = a.out + (a.opk ? (int64_t)xop_at(row, d, a.opk) : (int64_t)row * a.out_stride + d);

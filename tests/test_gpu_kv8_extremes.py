@@ -60,3 +60,19 @@ def test_infinities_in_pages_that_every_row_sees(torch, D, R):  # noqa: F811
         c.vis[0, 1:] = np.arange(1, R) * 13 % 150
         out, _ = _check(c)
         np.testing.assert_array_equal(out[0], first)
+
+
+@pytest.mark.parametrize("n", [9 * PAGE, 9077])   # a few groups; as many as the combine takes four a wave
+def test_infinities_whose_weight_vanishes(torch, n):  # noqa: F811
+    """Infinite values with weights of e^-128 beside later keys, too small for the factor that joins their groups in 32
+    bits: infinite all the same."""
+    c = Case(torch, 44, 2, 1, 64, [n], [0], np.array([[n, 90]], np.int32))
+    c.q[:] = ref.bf16(np.float32(4))
+    late = np.zeros(c.n16, bool)
+    late[c.table[0, 4:-(-n // PAGE)]] = True
+    c.k16[:] = ref.bf16(np.where(late, 4.0, 0.0))[:, None, None, None]
+    c.v16[:] = ref.bf16(np.random.default_rng(1).standard_normal(c.v16.shape))
+    c.v16[c.table[0, 1], 0, 3, 30], c.v16[c.table[0, 1], 0, 4, 31] = 0x7F80, 0xFF80
+    c.v16[c.table[0, 1], 0, 5, 2] = 0x7F80       # slot 66: row 1 sees it as well
+    out, _ = _check(c)
+    assert np.isposinf(out[0, 3]) and np.isneginf(out[0, 4]) and np.isfinite(out[1, 3:5]).all() and np.isposinf(out[:, 5]).all()
