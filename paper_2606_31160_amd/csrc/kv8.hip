@@ -7,7 +7,7 @@
 //   s = the smallest power of two with max |x| <= 448 s (at least 2^-126; 1 for a page of zeros)
 //   code = e4m3(x / s), to nearest even
 // A power of two costs a floating format nothing but range, and what a code stands
-// for, s e4m3, is a bf16 number: reading a page in bf16 or fp16 rounds nothing.
+// for, s e4m3, is a bf16 number: reading a page in bf16 rounds nothing.
 #include <hip/hip_ext.h>
 
 #include <algorithm>
@@ -19,10 +19,7 @@ namespace specdec {
 
 namespace {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // e with 2^e the smallest power of two such that big <= 448 2^e (0 for big = 0); big = f
 // 2^x with f in [1/2, 1), and 448 = 7/8 2^9.
@@ -241,27 +238,26 @@ __device__ __forceinline__ int row_vis(const Kv8AttnArgs& a, const Groups& g, co
   return j < count ? base + (j < causal ? j + 1 : count) : -1;
 }
 
-__device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi) {
+// scale: a power of two
+__device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi, float scale) {
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  const b2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)};
+  const b2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)};
   return __builtin_bit_cast(u32x4, r);
 }
-__device__ __forceinline__ u32x4 f16_of_e4m3(uint32_t lo, uint32_t hi) {
-  const f16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false),
-                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
-                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false),
-                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
-  return __builtin_bit_cast(u32x4, r);
+// A scale as 2^e times a rest: e is its exponent as far as every code times 2^e is a normal bf16 number.
+__device__ __forceinline__ int exponent_of(float scale) {
+  int x;
+  frexpf(scale, &x);
+  return min(max(x - 1, -116), 118);
 }
 
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), f16x2));
-}
-__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+// x0, x1 as two bf16 numbers each: h the nearest, l what is left of them (2^-16 of x at most is lost).
+__device__ __forceinline__ void split2(float x0, float x1, uint32_t& h, uint32_t& l) {
+  h = pack2(x0, x1);
+  l = pack2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xffff0000u));
 }
 // Bit 7 of every byte that is a NaN code / bits 15 and 31 for bf16 numbers that are
 // not finite.
@@ -281,13 +277,11 @@ struct RowState {
   f32x4 o[NRB][NDT];
 };
 
-constexpr float kHead = 7.f;    // probabilities are held 2^7 times as large
-
 // Scores s of 16 keys per lane -> probabilities 2^(s sc - m + off), handed to put, and
 // l.  The maximum m follows only when a row's scores pass it by 2^8: until then O is not
-// rescaled and lanes are not compared, and a probability is at most 2^(8 + off), which
-// fits fp16 (off <= 7 there).  A row's sums depend on no other row.  (A maximum that
-// passes NaN on, as the row's sums do anyway, takes one instruction for three.)
+// rescaled and lanes are not compared, and a probability is at most 2^(8 + off).  A row's
+// sums depend on no other row.  (A maximum that passes NaN on, as the row's sums do
+// anyway, takes one instruction for three.)
 template <int NRB, int NDT, class Put>
 __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NRB][16], const float (&sc)[NRB], float off,
                                      Put put) {
@@ -344,12 +338,11 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
 //   Keys are read as bf16, like Q: an e4m3 code is exact in it.  (16x16x128 MFMA
 // of e4m3 numbers, against Q in two parts of four bits each, took as long, and their
 // sums drop what is some 2^-16 of the largest product: scores 1e-5 off, not 1e-7.)
-//   Values and probabilities are read as fp16: an e4m3 code is exact in it, and a
-// probability keeps 11 bits, as a rounding to bf16 would show in the bf16 result.
-// The value scale is part of the probability's exponent: with u the largest one of
-// the group, p vs / u 2^7 is in fp16's normal range down to 2^-21 (a page whose scale
-// is further below u has O turned to its own unit for as long).  bf16 pages take
-// their values as they are and each probability as the sum of two bf16 numbers.
+//   Values are read as bf16 as well, times their scale's power of two (a part of the
+// widening; what is left of a scale is part of the probability's exponent), and each
+// probability as the sum of two bf16 numbers, 16 bits of it in 32 bits' range: O is in
+// its true unit, whatever the scales of other pages.  (One fp16 number, in a unit common to
+// a group's pages, keeps 11 bits, and fewer on pages whose scale is below the largest.)
 //   Bound by a wave's own chain, scores to softmax to value product, with two waves a
 // SIMD (of 16 scenes of 2 to 8 thousand tokens, 80 MB: 9 rows each 29.6 us, vector
 // unit 35% busy, matrix unit 14%; one row each 18.1 us, 4.4 TB/s), and where a wave has
@@ -452,20 +445,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       for (int i = 0; i < 16; ++i)
         if (k0 + 16 * g4 + i >= min(vis[rb], end)) s[rb][i] = -INFINITY;
   };
-  auto turn_o = [&](float f) {
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= f;
-  };
-  // A page whose unit is far from u: O is turned by 2^far while it is added, and
-  // what 2^60 leaves (seen in no sound cache) is taken by the probabilities.
-  auto far_of = [](float off) { return fabsf(off) > 16.f ? fminf(fmaxf(-off, -60.f), 60.f) : 0.f; };
   // Pages with values that are not finite: these are taken as zero here, as zero
   // probability times one is not zero, and the combine gives them to the rows that see
   // their slots.  (8-bit pages that every row sees keep theirs, which are all NaN.)
   uint64_t odd_pages = 0;
-  float u = 1.f, lv = 0.f;                          // unit of O; lane l: log2 of the l-th page's value scale / u
 
   if (n8 > 0) {                                     // workgroup-uniform
     const bool own = lane < n8 && page >= 0;
@@ -504,9 +487,8 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
     if (own && !fine && a.err) *a.err = SPEC_E_INVAL;
     const uint64_t good = __ballot(own && fine);
-    const int um = wave_max(own && fine ? (int)__float_as_uint(vsc) : 0);   // (positive floats order as integers)
-    if (um != 0) u = __uint_as_float((uint32_t)um);
-    lv = (lane < n8 ? __builtin_amdgcn_logf(vsc) : 0.f) - __builtin_amdgcn_logf(u);
+    const int ev = own && fine ? exponent_of(vsc) : 0;   // lane l: the l-th page's value scale, 2^ev 2^lv
+    const float lv = own && fine ? __builtin_amdgcn_logf(vsc * power_of_two(-ev)) : 0.f, vp = power_of_two(ev);
 
     while (p < 64) {
       t8 &= t8 - 1;
@@ -534,7 +516,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
           for (int k = t; k < t + 2; ++k) {
             const u32x4 w = kr[k][h >> 1];
-            const u32x4 x = h & 1 ? bf16_of_e4m3(w.z, w.w) : bf16_of_e4m3(w.x, w.y);
+            const u32x4 x = h & 1 ? bf16_of_e4m3(w.z, w.w, 1.f) : bf16_of_e4m3(w.x, w.y, 1.f);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) acc[k][rb] = mfma16x16x32(x, qf[rb][h], h ? acc[k][rb] : f32x4{0.f, 0.f, 0.f, 0.f});
           }
@@ -547,21 +529,19 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       __builtin_amdgcn_sched_barrier(0);
       load_k(nat);
       if (!full) mask(s, k0, sound ? INT32_MAX : 0);
-      const float off = sound ? lane_f(lv, p) : 0.f, far = far_of(off);
-      if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
-      const float rest = far != 0.f ? __builtin_amdgcn_exp2f(off + far) : 1.f;
       float sc[NRB];
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) sc[rb] = fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f);
-      u32x4 pb[NRB][2];
-      soft(st, s, sc, far != 0.f ? kHead : off + kHead, [&](int rb, float (&x)[16]) {
-        if (rest != 1.f)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] *= rest;
+      u32x4 pb[NRB][2][2];                        // the parts of the probabilities of keys 8 e ..
+      soft(st, s, sc, lane_f(lv, p), [&](int rb, float (&x)[16]) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) pb[rb][e][k] = pack_f16(x[8 * e + 2 * k], x[8 * e + 2 * k + 1]);
+          for (int k = 0; k < 4; ++k) {
+            uint32_t h, l;
+            split2(x[8 * e + 2 * k], x[8 * e + 2 * k + 1], h, l);
+            pb[rb][e][0][k] = h, pb[rb][e][1][k] = l;
+          }
       });
       if (!full) {
         const int valid = (sound ? min(vmax - k0, kAttnChunk) : 0) - 16 * g4;   // of this lane's 16 keys
@@ -581,19 +561,24 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
           }
         if (__any(odd != 0)) odd_pages |= 1ull << p;
       }
+      const float vpp = lane_f(vp, p);
 #pragma unroll
       for (int dt = 0; dt < NDT; dt += 2)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+          u32x4 v[2];
 #pragma unroll
-          for (int k = dt; k < dt + 2; ++k) {
-            const u32x4 v = e ? f16_of_e4m3(vr[k].z, vr[k].w) : f16_of_e4m3(vr[k].x, vr[k].y);
+          for (int k = 0; k < 2; ++k)
+            v[k] = e ? bf16_of_e4m3(vr[dt + k].z, vr[dt + k].w, vpp) : bf16_of_e4m3(vr[dt + k].x, vr[dt + k].y, vpp);
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) st.o[rb][k] = mfma_f16(v, pb[rb][e], st.o[rb][k]);
-          }
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int rb = 0; rb < NRB; ++rb) st.o[rb][dt + k] = mfma16x16x32(v[k], pb[rb][e][h], st.o[rb][dt + k]);
+        }
       __builtin_amdgcn_sched_barrier(0);
       load_v(nat);
-      if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
       p = next;
     }
   }
@@ -638,25 +623,18 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
       for (int e = 0; e < 2; ++e) w[2 * dt + e] = ld16(vp + 16 * dt * kAttnChunk + 8 * e);
     if (!full) mask(s, k0, INT32_MAX);
-    const float off = lane_f(lv, p), far = far_of(off);
-    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(far));
-    const float rest = far != 0.f ? __builtin_amdgcn_exp2f(off + far) : 1.f;
     float sc[NRB];
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) sc[rb] = a.scale_log2;
     u32x4 ph[NRB][2], pl[NRB][2];
-    soft(st, s, sc, far != 0.f ? kHead : off + kHead, [&](int rb, float (&x)[16]) {
-      if (rest != 1.f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= rest;
+    soft(st, s, sc, 0.f, [&](int rb, float (&x)[16]) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float x0 = x[8 * e + 2 * k], x1 = x[8 * e + 2 * k + 1];
-          const uint32_t h = pack2(x0, x1);
-          ph[rb][e][k] = h;
-          pl[rb][e][k] = pack2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xffff0000u));
+          uint32_t h, l;
+          split2(x[8 * e + 2 * k], x[8 * e + 2 * k + 1], h, l);
+          ph[rb][e][k] = h, pl[rb][e][k] = l;
         }
     });
     if (!full) {
@@ -692,11 +670,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
           st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], ph[rb][e], st.o[rb][dt]);
           st.o[rb][dt] = mfma16x16x32(w[2 * dt + e], pl[rb][e], st.o[rb][dt]);
         }
-    if (far != 0.f) turn_o(__builtin_amdgcn_exp2f(-far));
   }
 
   // Join the four key waves' sums: key wave w the head dimensions of tiles ND4 w ..
-  u *= __builtin_amdgcn_exp2f(-kHead);
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
     st.l[rb] += __shfl_xor(st.l[rb], 16);
@@ -722,7 +698,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       const float f = mx[w] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx[w] - M);
       L = __builtin_fmaf(f, s_l[w][wr][16 * rb + n16], L);
     }
-    const float f = (st.m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[rb] - M)) * u;
+    const float f = st.m[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[rb] - M);
     if (rb) lds_barrier();                          // the last block's tiles have been read
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) s_o[wr][wk][dt][lane] = st.o[rb][dt] * f;

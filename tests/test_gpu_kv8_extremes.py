@@ -76,3 +76,45 @@ def test_infinities_whose_weight_vanishes(torch, n):  # noqa: F811
     c.v16[c.table[0, 1], 0, 5, 2] = 0x7F80       # slot 66: row 1 sees it as well
     out, _ = _check(c)
     assert np.isposinf(out[0, 3]) and np.isneginf(out[0, 4]) and np.isfinite(out[1, 3:5]).all() and np.isposinf(out[:, 5]).all()
+
+
+# -- scales ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("far", [3, 15, 60, 110])
+def test_small_scales_beside_large_ones(torch, far):  # noqa: F811
+    """Pages of small values keep their digits whatever the scales of other pages of their group, seen or not: a row that
+    sees a page of small values alone, most of it weighing 2^-10 to 2^-20 of one key whose value is zero, beside rows
+    that see pages of large values as well."""
+    c = Case(torch, 47, 6, 2, 64, [9 * PAGE], [9], np.array([[PAGE, 9 * PAGE, 2 * PAGE, 40]], np.int32))
+    c.q[:] = 0
+    c.q[:, ::64] = ref.bf16(np.float32(8))       # a score is its key's first element
+    p = c.table[0, 0]
+    c.ks[:], c.vs[:] = 1.0, 1.0
+    c.k8[p, :, :, 0] = np.random.default_rng(2).integers(0x40, 0x52, (2, PAGE))   # 2 to 9
+    c.k8[p, :, 11, 0] = 0x58                     # 16
+    c.v8[p, :, :, 11] = 0
+    c.vs[p] = 2.0 ** -far
+    c.vs[c.table[0, 1]] = 2.0 ** far
+    first, _ = _check(c)
+    c.vis[0, 1:] = PAGE                          # the same row beside rows that see no more
+    alone, _ = _check(c)
+    np.testing.assert_array_equal(first[0], alone[0])
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -126, 1e-40, 2.0 ** -149, 1.3 * 2.0 ** 60, 2.0 ** 118])
+def test_value_scales_far_out(torch, scale):  # noqa: F811
+    """8-bit pages all of one scale, alone and with bf16 pages behind them."""
+    for n, packed in ((5 * PAGE, 5), (5 * PAGE + 40, 4)):
+        c = Case(torch, 48, 4, 2, 64, [n], [packed], _causal([n], 3))
+        c.vs[:] = scale
+        # results are bf16 numbers of steps of 2^-133 there, and 32-bit sums of steps of 2^-149 (held 2^8 times as coarse)
+        _check(c, floor=2.0 ** -133)
+
+
+def test_value_scales_of_every_magnitude(torch):  # noqa: F811
+    rng = np.random.default_rng(3)
+    for seed in range(3):
+        n = 12 * PAGE + 7
+        c = Case(torch, 49 + seed, 4, 2, 128, [n], [10], np.array([[n, 64, 200, 500, 11 * PAGE]], np.int32))
+        c.vs[:] = np.exp2(rng.integers(-126, 110, c.vs.shape)).astype(np.float32) * rng.uniform(1, 2, c.vs.shape).astype(np.float32)
+        _check(c, floor=2.0 ** -133)
