@@ -278,10 +278,12 @@ struct RowState {
 };
 
 // Scores s of 16 keys per lane -> probabilities 2^(s sc - m + off), handed to put, and
-// l.  The maximum m follows only when a row's scores pass it by 2^8: until then O is not
-// rescaled and lanes are not compared, and a probability is at most 2^(8 + off).  A row's
-// sums depend on no other row.  (A maximum that passes NaN on, as the row's sums do
-// anyway, takes one instruction for three.)
+// l.  m is kAbove over the row's maximum when it is set, and set again only when a row's
+// scores pass it: until then O is not rescaled and lanes are not compared, and a
+// probability is at most 2^off, so that O keeps within the values' range.  A row's sums depend
+// on no other row.  (A maximum that passes NaN on, as the row's sums do anyway, takes one
+// instruction for three.)
+constexpr float kAbove = 8.f, kAboveFactor = 256.f;   // 2^kAbove
 template <int NRB, int NDT, class Put>
 __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NRB][16], const float (&sc)[NRB], float off,
                                      Put put) {
@@ -293,16 +295,16 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
 #pragma unroll
     for (int i = 1; i < 16; ++i) x = __builtin_elementwise_maximum(x, s[rb][i]);
     pm[rb] = x * sc[rb];
-    grow |= pm[rb] > st.m[rb] + 8.f;
+    grow |= pm[rb] > st.m[rb];
   }
   if (__any(grow)) {
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 16));
       pm[rb] = fmaxf(pm[rb], __shfl_xor(pm[rb], 32));
-      if (pm[rb] > st.m[rb] + 8.f) {
-        const float alpha = st.m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[rb] - pm[rb]);
-        st.m[rb] = pm[rb];
+      if (pm[rb] > st.m[rb]) {
+        const float m = pm[rb] + kAbove, alpha = st.m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m[rb] - m);
+        st.m[rb] = m;
         st.l[rb] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) st.o[rb][dt] *= alpha;
@@ -677,6 +679,9 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   for (int rb = 0; rb < NRB; ++rb) {
     st.l[rb] += __shfl_xor(st.l[rb], 16);
     st.l[rb] += __shfl_xor(st.l[rb], 32);
+    // (of a sum near 1 the logarithm is exact to more digits; O stays as it is)
+    st.m[rb] -= kAbove;
+    st.l[rb] *= kAboveFactor;
     if (g4 == 0) {
       s_m[wk][wr][16 * rb + n16] = st.m[rb];
       s_l[wk][wr][16 * rb + n16] = st.l[rb];
@@ -843,7 +848,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   if (vis == 0) {
     o = f32x4{0.f, 0.f, 0.f, 0.f};
   } else {
-    o = o * (1.f / L) + x;
+    o = o * (kAboveFactor / L) + x;
   }
   const int row = b * a.R + j, d = hq * D + 16 * dt + 4 * g4;
   bf16_t* out = a.out + (a.opk ? (int64_t)xop_at(row, d, a.opk) : (int64_t)row * a.out_stride + d);

@@ -6,6 +6,7 @@ from tests import _operators as ref
 from tests.test_gpu_kv8 import PAGE, Case, _causal, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+MAX = 0x7F7F                                      # the largest bf16 number
 
 
 def _compare(c, out, lse, floor=0.0):
@@ -76,6 +77,28 @@ def test_infinities_whose_weight_vanishes(torch, n):  # noqa: F811
     c.v16[c.table[0, 1], 0, 5, 2] = 0x7F80       # slot 66: row 1 sees it as well
     out, _ = _check(c)
     assert np.isposinf(out[0, 3]) and np.isneginf(out[0, 4]) and np.isfinite(out[1, 3:5]).all() and np.isposinf(out[:, 5]).all()
+
+
+def test_the_largest_values(torch):  # noqa: F811
+    """One slot of the largest numbers, and a few of them."""
+    for n in (1, 2, 5):
+        for packed in (0, 1):
+            c = Case(torch, 45, 4, 2, 64, [n], [packed], np.array([[n]], np.int32))
+            c.v16[:] = MAX
+            c.v8[:], c.vs[:] = 0x6F, 2.0 ** 120   # 120 2^120
+            _check(c)
+
+
+def test_the_largest_values_behind_a_growing_maximum(torch):  # noqa: F811
+    """A page whose scores are 2^5 times the weight of those that its wave saw before, with a value near the largest."""
+    n = 72000
+    c = Case(torch, 46, 1, 1, 64, [n], [0], np.array([[n]], np.int32), extra=0)
+    c.k16[:], c.v16[:] = 0, 0
+    c.q[:] = 0
+    c.q[0, 0] = ref.bf16(np.float32(8))          # a score is its key's first element
+    c.k16[c.table[0, 4], 0, 7, 0] = ref.bf16(np.float32(3.5))
+    c.v16[c.table[0, 4], 0, 9, 7] = MAX
+    _check(c)
 
 
 # -- scales ------------------------------------------------------------------------
