@@ -11,6 +11,7 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <cfloat>
 
 #include "device.h"
 #include "kv8.h"
@@ -247,11 +248,11 @@ __device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t lo, uint32_t hi, float sc
                    __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)};
   return __builtin_bit_cast(u32x4, r);
 }
-// A scale as 2^e times a rest: e is its exponent as far as every code times 2^e is a normal bf16 number.
-__device__ __forceinline__ int exponent_of(float scale) {
+// A scale as 2^e times a rest: e is its exponent as far as the bounds reach.
+__device__ __forceinline__ int exponent_of(float scale, int least, int most) {
   int x;
   frexpf(scale, &x);
-  return min(max(x - 1, -116), 118);
+  return min(max(x - 1, least), most);
 }
 
 // x0, x1 as two bf16 numbers each: h the nearest, l what is left of them (2^-16 of x at most is lost).
@@ -283,6 +284,7 @@ struct RowState {
 // probability is at most 2^off, so that O keeps within the values' range.  A row's sums depend
 // on no other row.  (A maximum that passes NaN on, as the row's sums do anyway, takes one
 // instruction for three.)
+constexpr float kLeast = 1.4e-45f;   // factors of scores are positive and finite: -infinity times one is -infinity, zero is zero
 constexpr float kAbove = 8.f, kAboveFactor = 256.f;   // 2^kAbove
 template <int NRB, int NDT, class Put>
 __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NRB][16], const float (&sc)[NRB], float off,
@@ -337,12 +339,12 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
 //   The next page's keys are loaded while this one's softmax runs, its values while
 // the next scores are formed.  (Pages by way of LDS, for the two waves of WR = 2 at
 // once, took longer: 33 us where this takes 29.5, the waves in step at its barriers.)
-//   Keys are read as bf16, like Q: an e4m3 code is exact in it.  (16x16x128 MFMA
+//   Keys are read as bf16, like Q: an e4m3 code is exact in it, also times its scale's
+// power of two (what is left of a scale is part of the scores' factor).  (16x16x128 MFMA
 // of e4m3 numbers, against Q in two parts of four bits each, took as long, and their
 // sums drop what is some 2^-16 of the largest product: scores 1e-5 off, not 1e-7.)
-//   Values are read as bf16 as well, times their scale's power of two (a part of the
-// widening; what is left of a scale is part of the probability's exponent), and each
-// probability as the sum of two bf16 numbers, 16 bits of it in 32 bits' range: O is in
+//   Values are read as bf16 in the same way (with the rest of a scale in the
+// probability's exponent), and each probability as the sum of two bf16 numbers, 16 bits of it in 32 bits' range: O is in
 // its true unit, whatever the scales of other pages.  (One fp16 number, in a unit common to
 // a group's pages, keeps 11 bits, and fewer on pages whose scale is below the largest.)
 //   Bound by a wave's own chain, scores to softmax to value product, with two waves a
@@ -489,7 +491,10 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
     const bool fine = ks > 0.f && ks < INFINITY && vsc > 0.f && vsc < INFINITY;
     if (own && !fine && a.err) *a.err = SPEC_E_INVAL;
     const uint64_t good = __ballot(own && fine);
-    const int ev = own && fine ? exponent_of(vsc) : 0;   // lane l: the l-th page's value scale, 2^ev 2^lv
+    // lane l: the l-th page's scales, kp krest and vp 2^lv (kp, vp powers of two; every code times vp is a normal
+    // bf16 number, and kp leaves some range to queries of any magnitude)
+    const int ek = own && fine ? exponent_of(ks, -60, 60) : 0, ev = own && fine ? exponent_of(vsc, -116, 118) : 0;
+    const float krest = own && fine ? ks * power_of_two(-ek) : 1.f, kp = power_of_two(ek);
     const float lv = own && fine ? __builtin_amdgcn_logf(vsc * power_of_two(-ev)) : 0.f, vp = power_of_two(ev);
 
     while (p < 64) {
@@ -509,6 +514,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
         for (int h = 0; h < 2 * KH; ++h) qf[rb][h] = s_q[wr][rb][h][ql];
+      const float kpp = lane_f(kp, p);
       // (products on one accumulator stand apart, or the second waits for the first)
       f32x4 acc[4][NRB];
 #pragma unroll
@@ -518,7 +524,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
 #pragma unroll
           for (int k = t; k < t + 2; ++k) {
             const u32x4 w = kr[k][h >> 1];
-            const u32x4 x = h & 1 ? bf16_of_e4m3(w.z, w.w, 1.f) : bf16_of_e4m3(w.x, w.y, 1.f);
+            const u32x4 x = h & 1 ? bf16_of_e4m3(w.z, w.w, kpp) : bf16_of_e4m3(w.x, w.y, kpp);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) acc[k][rb] = mfma16x16x32(x, qf[rb][h], h ? acc[k][rb] : f32x4{0.f, 0.f, 0.f, 0.f});
           }
@@ -533,7 +539,7 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
       if (!full) mask(s, k0, sound ? INT32_MAX : 0);
       float sc[NRB];
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) sc[rb] = fmaxf(a.scale_log2 * lane_f(ks, p), 1e-37f);
+      for (int rb = 0; rb < NRB; ++rb) sc[rb] = fminf(fmaxf(a.scale_log2 * lane_f(krest, p), kLeast), FLT_MAX);
       u32x4 pb[NRB][2][2];                        // the parts of the probabilities of keys 8 e ..
       soft(st, s, sc, lane_f(lv, p), [&](int rb, float (&x)[16]) {
 #pragma unroll

@@ -141,3 +141,15 @@ def test_value_scales_of_every_magnitude(torch):  # noqa: F811
         c = Case(torch, 49 + seed, 4, 2, 128, [n], [10], np.array([[n, 64, 200, 500, 11 * PAGE]], np.int32))
         c.vs[:] = np.exp2(rng.integers(-126, 110, c.vs.shape)).astype(np.float32) * rng.uniform(1, 2, c.vs.shape).astype(np.float32)
         _check(c, floor=2.0 ** -133)
+
+
+@pytest.mark.parametrize("ks,q,scale", [(2.0 ** -126, 2e35, 128 ** -0.5), (1e-40, 2e36, 128 ** -0.5), (2.0 ** -149, 2e36, 1.0),
+                                        (2.0 ** 100, 2.0 ** -117, 2.0 ** 10), (2.0 ** 112, 2.0 ** -117, 2.0 ** -2),
+                                        (2.0 ** -120, 2.0 ** 10, 2.0 ** 107), (2.0 ** 126, 2.0 ** -117, 4.0)])
+def test_key_scales_far_out(torch, ks, q, scale):  # noqa: F811
+    for D in (64, 128):
+        n = 4 * PAGE
+        c = Case(torch, 52, 4, 2, D, [n], [4], _causal([n], 3))
+        c.q = ref.bf16(ref.bf16_value(c.q) * q)
+        c.ks[:], c.scale = ks, scale
+        _check(c)
