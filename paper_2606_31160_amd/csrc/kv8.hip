@@ -411,8 +411,11 @@ __global__ __launch_bounds__(64 * WR * kKeyWaves, 2) void k_kv8_attn(Kv8AttnArgs
   for (int rb = 0; rb < NRB; ++rb) {
     int j;
     const bf16_t* const qp = q_at(rb, j);
-    const int v = r0 + 16 * rb + n16 < rows ? row_vis(a, gr, s_vis[wave], b, j) : -1;
-    if (v > a.stride * kAttnChunk && a.err) *a.err = SPEC_E_INVAL;
+    int v = r0 + 16 * rb + n16 < rows ? row_vis(a, gr, s_vis[wave], b, j) : -1;
+    if (v > a.stride * kAttnChunk) {                // (no more than the table has: sums with it stay below 2^31)
+      if (a.err) *a.err = SPEC_E_INVAL;
+      v = a.stride * kAttnChunk;
+    }
     vis[rb] = v < 0 ? INT32_MAX : v;                // rows that nobody asked for need no mask
     vmin = min(vmin, vis[rb]);
     vmax = max(vmax, v);

@@ -153,3 +153,13 @@ def test_key_scales_far_out(torch, ks, q, scale):  # noqa: F811
         c.q = ref.bf16(ref.bf16_value(c.q) * q)
         c.ks[:], c.scale = ks, scale
         _check(c)
+
+
+# -- lengths -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("asked", [257, 2 ** 31 - 64, 2 ** 31 - 63, 2 ** 31 - 1])
+@pytest.mark.parametrize("packed", [0, 4])
+def test_rows_that_ask_for_more_than_there_is(torch, asked, packed):  # noqa: F811
+    """They see the table's slots, and the other rows their own."""
+    c = Case(torch, 53, 4, 2, 64, [4 * PAGE], [packed], np.array([[asked, 100, 0, -1, 256]], np.int32), extra=0)
+    _check(c, err=1)
