@@ -446,18 +446,26 @@ int attn_pages_per_workgroup(const spec_config* cfg, const spec_seq_init* seqs, 
 }
 
 // Pages of a group of the attention over a cache in 8 bits: fixed by the prompts
-// alone, as above, and so the same for every K.  A multiple of kKv8MinPages that leaves
-// no more groups than CUs; of kKv8MinPages itself, one page a wave, no more than run at
-// once in a pass of 17 rows, which may take two workgroups a group.  Verifies of 4
-// layers, 8 kv heads of 4 query heads, 4096 slots, with groups of 4 and 8 pages: 17 rows
-// 676, 644 us, 9 rows 582, 590, 5 rows 569, 565.
+// alone, as above, and so the same for every K.  A multiple of kKv8MinPages (to
+// kKv8MaxPages) that leaves no more groups than CUs; of kKv8MinPages itself, one page a
+// wave, no more than run at once in a pass of 17 rows, which may take two workgroups a
+// group.  Verifies of 4 layers, 8 kv heads of 4 query heads, 4096 slots, with groups of 4
+// and 8 pages: 17 rows 676, 644 us, 9 rows 582, 590, 5 rows 569, 565.
+//   Where sequences and kv heads are more than the CUs, no count leaves so few:
+// as many pages as divide groups of kKv8MinPages to about one a CU, up to
+// kKv8ManyPages, past which little is won and whole sequences in series leave the last
+// ones alone on the chip.  Verifies of 2 layers, 32 kv heads, K = 8, with 4, 8, 16, 32
+// and 64 pages: 16 scenes of 8192 tokens 1057, 666, 651, 644, 649 us; of 2048 tokens 340,
+// 326, 324, 329, 308; 9 scenes of 4096 tokens 336, 317, 314, 320, 362.
+constexpr int kKv8ManyPages = 16;
 int kv8_pages_per_group(const spec_config* cfg, const spec_seq_init* seqs, int ncu) {
   const int first = kv8_target_groups(17 * (cfg->target.q_heads / cfg->target.kv_heads), ncu);
   for (int ppw = kKv8MinPages;; ppw += kKv8MinPages) {
     long long groups = 0;
     for (int b = 0; b < cfg->batch; ++b) groups += cfg->target.kv_heads * (long long)(seqs[b].prefix_len / (kAttnChunk * ppw) + 1);
-    if (groups <= (ppw == kKv8MinPages ? first : ncu) || ppw >= kKv8MaxPages || (long long)cfg->batch * cfg->target.kv_heads > ncu)
-      return ppw;
+    if ((long long)cfg->batch * cfg->target.kv_heads > ncu)
+      return (int)std::min<long long>(groups / ncu * kKv8MinPages, kKv8ManyPages);
+    if (groups <= (ppw == kKv8MinPages ? first : ncu) || ppw >= kKv8MaxPages) return ppw;
   }
 }
 
