@@ -122,7 +122,7 @@ struct Ctx {
   float* part = nullptr;            // GEMV k-split partial sums
   size_t part_elems = 0;
   bf16_t* op = nullptr;             // [splits][B][q_heads][R][head_dim] attention partials (unnormalised)
-  size_t attn_rows = 0;             // splits * B * q_heads * R (max over the models)
+  size_t attn_rows = 0;             // splits * B * q_heads * R (max over the models that use op .. lp, rp)
   float* mp = nullptr;              // [splits][B][q_heads][R] running max (log2 units)
   float* lp = nullptr;              // [splits][B][q_heads][R] running sum
   float* amax_v = nullptr;          // [vocab/16][Mpad] per-tile maximum logit

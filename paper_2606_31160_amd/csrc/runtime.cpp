@@ -545,7 +545,9 @@ size_t carve(Ctx& c, const spec_config* cfg, const spec_seq_init* seqs, bool has
   c.rcs = cv.take<float2>((size_t)L.Mpad * (D / 2));
   c.part = cv.take<float>(part);
   c.part_elems = part;
-  const size_t attn_rows = (size_t)L.splits * L.B * nq * L.R;
+  // (a target cache in 8 bits has other partials, below)
+  const int attn_heads = !c.kv8 ? nq : has_draft ? cfg->draft.q_heads : 0;
+  const size_t attn_rows = (size_t)L.splits * L.B * attn_heads * L.R;
   c.attn_rows = attn_rows;
   c.op = cv.take<bf16_t>(attn_rows * D);
   c.mp = cv.take<float>(attn_rows);

@@ -22,3 +22,35 @@ def test_pages_of_a_group_grow_with_long_prompts_of_many_heads(scenes, kv_heads,
     for K in (0, 8):
         cfg, seqs, keep = _many_heads(scenes, kv_heads, prompt, K)
         assert B.spec_debug_attn_pages(cfg, seqs) == pages
+
+
+@pytest.mark.parametrize("draft", [True, False])
+def test_contexts_with_prompts_in_8_bits_hold_no_partials_that_nothing_writes(draft):
+    """Sixteen scenes of 8192 tokens at the 7B target's heads.  Of the 8-bit context: half the prompts' bytes and their
+    scales (8 bytes a page, layer and kv head); no bf16 attention's partials of the target (bf16 rows, two words, four
+    of the readout, for each page, sequence, query head and row), but its own (a row block of 16 fp32 rows, their
+    maxima and sums and a word, for each group)."""
+    w = W.get("C5")
+    if not draft:
+        w = w.with_(draft=None)
+    n, pages = {}, {}
+    for flags in (0, B.SPEC_FLAG_KV8):
+        cfg = _cfg(w.with_(draft=W.get("C5").draft), K=8, batch=16)
+        if not draft:
+            cfg.draft = B.dims(None)
+        cfg.flags = flags
+        seqs, keep = _seqs(w, cfg, prefix=8192, blocks=[])
+        n[flags] = B.spec_workspace_bytes(cfg, seqs)
+        pages[flags] = B.spec_debug_attn_pages(cfg, seqs)
+        each = B.spec_seq_pages(cfg, seqs[0])
+    t = w.target
+    slots = 16 * 8192 * t.kv_heads * t.head_dim * t.layers * 2
+    saved = slots - 16 * 128 * t.kv_heads * t.layers * 8
+    rows = each * 16 * 9
+    heads = t.q_heads - (w.draft.q_heads if draft else 0)
+    saved += rows * heads * (2 * t.head_dim + 8 + 16)
+    groups = 16 * t.kv_heads * -(-each // pages[B.SPEC_FLAG_KV8])
+    blocks = 4                                    # of 9 x 7 rows
+    own = groups * blocks * (16 * t.head_dim * 4 + 16 * 8 + 8)
+    assert t.q_heads // t.kv_heads == 7
+    assert abs(n[0] - n[B.SPEC_FLAG_KV8] - (saved - own)) <= 64 << 10     # page tables, alignment
