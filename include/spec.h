@@ -427,7 +427,7 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  * as they were.  Slots that a row does not see have no influence on it, whatever
  * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS; rows*q_heads/kv_heads < 2^20;
  * batch*kv_heads*table_stride <= 2^27.
- *   scale        positive and finite
+ *   scale        positive, at most 2^127
  *   d_table      [batch][table_stride] device int32; entries past a sequence's
  *                visible pages are not read
  *   d_packed     [batch] device int32

@@ -2,7 +2,6 @@
 // a cache held in 8 bits, attention over them, scores of logits.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
 #include <cstdio>
 
 #include "ctx.h"
@@ -126,7 +125,8 @@ spec_status spec_kv8_attn(const spec_kv8* c, int32_t batch, int32_t rows, int32_
   const int64_t width = (int64_t)q_heads * c->head_dim;
   if (q_stride < width || q_stride % 8 || out_stride < width || out_stride % 8)
     return fail(SPEC_E_INVAL, f, "q_stride and out_stride must be multiples of 8 and at least q_heads*head_dim");
-  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(SPEC_E_INVAL, f, "scale must be positive and finite");
+  // (its product with log2 e is finite)
+  if (!(scale > 0.f && scale <= 0x1p127f)) return fail(SPEC_E_INVAL, f, "scale must be positive and at most 2^127");
   if (!aligned(d_table, 4) || !aligned(d_packed, 4) || !aligned(d_visible, 4) || !aligned(q, 16) || !aligned(out, 16) ||
       (d_lse && !aligned(d_lse, 4)) || (d_err && !aligned(d_err, 4)))
     return fail(SPEC_E_INVAL, f, "null or misaligned pointer");

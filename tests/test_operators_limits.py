@@ -6,6 +6,7 @@ import pytest
 import workloads as W
 from paper_2606_31160_amd import binding as B
 from tests.test_abi_host import _cfg, _seqs
+from tests.test_operators_host import attn, cache, refused
 
 
 def _many_heads(scenes, kv_heads, prompt, K=8):
@@ -54,3 +55,10 @@ def test_contexts_with_prompts_in_8_bits_hold_no_partials_that_nothing_writes(dr
     own = groups * blocks * (16 * t.head_dim * 4 + 16 * 8 + 8)
     assert t.q_heads // t.kv_heads == 7
     assert abs(n[0] - n[B.SPEC_FLAG_KV8] - (saved - own)) <= 64 << 10     # page tables, alignment
+
+
+@pytest.mark.parametrize("scale,fine", [(2.0 ** 127, True), (1e-45, True), (1.0001 * 2.0 ** 127, False), (3.4e38, False)])
+def test_attention_scales_whose_product_with_log2_e_is_no_number_are_refused(scale, fine):
+    """(A call that is fine otherwise ends at its workspace.)"""
+    status, text = (3, "workspace") if fine else (1, "scale must be positive and at most 2^127")
+    refused(lambda: attn(cache(), scale=scale), status, text)
