@@ -115,8 +115,9 @@ typedef struct spec_dims {
                                       as spec_kv8_pack packs it (after rotation), the prompt's last slots and
                                       all later ones in bf16, as spec_kv8_attn reads them.  What a round rolls
                                       back never enters an 8-bit page, so greedy output stays the same for
-                                      every K.  The target's caches take half the bytes.  Each kind's pages
-                                      lie in a pool of their own, in the order of their page_table numbers.
+                                      every K.  The prompts' whole pages take half the bytes.  Each kind's
+                                      pages lie in a pool of their own, in the order of their page_table
+                                      numbers.
                                       The attention-budget readout of the target is not available. */
 #define SPEC_FLAG_DRAFT_MROPE 16   /* the draft rotates with 3D M-RoPE (its own mrope_section and
                                       interleaved, validated as the target's) instead of FlatRoPE: the
@@ -406,11 +407,11 @@ typedef struct spec_kv8 {
 } spec_kv8;
 
 /* Packs the keys (as the cache holds them, after rotation) and values of `rows`
- * (1..2^28) tokens into 8-bit pages: rows [64 i, 64 i + 64) into pool page d_pages[i]
- * (device int32, ceil(rows / 64) entries, no page twice).  k, v: bf16 rows of
- * [kv_heads][head_dim], 16-byte aligned, row_stride elements apart (a multiple of
- * 8; the rows may lie in a fused projection).  A page and head's scale is the
- * smallest power of two s, at least 2^-126, with max |x| <= 448 s over its finite
+ * (1..2^28) tokens of at most 65535 kv heads into 8-bit pages: rows [64 i, 64 i + 64)
+ * into pool page d_pages[i] (device int32, ceil(rows / 64) entries, no page twice).
+ * k, v: bf16 rows of [kv_heads][head_dim], 16-byte aligned, row_stride elements apart
+ * (a multiple of 8; the rows may lie in a fused projection).  A page and head's scale
+ * is the smallest power of two s, at least 2^-126, with max |x| <= 448 s over its finite
  * values (1 if all are zero); codes are x / s to nearest even.  NaN and infinities
  * become NaN.  Slots past the rows are set to zero.  What a page stands for is
  * exact in bf16 (but for magnitudes from 248 * 2^120, which round to 2^128).  An
@@ -425,7 +426,9 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  *   out = sum_s p_s v_s,  p = softmax(scale * q . k_s),  lse = ln sum_s e^(scale * q . k_s).
  * n = 0: out = 0 and lse = -infinity.  n < 0: no such row; its out and lse are left
  * as they were.  Slots that a row does not see have no influence on it, whatever
- * they hold.  1 <= batch*rows <= SPEC_MAX_ROWS; rows*q_heads/kv_heads < 2^20;
+ * they hold.  An infinite value that a row sees makes its result infinite however
+ * small its p (NaN against the other infinity).  1 <= batch*rows <= SPEC_MAX_ROWS;
+ * rows*q_heads/kv_heads <= 1048560; q_heads*head_dim <= 2^20; table_stride < 2^25;
  * batch*kv_heads*table_stride <= 2^27.
  *   scale        positive, at most 2^127
  *   d_table      [batch][table_stride] device int32; entries past a sequence's
@@ -439,8 +442,10 @@ spec_status spec_kv8_pack(const spec_kv8* cache, const void* k, const void* v, i
  *                table entry lay outside its pool or a scale was not positive and
  *                finite (the page is then taken as not visible; a row that sees no
  *                other has NaN in out and -infinity in lse), or a row wanted more
- *                slots than the table has
- * Sums are formed in 32 bits, in an order fixed by the arguments and lengths. */
+ *                slots than the table has (it sees those there are)
+ * Scores, softmax and sums are formed in 32 bits, in an order fixed by the arguments
+ * and lengths; p meets the values as the sum of two bf16 numbers, within 2^-16 of
+ * itself. */
 spec_status spec_kv8_attn(const spec_kv8* cache, int32_t batch, int32_t rows, int32_t q_heads, const int32_t* d_table,
                           int32_t table_stride, const int32_t* d_packed, const int32_t* d_visible, const void* q,
                           int64_t q_stride, float scale, void* out, int64_t out_stride, float* d_lse, int32_t* d_err,

@@ -62,3 +62,16 @@ def test_attention_scales_whose_product_with_log2_e_is_no_number_are_refused(sca
     """(A call that is fine otherwise ends at its workspace.)"""
     status, text = (3, "workspace") if fine else (1, "scale must be positive and at most 2^127")
     refused(lambda: attn(cache(), scale=scale), status, text)
+
+
+def test_attention_takes_what_its_limits_say():
+    """Each limit of a pass, and one more."""
+    n = lambda c, *a: B.spec_kv8_attn_workspace_bytes(c, *a)  # noqa: E731
+    one = cache(kv_heads=1)
+    assert n(one, 1, 80, 13107, 1) > 0                                            # 80 x 13107 = 1048560 rows of a kv head
+    refused(lambda: n(one, 1, 70, 14980, 1), 1, "rows*q_heads/kv_heads")          # 1048600
+    assert n(cache(kv_heads=16384), 1, 1, 16384, 1) > 0                           # q_heads*head_dim = 2^20
+    refused(lambda: n(cache(kv_heads=16385), 1, 1, 16385, 1), 1, "q_heads*head_dim")
+    assert n(one, 4, 1, 1, 2 ** 25 - 1) > 0                                       # table_stride, and 2^27 pages less four
+    refused(lambda: n(one, 1, 1, 1, 2 ** 25), 1, "table_stride")
+    refused(lambda: n(one, 5, 1, 1, 2 ** 25 - 1), 1, "batch*kv_heads*table_stride")
