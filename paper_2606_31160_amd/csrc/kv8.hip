@@ -840,8 +840,9 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
     s_l[wave][n16] = L;
   }
   __syncthreads();
-  if (wave != 0 || sub != 0) return;
-  if (vis < 0) return;                              // no such row: left as it was
+  if (wave != 0) return;
+  const uint64_t having = __ballot(lane < NW && s_has[lane % NW]);
+  if (sub != 0 || vis < 0) return;                  // no such row: left as it was
   M = -INFINITY;
 #pragma unroll
   for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][n16]);
@@ -849,11 +850,11 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_combine(Kv8AttnArgs a, int nrb)
   L = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    if (s_has[w]) x += s_x[w][lane];
     const float m = s_m[w][n16], f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
     o += s_o[w][lane] * f;
     L += s_l[w][n16] * f;
   }
+  for (uint64_t w = having; w; w &= w - 1) x += s_x[__builtin_ctzll(w)][lane];
   if (vis == 0) {
     o = f32x4{0.f, 0.f, 0.f, 0.f};
   } else {
