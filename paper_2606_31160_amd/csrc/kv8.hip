@@ -37,6 +37,7 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 // cache would hold them.  Infinities become NaN and count for no scale.  Slots
 // past the rows are zero.  Bound by memory: 4096 tokens of 8 heads of 128, 17 MB read
 // and 8 MB written, 6.4 us a call in graphs (3.9 TB/s; a copy of 4 GiB reaches 4.7).
+// With rotation, in a trace, 10.4 us where 7.6 without: a table's row for each pair.
 // ---------------------------------------------------------------------------
 template <int D, bool ROT>
 __global__ __launch_bounds__(256) void k_kv8_pack(Kv8PackArgs a) {
@@ -338,20 +339,22 @@ __device__ __forceinline__ void soft(RowState<NRB, NDT>& st, const float (&s)[NR
 // is the same in Q's operand.
 //   The next page's keys are loaded while this one's softmax runs, its values while
 // the next scores are formed.  (Pages by way of LDS, for the two waves of WR = 2 at
-// once, took longer: 33 us where this takes 29.5, the waves in step at its barriers.)
+// once, took longer: 33 us where registers took 29.5, the waves in step at its barriers.)
 //   Keys are read as bf16, like Q: an e4m3 code is exact in it, also times its scale's
 // power of two (what is left of a scale is part of the scores' factor).  (16x16x128 MFMA
 // of e4m3 numbers, against Q in two parts of four bits each, took as long, and their
 // sums drop what is some 2^-16 of the largest product: scores 1e-5 off, not 1e-7.)
 //   Values are read as bf16 in the same way (with the rest of a scale in the
-// probability's exponent), and each probability as the sum of two bf16 numbers, 16 bits of it in 32 bits' range: O is in
-// its true unit, whatever the scales of other pages.  (One fp16 number, in a unit common to
-// a group's pages, keeps 11 bits, and fewer on pages whose scale is below the largest.)
+// probability's exponent), and each probability as the sum of two bf16 numbers, 16 bits
+// of it in 32 bits' range: O is in its true unit, whatever the scales of other pages.
+// (One fp16 number, in a unit common to a group's pages, keeps 11 bits, and fewer on
+// pages whose scale is below the largest; with half the value products it took 34.3 us a
+// call where this takes 35.1, 16 scenes of 9 rows, and 15.0 for 15.3, one scene.)
 //   Bound by a wave's own chain, scores to softmax to value product, with two waves a
-// SIMD (of 16 scenes of 2 to 8 thousand tokens, 80 MB: 9 rows each 29.6 us, vector
-// unit 35% busy, matrix unit 14%; one row each 18.1 us, 4.4 TB/s), and where a wave has
+// SIMD (of 16 scenes of 2 to 8 thousand tokens, 80 MB: 9 rows each 31.2 us, vector
+// unit 39% busy, matrix unit 21%; one row each 18.5 us, 4.3 TB/s), and where a wave has
 // a page or two by the loads before the first product, each waiting for the last:
-// about 5 us of 11.6 for 9 rows of one sequence of 4096.
+// about 5 us of 11.8 for 9 rows of one sequence of 4096.
 //   Which pages share a wave depends on the group only, and a row's sums on no
 // other row, so contexts that differ in K, and so in NRB and WR, sum alike.
 template <int D, int NRB, int WR>
