@@ -476,6 +476,111 @@ spec_status spec_logprobs(const void* logits, int32_t dtype, int32_t rows, int32
                           hipStream_t stream);
 spec_status spec_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top, size_t* bytes);
 
+/* A pass over trees of drafted tokens.  Where spec_verify checks one chain of
+ * proposals, a tree holds several alternatives for a position: each row continues
+ * its parent, a row sees its ancestors and no sibling, and the longest path that
+ * greedy decoding confirms is committed.  Three operators, over pages laid out as a
+ * context's own: spec_kv_append writes the rows' keys and values to the cache,
+ * spec_tree_attn is the attention of each layer, and spec_tree_commit, after the
+ * target's greedy tokens are known, takes the path and moves its keys and values to
+ * consecutive slots in every layer. */
+
+/* A model's KV cache in bf16 pages. */
+typedef struct spec_kv {
+  int32_t kv_heads;          /* 1..65535 */
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t pages;             /* pages of a layer's pool, >= 1 */
+  int32_t layers;            /* 1..SPEC_MAX_LAYERS */
+  int64_t layer_stride;      /* elements from a layer's pool to the next one's, the same for keys and
+                                values: a multiple of 8, at least a pool (any value for one layer) */
+  void* k;                   /* bf16 [layers][pages][kv_heads][SPEC_KV_PAGE][head_dim], 16-byte aligned */
+  void* v;                   /* bf16 [layers][pages][kv_heads][head_dim][SPEC_KV_PAGE] (transposed), 16-byte aligned */
+} spec_kv;
+
+/* The rows of a pass.  Sequence b has rows d_first[b] .. d_first[b + 1] - 1 (none is
+ * allowed), row d_first[b] + j standing for slot d_len[b] + j: page d_table[b][slot / 64]
+ * of the pool, offset slot % 64.  Rows outside every sequence are left as they were in
+ * every output.
+ * What the host cannot see is checked on the device, which sets *d_err to SPEC_E_INVAL
+ * (else leaves it alone) and goes on in bounds: if d_first decreases or leaves [0, rows], no
+ * sequence has rows; one whose d_len is negative or more than its table's slots has none; a
+ * parent that is not an earlier row of the sequence counts as -1; slots past the table, and
+ * pages outside the pool, are not written, not moved and not visible.
+ * No page may belong to two sequences where one of them writes it. */
+typedef struct spec_rows {
+  int32_t batch;             /* 1..SPEC_MAX_ROWS */
+  int32_t rows;              /* rows of the buffers: 1..SPEC_MAX_ROWS (spec_kv_append without trees: to 2^28) */
+  const int32_t* d_first;    /* [batch + 1] device int32 */
+  const int32_t* d_len;      /* [batch] slots in use before the pass */
+  const int32_t* d_table;    /* [batch][table_stride]; entries of pages that a call does not touch are not read */
+  int32_t table_stride;      /* 1..2^25 - 1 */
+  const int32_t* d_parent;   /* [rows] row of the same sequence (counted from its first) that the row continues, an
+                                earlier one, or -1; NULL: chains, each row continues the one before it */
+  int32_t* d_err;            /* device int32 or NULL */
+} spec_rows;
+
+/* Rotary positions: pair d of a head (dimensions 2d, 2d + 1) turns by
+ * base^(-2d/head_dim) times the position on its axis, T, H or W, assigned as
+ * spec_dims does (FlatRoPE: section {head_dim/2, 0, 0}). */
+typedef struct spec_rope {
+  float base;                /* > 1 */
+  int32_t section[3];        /* pairs per axis, summing to head_dim/2 */
+  int32_t interleaved;       /* 1: pair d takes axis d mod 3, whatever the sections */
+} spec_rope;
+
+/* Writes a pass's rows to their slots of layer `layer`: keys rotated, values
+ * transposed; queries are rotated into q_out (q may be NULL with q_heads = 0; q_out may be
+ * q itself with the same stride; otherwise outputs overlap no input).
+ *   d_pos   [3][rows] device int32: positions on T, H and W (axes without pairs are not
+ *           read), or NULL: on every axis d_len[b] + the number of the row's
+ *           ancestors (then rows <= SPEC_MAX_ROWS if d_parent is given)
+ *   q, k, v bf16 rows of [q_heads] and [kv_heads] x head_dim, 16-byte aligned, q_stride and
+ *           kv_stride elements apart (multiples of 8; they may lie in a fused projection)
+ * q_heads need not be a multiple of kv_heads; q_heads*head_dim <= 2^20.  Angles are
+ * formed in 64 bits, a result is rounded to bf16 once, values are copied as they are. */
+spec_status spec_kv_append(const spec_kv* cache, int32_t layer, const spec_rows* rows, const spec_rope* rope,
+                           const int32_t* d_pos, int32_t q_heads, const void* q, int64_t q_stride, const void* k,
+                           const void* v, int64_t kv_stride, void* q_out, int64_t q_out_stride, hipStream_t stream);
+
+/* Grouped-query attention of a pass's rows over layer `layer`, whose slots hold the
+ * rows' own keys and values already.  A row of sequence b sees slots [0, d_len[b]),
+ * its ancestors' slots and its own; for query head h of kv head h / (q_heads / kv_heads)
+ *   out = sum_s p_s v_s,  p = softmax(scale * q . k_s),  lse = ln sum_s e^(scale * q . k_s).
+ * Slots that a row does not see have no influence on it, whatever they hold.  An
+ * infinite value that a row sees makes its result infinite however small its p
+ * (NaN against the other infinity).  A row that sees no slot (its page lies outside the pool) has
+ * NaN in out and -infinity in lse.
+ *   scale   positive, at most 2^127
+ *   q, out  bf16, row r at r * stride, [q_heads][head_dim]; strides are multiples of 8,
+ *           pointers 16-byte aligned; they do not overlap
+ *   d_lse   [rows][q_heads] device float, or NULL
+ * q_heads is a multiple of kv_heads; q_heads*head_dim <= 2^20; batch*kv_heads*table_stride <= 2^27.
+ * Scores, softmax and sums are formed in 32 bits, in an order fixed by the arguments and
+ * lengths; p meets the values as the sum of two bf16 numbers, within 2^-16 of itself. */
+spec_status spec_tree_attn(const spec_kv* cache, int32_t layer, const spec_rows* rows, int32_t q_heads, const void* q,
+                           int64_t q_stride, float scale, void* out, int64_t out_stride, float* d_lse, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+spec_status spec_tree_attn_workspace_bytes(const spec_kv* cache, const spec_rows* rows, int32_t q_heads, size_t* bytes);
+
+/* Accept and commit of a tree (Eq. accept, Eq. commit on the tree's paths).  Row 0 of a
+ * sequence is its pending token.  The path begins there and goes from row j on to the
+ * lowest row whose parent is j and whose token is j's greedy token, as long as there is one;
+ * the greedy tokens along the path, l + 1 of them, are committed, cut after a stop token or
+ * at the budget.  Of n committed tokens, the first n rows of the path move to slots
+ * d_len[b] .. d_len[b] + n - 1, in every layer, and the sequence goes on with n more
+ * slots and the last committed token pending.  Other slots are left as they were.
+ *   d_tokens     [rows] device int32: token of each row
+ *   d_greedy     [rows]: the target's greedy token after each row
+ *   stop_token   -1: none
+ *   d_budget     [batch]: tokens that may yet be committed (a sequence with none left commits none), or NULL
+ *   d_path       [rows]: entry d_first[b] + i is the i-th committed step's row of the sequence
+ *   d_committed  [rows]: ... its greedy token (entries past n are left as they were in both)
+ *   d_n          [batch]: n;  d_new_len [batch]: d_len + n
+ * Any of d_path, d_committed, d_n and d_new_len may be NULL; none may overlap an input or another. */
+spec_status spec_tree_commit(const spec_kv* cache, const spec_rows* rows, const int32_t* d_tokens, const int32_t* d_greedy,
+                             int32_t stop_token, const int32_t* d_budget, int32_t* d_path, int32_t* d_committed,
+                             int32_t* d_n, int32_t* d_new_len, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -76,6 +76,20 @@ class spec_kv8(Structure):
                 ("v16", c_void_p)]
 
 
+class spec_kv(Structure):
+    _fields_ = [("kv_heads", c_int32), ("head_dim", c_int32), ("pages", c_int32), ("layers", c_int32),
+                ("layer_stride", c_int64), ("k", c_void_p), ("v", c_void_p)]
+
+
+class spec_rows(Structure):
+    _fields_ = [("batch", c_int32), ("rows", c_int32), ("d_first", c_void_p), ("d_len", c_void_p), ("d_table", c_void_p),
+                ("table_stride", c_int32), ("d_parent", c_void_p), ("d_err", c_void_p)]
+
+
+class spec_rope(Structure):
+    _fields_ = [("base", c_float), ("section", c_int32 * 3), ("interleaved", c_int32)]
+
+
 class SpecError(RuntimeError):
     def __init__(self, status: int, func: str, msg: str):
         self.status = status
@@ -119,6 +133,12 @@ def lib():
             "spec_kv8_attn_workspace_bytes": [POINTER(spec_kv8), c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)],
             "spec_logprobs": [P, c_int32, c_int32, c_int32, c_int64, P, c_int32, c_int32, P, P, P, P, P, c_size_t, P],
             "spec_logprobs_workspace_bytes": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
+            "spec_kv_append": [POINTER(spec_kv), c_int32, POINTER(spec_rows), POINTER(spec_rope), P, c_int32, P, c_int64, P,
+                               P, c_int64, P, c_int64, P],
+            "spec_tree_attn": [POINTER(spec_kv), c_int32, POINTER(spec_rows), c_int32, P, c_int64, c_float, P, c_int64, P,
+                               P, c_size_t, P],
+            "spec_tree_attn_workspace_bytes": [POINTER(spec_kv), POINTER(spec_rows), c_int32, POINTER(c_size_t)],
+            "spec_tree_commit": [POINTER(spec_kv), POINTER(spec_rows), P, P, c_int32, P, P, P, P, P, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -294,6 +314,45 @@ def spec_logprobs(logits: int, dtype: int, rows: int, vocab: int, row_stride: in
                   workspace_bytes: int, stream: int = 0) -> None:
     _check(lib().spec_logprobs(logits, dtype, rows, vocab, row_stride, d_tokens, n_tokens, top, d_logprob, d_entropy,
                                d_top_token, d_top_logprob, workspace, workspace_bytes, stream), "spec_logprobs")
+
+
+def kv(kv_heads: int, head_dim: int, pages: int, k: int, v: int, layers: int = 1, layer_stride: int = 0) -> spec_kv:
+    """The description of a model's KV cache in bf16 pages."""
+    return spec_kv(kv_heads, head_dim, pages, layers, layer_stride, k, v)
+
+
+def rows(batch: int, rows: int, d_first: int, d_len: int, d_table: int, table_stride: int, d_parent: int = 0,
+         d_err: int = 0) -> spec_rows:
+    """The description of a pass's rows: whose they are, their slots and the rows that they continue."""
+    return spec_rows(batch, rows, d_first, d_len, d_table, table_stride, d_parent, d_err)
+
+
+def rope(base: float, section, interleaved: int = 0) -> spec_rope:
+    return spec_rope(base, tuple(section), interleaved)
+
+
+def spec_kv_append(cache: spec_kv, layer: int, rows: spec_rows, rope: spec_rope, d_pos: int, q_heads: int, q: int,
+                   q_stride: int, k: int, v: int, kv_stride: int, q_out: int, q_out_stride: int, stream: int = 0) -> None:
+    _check(lib().spec_kv_append(cache, layer, rows, rope, d_pos, q_heads, q, q_stride, k, v, kv_stride, q_out,
+                                q_out_stride, stream), "spec_kv_append")
+
+
+def spec_tree_attn_workspace_bytes(cache: spec_kv, rows: spec_rows, q_heads: int) -> int:
+    n = c_size_t(0)
+    _check(lib().spec_tree_attn_workspace_bytes(cache, rows, q_heads, ctypes.byref(n)), "spec_tree_attn_workspace_bytes")
+    return n.value
+
+
+def spec_tree_attn(cache: spec_kv, layer: int, rows: spec_rows, q_heads: int, q: int, q_stride: int, scale: float, out: int,
+                   out_stride: int, d_lse: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().spec_tree_attn(cache, layer, rows, q_heads, q, q_stride, scale, out, out_stride, d_lse, workspace,
+                                workspace_bytes, stream), "spec_tree_attn")
+
+
+def spec_tree_commit(cache: spec_kv, rows: spec_rows, d_tokens: int, d_greedy: int, stop_token: int = -1, d_budget: int = 0,
+                     d_path: int = 0, d_committed: int = 0, d_n: int = 0, d_new_len: int = 0, stream: int = 0) -> None:
+    _check(lib().spec_tree_commit(cache, rows, d_tokens, d_greedy, stop_token, d_budget, d_path, d_committed, d_n, d_new_len,
+                                  stream), "spec_tree_commit")
 
 
 def spec_timing(ctx, enable: bool) -> None:

@@ -1,12 +1,14 @@
 // Entry points of the operators that need no context (include/spec.h): pages of
-// a cache held in 8 bits, attention over them, scores of logits.
+// a cache held in 8 bits, attention over them, scores of logits; passes over trees.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdio>
 
 #include "ctx.h"
 #include "kv8.h"
 #include "logprobs.h"
+#include "tree.h"
 
 using namespace specdec;
 
@@ -74,6 +76,54 @@ const char* bad_scores(int32_t rows, int32_t vocab, int32_t top) {
   if (vocab < 1 || vocab > kLogprobMaxVocab) return "vocab out of range";
   if (top < 0 || top > SPEC_MAX_TOP || top > vocab) return "top must be 0..SPEC_MAX_TOP and at most vocab";
   return nullptr;
+}
+
+constexpr int32_t kMaxTable = INT32_MAX / SPEC_KV_PAGE;
+
+// What is wrong with a cache, or with a pass over it, or null.
+const char* bad_kv(const spec_kv* c) {
+  if (!c) return "null cache";
+  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+  if (c->kv_heads < 1 || c->kv_heads > 65535) return "kv_heads must be 1..65535";
+  if (c->pages < 1) return "pages must be at least 1";
+  if (c->layers < 1 || c->layers > SPEC_MAX_LAYERS) return "layers must be 1..SPEC_MAX_LAYERS";
+  if (c->layers > 1 && (c->layer_stride % 8 || c->layer_stride / (SPEC_KV_PAGE * c->head_dim) < (int64_t)c->pages * c->kv_heads ||
+                        c->layer_stride > INT64_MAX / (4 * SPEC_MAX_LAYERS)))
+    return "layer_stride must be a multiple of 8 and at least a pool";
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return "keys or values null or misaligned";
+  return nullptr;
+}
+const char* bad_layer(const spec_kv* c, int32_t layer) {
+  if (const char* w = bad_kv(c)) return w;
+  return layer < 0 || layer >= c->layers ? "no such layer" : nullptr;
+}
+const char* bad_rows(const spec_rows* r, int32_t most) {
+  if (!r) return "null rows";
+  if (r->batch < 1 || r->batch > SPEC_MAX_ROWS) return "batch must be 1..SPEC_MAX_ROWS";
+  if (r->rows < 1 || r->rows > most) return "rows out of range";
+  if (r->table_stride < 1 || r->table_stride > kMaxTable) return "table_stride out of range";
+  if (!aligned(r->d_first, 4) || !aligned(r->d_len, 4) || !aligned(r->d_table, 4) || (r->d_parent && !aligned(r->d_parent, 4)) ||
+      (r->d_err && !aligned(r->d_err, 4)))
+    return "rows: null or misaligned pointer";
+  return nullptr;
+}
+const char* bad_tree_pass(const spec_kv* c, const spec_rows* r, int32_t q_heads) {
+  if (const char* w = bad_rows(r, SPEC_MAX_ROWS)) return w;
+  if (q_heads < 1 || q_heads % c->kv_heads) return "q_heads must be a multiple of kv_heads";
+  if ((int64_t)q_heads * c->head_dim > (1 << 20)) return "q_heads*head_dim too large";
+  if ((int64_t)r->batch * c->kv_heads * r->table_stride > kMaxPageHeads) return "batch*kv_heads*table_stride too large";
+  return nullptr;
+}
+TreeRows tree_rows(const spec_kv* c, const spec_rows* r) {
+  return TreeRows{r->batch, r->rows, r->table_stride, r->d_first, r->d_len, r->d_table, r->d_parent, r->d_err, c->pages, c->kv_heads};
+}
+bf16_t* layer_of(const spec_kv* c, void* pool, int32_t layer) {
+  return static_cast<bf16_t*>(pool) + (c->layers > 1 ? layer * c->layer_stride : 0);
+}
+// Whether [a, a + n) and [b, b + m) share a byte (null: nothing there).
+bool overlap(const void* a, size_t n, const void* b, size_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x && y && x < y + m && y < x + n;
 }
 
 }  // namespace
@@ -208,6 +258,124 @@ spec_status spec_logprobs(const void* logits, int32_t dtype, int32_t rows, int32
   a.keys = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + stats);
   a.splits = splits;
   return launched(launch_logprobs(a, dtype, stream), f);
+}
+
+spec_status spec_kv_append(const spec_kv* c, int32_t layer, const spec_rows* r, const spec_rope* rope, const int32_t* d_pos,
+                           int32_t q_heads, const void* q, int64_t q_stride, const void* k, const void* v, int64_t kv_stride,
+                           void* q_out, int64_t q_out_stride, hipStream_t stream) {
+  const char* const f = "spec_kv_append";
+  if (const char* w = bad_layer(c, layer)) return fail(SPEC_E_INVAL, f, w);
+  if (const char* w = bad_rows(r, r && r->d_parent && !d_pos ? SPEC_MAX_ROWS : kMaxPackRows)) return fail(SPEC_E_INVAL, f, w);
+  if (!rope) return fail(SPEC_E_INVAL, f, "null rope");
+  if (!(rope->base > 1.f) || !std::isfinite(rope->base)) return fail(SPEC_E_INVAL, f, "base must be > 1");
+  if (rope->interleaved != 0 && rope->interleaved != 1) return fail(SPEC_E_INVAL, f, "interleaved must be 0 or 1");
+  const int32_t *sec = rope->section, half = c->head_dim / 2;
+  if (sec[0] < 0 || sec[1] < 0 || sec[2] < 0 || (int64_t)sec[0] + sec[1] + sec[2] != half)
+    return fail(SPEC_E_INVAL, f, "section must be non-negative and sum to head_dim/2");
+  if (q_heads < 0 || (int64_t)q_heads * c->head_dim > (1 << 20)) return fail(SPEC_E_INVAL, f, "q_heads out of range");
+  const int64_t width = (int64_t)q_heads * c->head_dim;
+  if (q_heads > 0 && (q_stride < width || q_stride % 8 || q_out_stride < width || q_out_stride % 8))
+    return fail(SPEC_E_INVAL, f, "q_stride and q_out_stride must be multiples of 8 and at least q_heads*head_dim");
+  if (kv_stride < (int64_t)c->kv_heads * c->head_dim || kv_stride % 8)
+    return fail(SPEC_E_INVAL, f, "kv_stride must be a multiple of 8 and at least kv_heads*head_dim");
+  if (!aligned(k, 16) || !aligned(v, 16) || (q_heads > 0 && (!aligned(q, 16) || !aligned(q_out, 16))) || (d_pos && !aligned(d_pos, 4)))
+    return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
+  if (q_heads > 0 && q == q_out && q_stride != q_out_stride) return fail(SPEC_E_INVAL, f, "q_out on q needs the same stride");
+  AppendArgs a{};
+  a.t = tree_rows(c, r);
+  a.kc = layer_of(c, c->k, layer);
+  a.vt = layer_of(c, c->v, layer);
+  a.q = static_cast<const bf16_t*>(q);
+  a.k = static_cast<const bf16_t*>(k);
+  a.v = static_cast<const bf16_t*>(v);
+  a.q_stride = q_stride;
+  a.kv_stride = kv_stride;
+  a.q_out = static_cast<bf16_t*>(q_out);
+  a.q_out_stride = q_out_stride;
+  a.nq = q_heads;
+  a.pos = d_pos;
+  a.axis_end[0] = rope->interleaved ? -1 : sec[0];
+  a.axis_end[1] = rope->interleaved ? -1 : sec[0] + sec[1];
+  for (int d = 0; d < half; ++d)
+    a.turns[d] = std::pow((double)rope->base, -2.0 * d / c->head_dim) / 6.283185307179586476925286766559;
+  return launched(launch_kv_append(a, c->head_dim, stream), f);
+}
+
+spec_status spec_tree_attn_workspace_bytes(const spec_kv* c, const spec_rows* r, int32_t q_heads, size_t* bytes) {
+  const char* const f = "spec_tree_attn_workspace_bytes";
+  if (!bytes) return fail(SPEC_E_INVAL, f, "null result");
+  if (const char* w = bad_kv(c)) return fail(SPEC_E_INVAL, f, w);
+  if (const char* w = bad_tree_pass(c, r, q_heads)) return fail(SPEC_E_INVAL, f, w);
+  *bytes = kAlign;
+  return SPEC_OK;
+}
+
+spec_status spec_tree_attn(const spec_kv* c, int32_t layer, const spec_rows* r, int32_t q_heads, const void* q, int64_t q_stride,
+                           float scale, void* out, int64_t out_stride, float* d_lse, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream) {
+  const char* const f = "spec_tree_attn";
+  if (const char* w = bad_layer(c, layer)) return fail(SPEC_E_INVAL, f, w);
+  if (const char* w = bad_tree_pass(c, r, q_heads)) return fail(SPEC_E_INVAL, f, w);
+  const int64_t width = (int64_t)q_heads * c->head_dim;
+  if (q_stride < width || q_stride % 8 || out_stride < width || out_stride % 8)
+    return fail(SPEC_E_INVAL, f, "q_stride and out_stride must be multiples of 8 and at least q_heads*head_dim");
+  // (its product with log2 e is finite)
+  if (!(scale > 0.f && scale <= 0x1p127f)) return fail(SPEC_E_INVAL, f, "scale must be positive and at most 2^127");
+  if (!aligned(q, 16) || !aligned(out, 16) || (d_lse && !aligned(d_lse, 4))) return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
+  if (!aligned(workspace, kAlign)) return fail(SPEC_E_INVAL, f, "workspace: null or not 256-byte aligned");
+  if (workspace_bytes < kAlign) return fail(SPEC_E_CAPACITY, f, "workspace too small (query spec_tree_attn_workspace_bytes)");
+  TreeAttnArgs a{};
+  a.t = tree_rows(c, r);
+  a.kc = layer_of(c, c->k, layer);
+  a.vt = layer_of(c, c->v, layer);
+  a.q = static_cast<const bf16_t*>(q);
+  a.q_stride = q_stride;
+  a.out = static_cast<bf16_t*>(out);
+  a.out_stride = out_stride;
+  a.lse = d_lse;
+  a.nq = q_heads;
+  a.G = q_heads / c->kv_heads;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  return launched(launch_tree_attn(a, c->head_dim, stream), f);
+}
+
+spec_status spec_tree_commit(const spec_kv* c, const spec_rows* r, const int32_t* d_tokens, const int32_t* d_greedy,
+                             int32_t stop_token, const int32_t* d_budget, int32_t* d_path, int32_t* d_committed, int32_t* d_n,
+                             int32_t* d_new_len, hipStream_t stream) {
+  const char* const f = "spec_tree_commit";
+  if (const char* w = bad_kv(c)) return fail(SPEC_E_INVAL, f, w);
+  if (const char* w = bad_rows(r, SPEC_MAX_ROWS)) return fail(SPEC_E_INVAL, f, w);
+  if (stop_token < -1) return fail(SPEC_E_INVAL, f, "stop_token must be -1 or a token");
+  if (c->kv_heads > 32767) return fail(SPEC_E_INVAL, f, "too many kv heads");
+  const size_t rows = 4 * (size_t)r->rows, batch = 4 * (size_t)r->batch;
+  const struct { const void* p; size_t n; } in[] = {{r->d_first, batch + 4}, {r->d_len, batch}, {r->d_table, batch * r->table_stride},
+                                                    {r->d_parent, rows}, {d_tokens, rows}, {d_greedy, rows}, {d_budget, batch}},
+                                            out[] = {{d_path, rows}, {d_committed, rows}, {d_n, batch}, {d_new_len, batch}};
+  if (!aligned(d_tokens, 4) || !aligned(d_greedy, 4) || (d_budget && !aligned(d_budget, 4)))
+    return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
+  for (const auto& o : out) {
+    if (o.p && !aligned(o.p, 4)) return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
+    // every workgroup reads the inputs while one writes these
+    for (const auto& i : in)
+      if (overlap(o.p, o.n, i.p, i.n)) return fail(SPEC_E_INVAL, f, "an output overlaps an input");
+    for (const auto& p : out)
+      if (&p != &o && overlap(o.p, o.n, p.p, p.n)) return fail(SPEC_E_INVAL, f, "outputs overlap");
+  }
+  TreeCommitArgs a{};
+  a.t = tree_rows(c, r);
+  a.layers = c->layers;
+  a.layer_stride = c->layers > 1 ? c->layer_stride : 0;
+  a.kc = static_cast<bf16_t*>(c->k);
+  a.vt = static_cast<bf16_t*>(c->v);
+  a.tokens = d_tokens;
+  a.greedy = d_greedy;
+  a.budget = d_budget;
+  a.stop = stop_token;
+  a.path = d_path;
+  a.committed = d_committed;
+  a.n = d_n;
+  a.new_len = d_new_len;
+  return launched(launch_tree_commit(a, c->head_dim, stream), f);
 }
 
 }  // extern "C"
