@@ -117,6 +117,9 @@ const char* bad_tree_pass(const spec_kv* c, const spec_rows* r, int32_t q_heads)
 TreeRows tree_rows(const spec_kv* c, const spec_rows* r) {
   return TreeRows{r->batch, r->rows, r->table_stride, r->d_first, r->d_len, r->d_table, r->d_parent, r->d_err, c->pages, c->kv_heads};
 }
+TreeAttnPlan attn_plan(const spec_kv* c, const spec_rows* r, int32_t q_heads) {
+  return tree_attn_plan(r->batch, r->rows, c->kv_heads, q_heads / c->kv_heads, c->head_dim, r->table_stride, num_cus());
+}
 bf16_t* layer_of(const spec_kv* c, void* pool, int32_t layer) {
   return static_cast<bf16_t*>(pool) + (c->layers > 1 ? layer * c->layer_stride : 0);
 }
@@ -306,7 +309,7 @@ spec_status spec_tree_attn_workspace_bytes(const spec_kv* c, const spec_rows* r,
   if (!bytes) return fail(SPEC_E_INVAL, f, "null result");
   if (const char* w = bad_kv(c)) return fail(SPEC_E_INVAL, f, w);
   if (const char* w = bad_tree_pass(c, r, q_heads)) return fail(SPEC_E_INVAL, f, w);
-  *bytes = kAlign;
+  *bytes = attn_plan(c, r, q_heads).bytes;
   return SPEC_OK;
 }
 
@@ -323,7 +326,8 @@ spec_status spec_tree_attn(const spec_kv* c, int32_t layer, const spec_rows* r, 
   if (!(scale > 0.f && scale <= 0x1p127f)) return fail(SPEC_E_INVAL, f, "scale must be positive and at most 2^127");
   if (!aligned(q, 16) || !aligned(out, 16) || (d_lse && !aligned(d_lse, 4))) return fail(SPEC_E_INVAL, f, "null or misaligned pointer");
   if (!aligned(workspace, kAlign)) return fail(SPEC_E_INVAL, f, "workspace: null or not 256-byte aligned");
-  if (workspace_bytes < kAlign) return fail(SPEC_E_CAPACITY, f, "workspace too small (query spec_tree_attn_workspace_bytes)");
+  const TreeAttnPlan p = attn_plan(c, r, q_heads);
+  if (workspace_bytes < p.bytes) return fail(SPEC_E_CAPACITY, f, "workspace too small (query spec_tree_attn_workspace_bytes)");
   TreeAttnArgs a{};
   a.t = tree_rows(c, r);
   a.kc = layer_of(c, c->k, layer);
@@ -336,7 +340,7 @@ spec_status spec_tree_attn(const spec_kv* c, int32_t layer, const spec_rows* r, 
   a.nq = q_heads;
   a.G = q_heads / c->kv_heads;
   a.scale_log2 = scale * 1.4426950408889634f;
-  return launched(launch_tree_attn(a, c->head_dim, stream), f);
+  return launched(launch_tree_attn(a, p, c->head_dim, workspace, stream), f);
 }
 
 spec_status spec_tree_commit(const spec_kv* c, const spec_rows* r, const int32_t* d_tokens, const int32_t* d_greedy,

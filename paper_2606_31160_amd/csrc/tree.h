@@ -29,6 +29,12 @@ struct AppendArgs {
 };
 hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s);
 
+// A (sequence, kv head, chunk of query rows), as the combine needs it.
+struct TreeUnit {
+  int part, groups;        // its first group's number, how many
+  int first, row, rows, head;   // the sequence's first row; of the kv head's query rows the chunk's first, and all; its first head
+};
+
 struct TreeAttnArgs {
   TreeRows t;
   const bf16_t *kc, *vt;
@@ -39,8 +45,20 @@ struct TreeAttnArgs {
   float* lse;              // [rows][nq] or null
   int nq, G;
   float scale_log2;
+  int target;              // groups of pages aimed at
+  float __attribute__((ext_vector_type(4)))* part;   // [groups][tiles * D / 8][64] outputs of groups
+  float2* ml;              // [groups][32 * tiles] (maximum in log2 units, sum)
+  TreeUnit* units;         // [0].first: how many; then each
 };
-hipError_t launch_tree_attn(const TreeAttnArgs& a, int D, hipStream_t s);
+// How a call is laid out, and its workspace: part, ml, units.
+struct TreeAttnPlan {
+  int tiles;               // of 32 query rows of a kv head that a workgroup has
+  int units, target, grid;
+  bool combine;            // a sequence may have several groups
+  size_t ml, unit, bytes;
+};
+TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu);
+hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void* workspace, hipStream_t s);
 
 struct TreeCommitArgs {
   TreeRows t;

@@ -2,15 +2,14 @@
 // paged cache, attention of the rows over it, and the commit of the accepted paths.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device.h"
 #include "tree.h"
 
 namespace specdec {
 
 namespace {
-
-constexpr int kWords = (SPEC_MAX_ROWS + 63) / 64;   // of a row's ancestors
-constexpr float kAbove = 24.f;
 
 __device__ __forceinline__ void flag(const TreeRows& t) {
   if (t.err) *t.err = SPEC_E_INVAL;
@@ -110,76 +109,639 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
       a.vt[((int64_t)page * t.nkv * D + e) * SPEC_KV_PAGE + off] = a.v[(int64_t)r * a.kv_stride + e];
 }
 
-// One workgroup of 4 waves per row and query head; wave w takes pages w, w + 4, ...  A lane has one
-// key of a page, then D / 64 dimensions of the output.
-template <int D>
-__global__ __launch_bounds__(256) void k_tree_attn(TreeAttnArgs a) {
+// ---------------------------------------------------------------------------
+// Attention.  A kv head's query rows r = j G + g of a sequence (pass row j, query head g of the
+// kv head's G) are cut into chunks of 32 NT.  A workgroup of four waves has one chunk and a group of
+// consecutive pages; wave w takes the group's pages w, w + 4, ... on its own, with a running maximum and
+// sum of each row, so that no wave waits for another before the end.  Per page
+//   S^T = K Q^T   (32x32x16 bf16 products, keys down, query rows across)
+//   p = 2^(scale log2e s - m), l += p
+//   O^T += V^T P^T, p as the sum of two bf16 numbers
+// and the waves' (m, l, O) are joined in LDS: the group gives O / L, (m, L) of every row.  One group of a
+// sequence is its result; several are joined by k_tree_combine.
+//
+// A wave's page lies in LDS, its keys and its values each in one buffer, copied there by loads
+// that pass no register: the next page's keys while this one's probabilities meet its values, the next values
+// while the next scores are formed.  The 16-byte chunks of a row are permuted by an xor, so that the eight
+// lanes that an LDS read serves together fall in distinct banks: keys' row r, chunk c at
+// c ^ ((r & 3) + 4 ((r >> 3) & 1)), values' row d at c ^ (d & 7).  Row m of a 32-key score tile is key
+// (m & 3) + 4 ((m >> 3) & 1) + 8 ((m >> 2) & 1) + 16 (m >> 4): a lane's eight scores of a 16-key step are
+// then eight consecutive keys, one 16-byte read of a value row.
+//
+// Masks: pages below the sequence's length are seen whole.  In the others, a lane walks up its row's ancestors and has 64
+// bits, one for each key.  Values of slots that no row sees are taken as zero there.
+//
+// What is not finite.  A value that is not finite (or sums that leave the range, of values near its end)
+// makes a sum that is not finite, which the end of the loop sees; the wave then goes over its pages once more, with
+// such values taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
+// ---------------------------------------------------------------------------
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma32x32x16(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Sum over the lanes up to and including each.
+__device__ __forceinline__ int scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15, rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31, rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+
+// What workgroup i of an attention call does.
+struct Work {
+  int b, kvh, chunk, groups, lo, hi;   // pages [lo, hi) of the sequence's
+  int unit, part;                      // number of the (sequence, kv head, chunk), and of this group among all
+  Seq s;
+};
+
+// Whether there is a workgroup i.  Every (sequence, kv head, chunk) has as many groups, of equal size or one page
+// less, as leave at most `target` workgroups, and no group fewer than kMinPages pages.  The chunks of one group are eight workgroups apart,
+// where its size allows: on one XCD, whose L2 gives its pages to all of them.
+constexpr int kMinPages = 4;
+template <int NT>
+__device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
+  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64;
   const TreeRows& t = a.t;
-  constexpr int P = SPEC_KV_PAGE, U = D / 64;
-  __shared__ float s_q[D], s_p[4][P], s_m[4], s_l[4], s_o[4][D];
-  __shared__ uint64_t s_up[kWords + 1];
-  const int r = blockIdx.x, h = blockIdx.y, kvh = h / a.G;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (!sound(t)) return flag(t);
-  const int b = sequence_of(t, r);
-  if (b < 0) return;
-  const Seq s = sequence(t, b);
-  if (!s.rows) return flag(t);
-  if (threadIdx.x == 0) {
-    for (int i = 0; i <= kWords; ++i) s_up[i] = 0;
-    for (int i = r - s.first; i >= 0; i = parent_of(t, s, i)) s_up[i >> 6] |= 1ull << (i & 63);
-  }
-  for (int d = threadIdx.x; d < D; d += 256) s_q[d] = bf2f(a.q[(int64_t)r * a.q_stride + (int64_t)h * D + d]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o[U] = {};
-  const int end = s.len + s.rows;
-  for (int pg = wave; pg * P < end; pg += 4) {
-    const int page = page_of(t, b, pg * P), slot = pg * P + lane;
-    if (page < 0) {
-      flag(t);
-      continue;
+  const int lane = threadIdx.x & 63;
+  int first[NS], n[NS], len[NS], chunks[NS], pages[NS];
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    first[k] = n[k] = len[k] = chunks[k] = pages[k] = 0;
+    if (64 * k < t.B) {
+      const int b = min(64 * k + lane, t.B - 1);
+      first[k] = t.first[b], n[k] = t.first[b + 1], len[k] = t.len[b];
     }
-    const int i = slot - s.len;
-    const bool see = i < 0 || (i < s.rows && (s_up[i >> 6] >> (i & 63) & 1));
-    const bf16_t* k = a.kc + (((int64_t)page * t.nkv + kvh) * P + lane) * D;
-    float z = 0.f;
-    for (int d = 0; d < D; ++d) z += s_q[d] * bf2f(k[d]);
-    z = see ? z * a.scale_log2 : -INFINITY;
-    float mx = z;
-    for (int x = 32; x; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-    mx = fmaxf(mx + kAbove, m);                    // so that sums of the largest values stay in range
-    const float e = see ? exp2f(z - (mx == -INFINITY ? 0.f : mx)) : 0.f, f = m == -INFINITY ? 0.f : exp2f(m - mx);
-    float sum = e;
-    for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-    l = l * f + sum;
-    m = mx;
-    s_p[wave][lane] = e;
-    const uint64_t seen = __ballot(see);
-    const bf16_t* v = a.vt + ((int64_t)page * t.nkv + kvh) * D * P;
-    for (int u = 0; u < U; ++u) {
-      float acc = isfinite(o[u]) ? o[u] * f : o[u];
-      for (int c = 0; c < P; ++c) {
-        const float x = bf2f(v[(lane + 64 * u) * P + c]);
-        if (seen >> c & 1) acc += isfinite(x) ? s_p[wave][c] * x : x;
+  }
+  bool bad = false, off_table = false;
+  int units = 0;
+  int64_t all = 0;                                  // pages of all units
+  int longest = 0;
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+    if (64 * k < t.B) {
+      const bool in = 64 * k + lane < t.B;
+      bad |= in && (first[k] < 0 || n[k] < first[k] || n[k] > t.rows);
+      const bool off = len[k] < 0 || len[k] > t.stride * SPEC_KV_PAGE;
+      off_table |= in && n[k] > first[k] && (off || len[k] + n[k] - first[k] > t.stride * SPEC_KV_PAGE);
+      n[k] = in && !off ? n[k] - first[k] : 0;
+      chunks[k] = (n[k] * a.G + 32 * NT - 1) / (32 * NT) * t.nkv;   // of all kv heads
+      pages[k] = n[k] ? min((len[k] + n[k] + SPEC_KV_PAGE - 1) / SPEC_KV_PAGE, t.stride) : 0;
+    }
+  bad = __any(bad);
+  if (i == 0 && threadIdx.x < 64 && (bad || off_table)) flag(t);
+  if (bad) {
+    if (i == 0 && threadIdx.x == 0) a.units[0].first = 0;
+    return false;
+  }
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+    if (64 * k < t.B) {
+      units += last_lane(scan(chunks[k]));
+      // (a wave's pages may pass 32 bits together: halves apart)
+      const int64_t x = (int64_t)chunks[k] * pages[k];
+      all += ((int64_t)last_lane(scan((int)(x >> 16))) << 16) + last_lane(scan((int)(x & 0xffff)));
+      int p = pages[k];
+      for (int o = 32; o; o >>= 1) p = max(p, __shfl_xor(p, o));
+      longest = max(longest, p);
+    }
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  if (i == 0 && threadIdx.x == 0) a.units[0].first = units;
+  // pages of a group: the fewest that leave at most `target` groups
+  auto groups_of = [&](int per) {
+    int g = 0;
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+      if (64 * k < t.B) g += last_lane(scan(chunks[k] * ((pages[k] + per - 1) / per)));
+    return g;
+  };
+  int per = max(longest, 1);
+  if (units < a.target) {
+    int lo = (int)max(all / a.target, (int64_t)kMinPages);
+    int hi = (int)min(max(all / (a.target - units) + 1, (int64_t)lo), (int64_t)max(longest, lo));
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (groups_of(mid) <= a.target)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    per = lo;
+  }
+  int at = 0, unit = 0;                             // workgroups and units of the sequences before
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+    if (64 * k < t.B) {
+      const int g = (pages[k] + per - 1) / per, mine = chunks[k] * g;
+      const int ends = at + scan(mine), uends = unit + scan(chunks[k]);
+      if (i >= at && i < last_lane(ends)) {
+        const int l = __builtin_ctzll(__ballot(ends > i));
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        w.b = 64 * k + l;
+        w.s = Seq{of(first[k]), of(n[k]), of(len[k])};
+        w.groups = of(g);
+        const int begin = of(ends) - of(mine), nc = of(chunks[k]) / t.nkv, keys = t.nkv * w.groups;
+        int x = i - begin, key;                     // key: (group, kv head)
+        const int whole = keys / 8 * 8 * nc;
+        if (x < whole) {
+          const int o = x / (8 * nc);
+          x -= o * 8 * nc;
+          w.chunk = x >> 3;
+          key = 8 * o + (x & 7);
+        } else {
+          x -= whole;
+          w.chunk = x / (keys % 8);
+          key = keys / 8 * 8 + x % (keys % 8);
+        }
+        const int group = key / t.nkv, np = of(pages[k]), q = np / w.groups, r = np % w.groups;
+        w.kvh = key % t.nkv;
+        w.lo = group * q + min(group, r);
+        w.hi = w.lo + q + (group < r);
+        w.unit = of(uends) - of(chunks[k]) + w.kvh * nc + w.chunk;
+        w.part = begin + (w.kvh * nc + w.chunk) * w.groups + group;
+        if (group == 0 && threadIdx.x == 0) {
+          TreeUnit u;
+          u.part = begin + (w.kvh * nc + w.chunk) * w.groups;
+          u.groups = w.groups;
+          u.first = w.s.first;
+          u.row = w.chunk * 32 * NT;
+          u.rows = w.s.rows * a.G;
+          u.head = w.kvh * a.G;
+          a.units[1 + w.unit] = u;
+        }
+        return true;
       }
-      o[u] = acc;
+      at = last_lane(ends), unit = last_lane(uends);
+    }
+  return false;
+}
+
+// What a bf16 pair holds that is not finite: 0x8000 in those halves.
+__device__ __forceinline__ uint32_t not_finite16(uint32_t w) {
+  return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+
+// (hi, lo) bf16 pairs whose sums are x and y within 2^-16.
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
+  hi = pack2(x, y);
+  lo = pack2(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+}
+
+__device__ __forceinline__ float other_half(float x) {   // of lane ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// 64 x 16 bytes of a page to LDS: lane l's, `off` bytes into the page and `step` on, to `lds` + 16 l.  Written out, as
+// the compiler would wait for all such loads before every LDS read; a load has no register to write.
+__device__ __forceinline__ void page_to_lds(__amdgpu_buffer_rsrc_t page, uint32_t lds, uint32_t off, uint32_t step) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(page), "s"(step)
+               : "memory");
+}
+// All LDS reads have returned (before their source is overwritten).
+__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void loads_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+template <int D, int NT>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArgs a) {
+  constexpr int P = SPEC_KV_PAGE, DT = D / 32, KS = D / 16, kOp = P * D * 2;   // bytes of a page's keys or values
+  constexpr int kLoads = kOp / 1024;
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ int16_t s_up[SPEC_MAX_ROWS];
+  __shared__ float s_m[4][32 * NT], s_l[4][32 * NT];
+  const TreeRows& t = a.t;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int n32 = lane & 31, half = lane >> 5;
+  Work w;
+  if (!work_of<NT>(a, blockIdx.x, w)) return;
+  const int row0 = w.chunk * 32 * NT, rows = w.s.rows * a.G;
+  const int tail = w.s.len / P;                     // pages from here on are not seen whole
+  const int32_t* const table = t.table + (int64_t)w.b * t.stride;
+  auto page_at = [&](int p) __attribute__((always_inline)) {                       // pool page, or -1
+    const int x = __builtin_amdgcn_readfirstlane(table[p]);
+    return x < t.pages ? max(x, -1) : -1;
+  };
+
+  unsigned char* const kbuf = lds + wave * 2 * kOp;
+  unsigned char* const vbuf = kbuf + kOp;
+  const uint32_t klds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kbuf);
+  // chunk `lane` of 64: keys' row lane / KC (+ 64 / KC a load), values' row lane / 8 (+ 8 a load)
+  constexpr int KC = D / 8;
+  uint32_t koff[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {                     // x: bit 3 of the row
+    const int r = lane / KC;
+    const int f = D == 128 ? (r & 3) + 4 * x : (r & 3);
+    koff[x] = r * D * 2 + ((lane % KC) ^ f) * 16;
+  }
+  const uint32_t voff = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
+  auto resource = [&](const bf16_t* pool, int page) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(pool + ((int64_t)max(page, 0) * t.nkv + w.kvh) * (P * D)), 0, kOp, 0x00020000);
+  };
+  auto load_k = [&](int page) __attribute__((always_inline)) {
+    const auto r = resource(a.kc, page);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      // rows of load i: from 64 / KC i on.  D = 128: 4 i, bit 3 is bit 1 of i.  D = 64: 8 i, bit 3 is bit 0 of i
+      const int x = D == 128 ? (i >> 1) & 1 : i & 1;
+      page_to_lds(r, klds + 1024 * i, D == 128 ? koff[x] : koff[0] ^ (64 * x), 1024 * i);
+    }
+  };
+  auto load_v = [&](int page) __attribute__((always_inline)) {
+    const auto r = resource(a.vt, page);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) page_to_lds(r, klds + kOp + 1024 * i, voff, 1024 * i);
+  };
+
+  int p = w.lo + wave, page = -1, next = -1;
+  auto first_pages = [&]() __attribute__((always_inline)) {
+    if (p < w.hi) {                                 // wave-uniform
+      page = page_at(p);
+      load_k(page);
+      load_v(page);
+      if (p + 4 < w.hi) next = page_at(p + 4);
+    }
+  };
+  first_pages();
+  if (w.hi > tail) {                                // workgroup-uniform
+    for (int j = threadIdx.x; j < w.s.rows; j += 256) s_up[j] = (int16_t)parent_of(t, w.s, j);
+  }
+  // Q operands, of rows that there are
+  u32x4 q[NT][KS];
+  int qj[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = row0 + 32 * nt + n32;
+    qj[nt] = r < rows ? r / a.G : 0;
+    const bf16_t* src = a.q + (int64_t)(w.s.first + qj[nt]) * a.q_stride + (int64_t)(w.kvh * a.G + (r < rows ? r % a.G : 0)) * D + 8 * half;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[nt][k] = ld16(src + 16 * k);
+    if (r >= rows)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[nt][k] = u32x4{0, 0, 0, 0};
+  }
+  __syncthreads();
+
+  // this lane's operand rows in LDS
+  const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
+  const int kswz = (krow & 3) + 4 * ((krow >> 3) & 1);
+  const unsigned char* const kptr = kbuf + krow * D * 2;
+  const unsigned char* const vptr = vbuf + n32 * 128;
+  auto k_operand = [&](int tile, int k) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kptr + tile * 32 * D * 2 + (((2 * k + half) ^ kswz) * 16)); };
+  auto v_operand = [&](int dt, int step) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(vptr + dt * 32 * 128 + (((2 * step + half) ^ (n32 & 7)) * 16)); };
+
+  float m[NT], l[NT];
+  f32x16 o[NT][DT];
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt] = -INFINITY, l[nt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[nt][dt][i] = 0.f;
+    }
+  };
+  clear();
+
+  bool careful = false;
+  float above = 0.f;
+  auto scores = [&](f32x16 (&s)[NT][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const u32x4 x = k_operand(tile, k);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (k == 0)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[nt][tile][i] = 0.f;
+          s[nt][tile] = mfma32x32x16(x, q[nt][k], s[nt][tile]);
+        }
+      }
+  };
+  // probabilities of a page's scores: parts of the keys of step 16 k in ph, pl[k]
+  auto soft = [&](int nt, f32x16 (&s)[2], u32x4 (&ph)[4], u32x4 (&pl)[4]) __attribute__((always_inline)) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+    mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+    // sums follow a maximum only when it has grown by 2^8
+    if (__any(mx > m[nt] + 8.f)) {
+      const float now = fmaxf(m[nt], mx);
+      const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
+      m[nt] = now;
+      l[nt] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = o[nt][dt][i];
+          o[nt][dt][i] = careful && !finite(x) ? x : x * f;
+        }
+    }
+    const float ref = m[nt] == -INFINITY ? 0.f : m[nt] + above;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 8 * (k & 1) + 2 * e;
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][i], a.scale_log2, -ref));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][i + 1], a.scale_log2, -ref));
+        sum += x + y;
+        uint32_t h, g;
+        split2(x, y, h, g);
+        ph[k][e] = h, pl[k][e] = g;
+      }
+    l[nt] += sum;
+  };
+  for (;;) {                                        // once, or twice
+    while (p < w.hi) {
+      const bool more = p + 4 < w.hi;
+      const bool whole = p < tail && page >= 0 && !careful;
+      f32x16 s[NT][2];
+      u32x4 ph[NT][4], pl[NT][4];
+      loads_but<kLoads>();                          // the keys have come
+      scores(s);
+      lds_read();
+      if (more) load_k(next);
+      if (whole) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) soft(nt, s[nt], ph[nt], pl[nt]);
+        if (more)
+          loads_but<kLoads>();                      // the values have come
+        else
+          loads_but<0>();
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const u32x4 x = v_operand(dt, step);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              o[nt][dt] = mfma32x32x16(x, ph[nt][step], o[nt][dt]);
+              o[nt][dt] = mfma32x32x16(x, pl[nt][step], o[nt][dt]);
+            }
+          }
+      } else {
+        // slots of this page below `seen` are everybody's, those from `end` on nobody's
+        const int seen = page < 0 ? 0 : min(max(w.s.len - p * P, 0), P);
+        const int end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * P, P);
+        uint64_t mask[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          uint64_t x = seen >= 64 ? ~0ull : (1ull << seen) - 1;
+          if (page >= 0 && seen < P)
+            for (int i = qj[nt]; i >= 0; i = s_up[i]) {
+              const int at = w.s.len + i - p * P;
+              if (at < 0) break;
+              if (at < P) x |= 1ull << at;
+            }
+          mask[nt] = x >> (8 * half);
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (!(mask[nt] >> (32 * (i >> 4) + 16 * ((i >> 3) & 1) + (i & 7)) & 1)) s[nt][i >> 4][i & 15] = -INFINITY;
+          soft(nt, s[nt], ph[nt], pl[nt]);
+        }
+        if (more)
+          loads_but<kLoads>();
+        else
+          loads_but<0>();
+        uint32_t odd = 0;
+        for (int step = 0; step < 4; ++step) {
+          uint32_t keep[4];
+          const int valid = end - 16 * step - 8 * half;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) keep[e] = (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+          u32x4 h[NT], g[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              h[nt][e] = step & 2 ? (step & 1 ? ph[nt][3][e] : ph[nt][2][e]) : (step & 1 ? ph[nt][1][e] : ph[nt][0][e]);
+              g[nt][e] = step & 2 ? (step & 1 ? pl[nt][3][e] : pl[nt][2][e]) : (step & 1 ? pl[nt][1][e] : pl[nt][0][e]);
+            }
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            u32x4 x = v_operand(dt, step);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[e] &= keep[e];
+              const uint32_t bad = not_finite16(x[e]);
+              odd |= bad;
+              if (careful) x[e] &= ~((bad >> 15) * 0xffffu);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              o[nt][dt] = mfma32x32x16(x, h[nt], o[nt][dt]);
+              o[nt][dt] = mfma32x32x16(x, g[nt], o[nt][dt]);
+            }
+          }
+        }
+        if (careful && __any(odd != 0)) {
+          // how many infinities, negative infinities and NaN of each dimension a row sees: ones of 1, 2^8 and 2^16
+          // against a one for each slot that it sees
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              f32x16 c;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) c[i] = 0.f;
+              for (int step = 0; step < 4; ++step) {
+                u32x4 x = v_operand(dt, step), y;
+                const int valid = end - 16 * step - 8 * half;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+                  uint32_t z = 0;
+                  y[e] = 0;
+#pragma unroll
+                  for (int b = 0; b < 2; ++b) {
+                    const uint32_t v = x[e] >> (16 * b) & 0xffff;
+                    z |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
+                    y[e] |= (mask[nt] >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
+                  }
+                  x[e] = z;
+                }
+                c = mfma32x32x16(x, y, c);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int z = (int)c[i];
+                if (z & 0xff) o[nt][dt][i] += INFINITY;
+                if (z & 0xff00) o[nt][dt][i] -= INFINITY;
+                if (z >> 16) o[nt][dt][i] = NAN;
+              }
+            }
+        }
+        if (page < 0) flag(t);
+      }
+      lds_read();
+      if (more) load_v(next);
+      p += 4;
+      page = next;
+      if (p + 4 < w.hi) next = page_at(p + 4);
+    }
+    bool bad = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float x = 0.f;                                // 0 times what is not finite is NaN
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[nt][dt][i], 0.f, x);
+      bad |= row0 + 32 * nt + n32 < rows && x != 0.f;
+    }
+    if (careful || !__any(bad)) break;
+    careful = true;
+    above = 20.f;
+    clear();
+    p = w.lo + wave;
+    first_pages();
+  }
+
+  // join the waves: each scales its sums by its part of the group's, wave w adds up the w-th quarter
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += other_half(l[nt]);
+    m[nt] += above;
+    if (half == 0) s_m[wave][32 * nt + n32] = m[nt], s_l[wave][32 * nt + n32] = l[nt];
+  }
+  __syncthreads();
+  float M[NT], L[NT];
+  f32x4* const sums = reinterpret_cast<f32x4*>(lds);   // [4][NT][DT][4][64], a wave's in its own pages' place
+  constexpr int Q = NT * DT * 4;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float x[4];
+    M[nt] = -INFINITY, L[nt] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[k] = s_m[k][32 * nt + n32];
+      M[nt] = fmaxf(M[nt], x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (x[k] != -INFINITY) L[nt] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[k] - M[nt]), s_l[k][32 * nt + n32], L[nt]);
+    const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - M[nt]) / L[nt];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = o[nt][dt][4 * i + e];
+          v[e] = finite(y) ? y * f : y;
+        }
+        sums[(wave * Q + (nt * DT + dt) * 4 + i) * 64 + lane] = v;
+      }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < Q / 4; ++k) {
+    const int g = 4 * k + wave, nt = k / DT, dt = k % DT, i = wave;
+    f32x4 v = sums[g * 64 + lane];
+#pragma unroll
+    for (int x = 1; x < 4; ++x) v += sums[(x * Q + g) * 64 + lane];
+    const int r = row0 + 32 * nt + n32;
+    if (r < rows) {
+      if (w.groups == 1) {
+        if (L[nt] == 0.f) v = f32x4{NAN, NAN, NAN, NAN};
+        bf16_t* to = a.out + (int64_t)(w.s.first + qj[nt]) * a.out_stride + (int64_t)(w.kvh * a.G + r % a.G) * D + 32 * dt + 8 * i + 4 * half;
+        *reinterpret_cast<u32x2*>(to) = u32x2{pack2(v.x, v.y), pack2(v.z, v.w)};
+      } else {
+        a.part[((int64_t)w.part * Q + g) * 64 + lane] = v;
+      }
     }
   }
-  if (lane == 0) s_m[wave] = m, s_l[wave] = l;
-  for (int u = 0; u < U; ++u) s_o[wave][lane + 64 * u] = o[u];
+  if (wave == 0 && half == 0)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + 32 * nt + n32;
+      if (r < rows) {
+        if (w.groups > 1)
+          a.ml[(int64_t)w.part * 32 * NT + 32 * nt + n32] = make_float2(M[nt], L[nt]);
+        else if (a.lse)
+          a.lse[(int64_t)(w.s.first + qj[nt]) * a.nq + w.kvh * a.G + r % a.G] = (M[nt] + __builtin_amdgcn_logf(L[nt])) * 0.6931471805599453f;
+      }
+    }
+}
+
+// Joins the groups of a (sequence, kv head, chunk): grid (units, quarters of 32-dimension tiles), four waves, of
+// which wave w takes the groups w, w + 4, ...  A lane has four dimensions of a row, as it wrote them.
+template <int D, int NT>
+__global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
+  constexpr int Q = NT * (D / 32) * 4, U = 4;
+  __shared__ f32x4 s_o[4][64];
+  __shared__ float s_m[4][64], s_a[4][64];
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int n32 = lane & 31, half = lane >> 5, g = blockIdx.y, nt = g / (D / 8), dt = g / 4 % (D / 32), i = g & 3;
+  const int units = a.units[0].first;
+  const TreeUnit u = a.units[1 + blockIdx.x];
+  if ((int)blockIdx.x >= units || u.groups < 2) return;
+  const int r = u.row + 32 * nt + n32;
+  const bool live = r < u.rows;
+  float M = -INFINITY, A = 0.f;                     // maximum and sum of the groups' weights
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = wave; k0 < u.groups; k0 += 4 * U) {
+    f32x4 x[U];
+    float2 ml[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int64_t part = u.part + min(k0 + 4 * k, u.groups - 1);
+      ml[k] = live ? a.ml[part * 32 * NT + 32 * nt + n32] : make_float2(-INFINITY, 0.f);
+      x[k] = live ? a.part[(part * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k0 + 4 * k >= u.groups) ml[k].y = 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (ml[k].y == 0.f) continue;                 // a group without slots that the row sees
+      const float now = fmaxf(M, ml[k].x);
+      const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - now), c = __builtin_amdgcn_exp2f(ml[k].x - now) * ml[k].y;
+      // o stays the average of the groups so far: sums of large values stay in range
+      const float sum = __builtin_fmaf(A, f, c), p = A * f / sum, q = c / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (finite(o[e]) ? o[e] * p : o[e]) + (finite(x[k][e]) ? x[k][e] * q : x[k][e]);
+      A = sum;
+      M = now;
+    }
+  }
+  s_o[wave][lane] = o, s_m[wave][lane] = M, s_a[wave][lane] = A;
   __syncthreads();
-  const float M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float L = 0.f, w[4];
-  for (int i = 0; i < 4; ++i) {
-    w[i] = s_m[i] == -INFINITY ? 0.f : exp2f(s_m[i] - M);
-    L += w[i] * s_l[i];
+  if (wave) return;
+  float mx = -INFINITY, sum = 0.f, c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) mx = fmaxf(mx, s_m[k][lane]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    c[k] = s_m[k][lane] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][lane] - mx) * s_a[k][lane];
+    sum += c[k];
   }
-  for (int d = threadIdx.x; d < D; d += 256) {
-    float x = 0.f;
-    for (int i = 0; i < 4; ++i) x += isfinite(s_o[i][d]) ? s_o[i][d] * (w[i] / L) : s_o[i][d];
-    a.out[(int64_t)r * a.out_stride + (int64_t)h * D + d] = f2bf(L == 0.f ? NAN : x);
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x4 x = s_o[k][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += finite(x[e]) ? x[e] * (c[k] / sum) : x[e];
   }
-  if (a.lse && threadIdx.x == 0) a.lse[(int64_t)r * a.nq + h] = (M - kAbove + log2f(L * 0x1p24f)) * 0.6931471805599453f;
+  if (!live) return;
+  if (sum == 0.f) o = f32x4{NAN, NAN, NAN, NAN};
+  const int j = r / a.G, h = u.head + r % a.G;
+  bf16_t* to = a.out + (int64_t)(u.first + j) * a.out_stride + (int64_t)h * D + 32 * dt + 8 * i + 4 * half;
+  *reinterpret_cast<u32x2*>(to) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
+  if (a.lse && dt == 0 && i == 0 && half == 0) a.lse[(int64_t)(u.first + j) * a.nq + h] = (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // One workgroup of 256 threads per layer, sequence and kv head, and keys or values.  Every
@@ -250,9 +812,45 @@ hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_tree_attn(const TreeAttnArgs& a, int D, hipStream_t s) {
-  hipLaunchKernelGGL(D == 128 ? k_tree_attn<128> : k_tree_attn<64>, dim3(a.t.rows, a.nq), dim3(256), 0, s, a);
+namespace {
+template <int D, int NT>
+hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
+  constexpr int lds = 4 * 2 * SPEC_KV_PAGE * D * 2;
+  static const hipError_t ready =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_tree_attn<D, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  hipLaunchKernelGGL((k_tree_attn<D, NT>), dim3(p.grid), dim3(256), lds, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.combine) return e;
+  hipLaunchKernelGGL((k_tree_combine<D, NT>), dim3(p.units, NT * (D / 8)), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+}  // namespace
+
+TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
+  TreeAttnPlan p;
+  p.tiles = (int64_t)((rows + batch - 1) / batch) * G > 32 ? 2 : 1;
+  const int64_t chunk = 32 * p.tiles;
+  // (every sequence may end inside a chunk)
+  p.units = (int)(nkv * (std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G)));
+  p.target = D == 128 ? ncu : 2 * ncu;
+  p.grid = std::max(p.target, p.units);
+  p.combine = stride > kMinPages;
+  const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8, units = (size_t)(1 + p.units) * sizeof(TreeUnit);
+  p.ml = (part + 255) / 256 * 256;
+  p.unit = p.ml + (ml + 255) / 256 * 256;
+  p.bytes = p.unit + (units + 255) / 256 * 256;
+  return p;
+}
+
+hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void* workspace, hipStream_t s) {
+  char* const w = static_cast<char*>(workspace);
+  a.part = reinterpret_cast<f32x4*>(w);
+  a.ml = reinterpret_cast<float2*>(w + p.ml);
+  a.units = reinterpret_cast<TreeUnit*>(w + p.unit);
+  a.target = p.target;
+  if (D == 128) return p.tiles == 2 ? attn<128, 2>(a, p, s) : attn<128, 1>(a, p, s);
+  return p.tiles == 2 ? attn<64, 2>(a, p, s) : attn<64, 1>(a, p, s);
 }
 
 hipError_t launch_tree_commit(const TreeCommitArgs& a, int D, hipStream_t s) {
