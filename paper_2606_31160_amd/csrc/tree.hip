@@ -26,6 +26,14 @@ __device__ bool sound(const TreeRows& t) {
   return !__any(bad);
 }
 
+// p[i] for an i that all lanes share, by a scalar load: a vector load could not be awaited apart from a wave's
+// loads into LDS.
+__device__ __forceinline__ int shared_at(const int32_t* p, int64_t i) {
+  const uint64_t at = (uint64_t)(p + i);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+  return *(const __attribute__((address_space(4))) int32_t*)((uint64_t)hi << 32 | lo);
+}
+
 struct Seq {
   int first, rows, len;
 };
@@ -142,32 +150,94 @@ __device__ __forceinline__ f32x16 mfma32x32x16(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // Sum over the lanes up to and including each.
-__device__ __forceinline__ int scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15, rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31, rows 2 and 3
+template <class T>
+__device__ __forceinline__ T scan(T x) {
+#define SD_STEP(ctrl, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, false))
+  SD_STEP(0x111, 0xf);                              // row_shr:1, 2, 4, 8
+  SD_STEP(0x112, 0xf);
+  SD_STEP(0x114, 0xf);
+  SD_STEP(0x118, 0xf);
+  SD_STEP(0x142, 0xa);                              // row_bcast:15, rows 1 and 3
+  SD_STEP(0x143, 0xc);                              // row_bcast:31, rows 2 and 3
+#undef SD_STEP
   return x;
 }
-__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+template <class T>
+__device__ __forceinline__ T lane_of(T x, int l) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+}
+template <class T>
+__device__ __forceinline__ T total(T x) {
+  return lane_of(scan(x), 63);
+}
 
 // What workgroup i of an attention call does.
 struct Work {
   int b, kvh, chunk, groups, lo, hi;   // pages [lo, hi) of the sequence's
-  int unit, part;                      // number of the (sequence, kv head, chunk), and of this group among all
+  int part;                            // this group's number
   Seq s;
 };
 
+// Groups of a sequence of so many pages, `per` to a group: one more than needed at most where the division rounds, and
+// the same for every workgroup that asks.
+__device__ __forceinline__ int groups_of(int pages, int per) {
+  return min((int)ceilf((float)pages * __builtin_amdgcn_rcpf((float)per)), pages);
+}
+
+// Workgroup x of a sequence's nc chunks x `groups` groups x nkv kv heads; its unit's first group and unit are numbered from
+// `part` and `unit` on.
+template <int NT>
+__device__ __forceinline__ void work_at(const TreeAttnArgs& a, int x, int nc, int pages, int part, int unit, Work& w) {
+  const int nkv = a.t.nkv, keys = nkv * w.groups;   // key: (group, kv head)
+  const int whole = (keys & ~7) * nc;
+  int key;
+  if (nc == 1) {
+    w.chunk = 0;
+    key = x;
+  } else if (x < whole) {
+    const int o = x / (8 * nc);
+    x -= o * 8 * nc;
+    w.chunk = x >> 3;
+    key = 8 * o + (x & 7);
+  } else {
+    x -= whole;
+    w.chunk = x / (keys & 7);
+    key = (keys & ~7) + x - w.chunk * (keys & 7);
+  }
+  const int group = key / nkv, q = pages / w.groups, r = pages - q * w.groups;
+  w.kvh = key - group * nkv;
+  w.lo = group * q + min(group, r);
+  w.hi = w.lo + q + (group < r);
+  const int u = w.kvh * nc + w.chunk;
+  w.part = part + u * w.groups + group;
+  if (group == 0 && threadIdx.x == 0)
+    a.units[1 + unit + u] = TreeUnit{part + u * w.groups, w.groups, w.s.first, w.chunk * 32 * NT, w.s.rows * a.G, w.kvh * a.G};
+}
+
 // Whether there is a workgroup i.  Every (sequence, kv head, chunk) has as many groups, of equal size or one page
-// less, as leave at most `target` workgroups, and no group fewer than kMinPages pages.  The chunks of one group are eight workgroups apart,
-// where its size allows: on one XCD, whose L2 gives its pages to all of them.
-constexpr int kMinPages = 4;
+// less, as leave at most `target` workgroups, and none fewer than `least` pages.  The chunks of one group are eight
+// workgroups apart, where its size allows: on one XCD, whose L2 gives its pages to all of them.
 template <int NT>
 __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
-  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64;
+  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64, C = 32 * NT;
   const TreeRows& t = a.t;
+  const bool one = i == 0 && threadIdx.x == 0;
+  if (t.B == 1) {                                   // nothing to look up
+    const int first = shared_at(t.first, 0), end = shared_at(t.first, 1), len = shared_at(t.len, 0);
+    const bool bad = first < 0 || end < first || end > t.rows, off = len < 0 || len > t.stride * SPEC_KV_PAGE;
+    const int n = bad || off ? 0 : end - first;
+    if (one && (bad || (off && end > first) || len + n > t.stride * SPEC_KV_PAGE)) flag(t);
+    const int nc = (n * a.G + C - 1) / C, units = nc * t.nkv;
+    const int pages = min((len + n + SPEC_KV_PAGE - 1) / SPEC_KV_PAGE, t.stride);
+    if (one) a.units[0].first = units;
+    if (i >= units && (i >= a.target || units == 0)) return false;
+    w.b = 0;
+    w.s = Seq{first, n, len};
+    w.groups = max(min(groups_of(pages, a.least), a.target / units), 1);
+    if (i >= units * w.groups) return false;
+    work_at<NT>(a, i, nc, pages, 0, 0, w);
+    return true;
+  }
   const int lane = threadIdx.x & 63;
   int first[NS], n[NS], len[NS], chunks[NS], pages[NS];
 #pragma unroll
@@ -179,9 +249,6 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
     }
   }
   bool bad = false, off_table = false;
-  int units = 0;
-  int64_t all = 0;                                  // pages of all units
-  int longest = 0;
 #pragma unroll
   for (int k = 0; k < NS; ++k)
     if (64 * k < t.B) {
@@ -190,93 +257,52 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
       const bool off = len[k] < 0 || len[k] > t.stride * SPEC_KV_PAGE;
       off_table |= in && n[k] > first[k] && (off || len[k] + n[k] - first[k] > t.stride * SPEC_KV_PAGE);
       n[k] = in && !off ? n[k] - first[k] : 0;
-      chunks[k] = (n[k] * a.G + 32 * NT - 1) / (32 * NT) * t.nkv;   // of all kv heads
+      chunks[k] = (n[k] * a.G + C - 1) / C * t.nkv;  // of all kv heads
       pages[k] = n[k] ? min((len[k] + n[k] + SPEC_KV_PAGE - 1) / SPEC_KV_PAGE, t.stride) : 0;
     }
   bad = __any(bad);
   if (i == 0 && threadIdx.x < 64 && (bad || off_table)) flag(t);
   if (bad) {
-    if (i == 0 && threadIdx.x == 0) a.units[0].first = 0;
+    if (one) a.units[0].first = 0;
     return false;
   }
+  int units = 0;
+  float all = 0;                                    // pages of all units
 #pragma unroll
   for (int k = 0; k < NS; ++k)
     if (64 * k < t.B) {
-      units += last_lane(scan(chunks[k]));
-      // (a wave's pages may pass 32 bits together: halves apart)
-      const int64_t x = (int64_t)chunks[k] * pages[k];
-      all += ((int64_t)last_lane(scan((int)(x >> 16))) << 16) + last_lane(scan((int)(x & 0xffff)));
-      int p = pages[k];
-      for (int o = 32; o; o >>= 1) p = max(p, __shfl_xor(p, o));
-      longest = max(longest, p);
+      units += total(chunks[k]);
+      all += total((float)chunks[k] * (float)pages[k]);
     }
-  longest = __builtin_amdgcn_readfirstlane(longest);
-  if (i == 0 && threadIdx.x == 0) a.units[0].first = units;
-  // pages of a group: the fewest that leave at most `target` groups
-  auto groups_of = [&](int per) {
+  if (one) a.units[0].first = units;
+  // pages of a group: from the average on, the first that leaves at most `target` groups
+  int per = max((int)(all / (float)a.target), a.least);
+  if (units >= a.target) per = INT32_MAX / 2;       // one group each
+  while (units < a.target) {
     int g = 0;
 #pragma unroll
     for (int k = 0; k < NS; ++k)
-      if (64 * k < t.B) g += last_lane(scan(chunks[k] * ((pages[k] + per - 1) / per)));
-    return g;
-  };
-  int per = max(longest, 1);
-  if (units < a.target) {
-    int lo = (int)max(all / a.target, (int64_t)kMinPages);
-    int hi = (int)min(max(all / (a.target - units) + 1, (int64_t)lo), (int64_t)max(longest, lo));
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (groups_of(mid) <= a.target)
-        hi = mid;
-      else
-        lo = mid + 1;
-    }
-    per = lo;
+      if (64 * k < t.B) g += total(chunks[k] * groups_of(pages[k], per));
+    if (g <= a.target) break;
+    per += max(per / 16, 1);
   }
   int at = 0, unit = 0;                             // workgroups and units of the sequences before
 #pragma unroll
   for (int k = 0; k < NS; ++k)
     if (64 * k < t.B) {
-      const int g = (pages[k] + per - 1) / per, mine = chunks[k] * g;
+      const int g = groups_of(pages[k], per), mine = chunks[k] * g;
       const int ends = at + scan(mine), uends = unit + scan(chunks[k]);
-      if (i >= at && i < last_lane(ends)) {
+      if (i < lane_of(ends, 63)) {
         const int l = __builtin_ctzll(__ballot(ends > i));
-        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        auto of = [&](int x) { return lane_of(x, l); };
         w.b = 64 * k + l;
         w.s = Seq{of(first[k]), of(n[k]), of(len[k])};
         w.groups = of(g);
-        const int begin = of(ends) - of(mine), nc = of(chunks[k]) / t.nkv, keys = t.nkv * w.groups;
-        int x = i - begin, key;                     // key: (group, kv head)
-        const int whole = keys / 8 * 8 * nc;
-        if (x < whole) {
-          const int o = x / (8 * nc);
-          x -= o * 8 * nc;
-          w.chunk = x >> 3;
-          key = 8 * o + (x & 7);
-        } else {
-          x -= whole;
-          w.chunk = x / (keys % 8);
-          key = keys / 8 * 8 + x % (keys % 8);
-        }
-        const int group = key / t.nkv, np = of(pages[k]), q = np / w.groups, r = np % w.groups;
-        w.kvh = key % t.nkv;
-        w.lo = group * q + min(group, r);
-        w.hi = w.lo + q + (group < r);
-        w.unit = of(uends) - of(chunks[k]) + w.kvh * nc + w.chunk;
-        w.part = begin + (w.kvh * nc + w.chunk) * w.groups + group;
-        if (group == 0 && threadIdx.x == 0) {
-          TreeUnit u;
-          u.part = begin + (w.kvh * nc + w.chunk) * w.groups;
-          u.groups = w.groups;
-          u.first = w.s.first;
-          u.row = w.chunk * 32 * NT;
-          u.rows = w.s.rows * a.G;
-          u.head = w.kvh * a.G;
-          a.units[1 + w.unit] = u;
-        }
+        const int begin = of(ends) - of(mine);
+        work_at<NT>(a, i - begin, of(chunks[k]) / t.nkv, of(pages[k]), begin, of(uends) - of(chunks[k]), w);
         return true;
       }
-      at = last_lane(ends), unit = last_lane(uends);
+      at = lane_of(ends, 63), unit = lane_of(uends, 63);
     }
   return false;
 }
@@ -322,11 +348,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
   const int n32 = lane & 31, half = lane >> 5;
   Work w;
   if (!work_of<NT>(a, blockIdx.x, w)) return;
+  auto shared = [](int& x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };   // known to the compiler only so
+  shared(w.b), shared(w.kvh), shared(w.chunk), shared(w.groups), shared(w.lo), shared(w.hi), shared(w.part);
+  shared(w.s.first), shared(w.s.rows), shared(w.s.len);
   const int row0 = w.chunk * 32 * NT, rows = w.s.rows * a.G;
   const int tail = w.s.len / P;                     // pages from here on are not seen whole
   const int32_t* const table = t.table + (int64_t)w.b * t.stride;
   auto page_at = [&](int p) __attribute__((always_inline)) {                       // pool page, or -1
-    const int x = __builtin_amdgcn_readfirstlane(table[p]);
+    const int x = shared_at(table, p);
     return x < t.pages ? max(x, -1) : -1;
   };
 
@@ -344,7 +373,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
   }
   const uint32_t voff = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
   auto resource = [&](const bf16_t* pool, int page) __attribute__((always_inline)) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(pool + ((int64_t)max(page, 0) * t.nkv + w.kvh) * (P * D)), 0, kOp, 0x00020000);
+    const uint64_t at = (uint64_t)(pool + ((int64_t)max(page, 0) * t.nkv + w.kvh) * (P * D));
+    // (the compiler does not see that it is the same for all lanes)
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, kOp, 0x00020000);
   };
   auto load_k = [&](int page) __attribute__((always_inline)) {
     const auto r = resource(a.kc, page);
@@ -389,6 +421,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
       for (int k = 0; k < KS; ++k) q[nt][k] = u32x4{0, 0, 0, 0};
   }
   __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(q[nt][k]));   // awaited here, not among the loads of the loop
 
   // this lane's operand rows in LDS
   const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
@@ -398,23 +434,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
   auto k_operand = [&](int tile, int k) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kptr + tile * 32 * D * 2 + (((2 * k + half) ^ kswz) * 16)); };
   auto v_operand = [&](int dt, int step) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(vptr + dt * 32 * 128 + (((2 * step + half) ^ (n32 & 7)) * 16)); };
 
-  float m[NT], l[NT];
-  f32x16 o[NT][DT];
-  auto clear = [&]() __attribute__((always_inline)) {
+  float m[NT], l[NT], above = 0.f;
+  f32x16 o[NT][DT], s[NT][2];
+  u32x4 ph[NT][4], pl[NT][4];
+  auto zero = [&](f32x16& x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt] = -INFINITY, l[nt] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[nt][dt][i] = 0.f;
-    }
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
   };
-  clear();
-
-  bool careful = false;
-  float above = 0.f;
-  auto scores = [&](f32x16 (&s)[NT][2]) __attribute__((always_inline)) {
+  auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int tile = 0; tile < 2; ++tile)
 #pragma unroll
@@ -422,32 +449,48 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
         const u32x4 x = k_operand(tile, k);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          if (k == 0)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[nt][tile][i] = 0.f;
+          if (k == 0) zero(s[nt][tile]);
           s[nt][tile] = mfma32x32x16(x, q[nt][k], s[nt][tile]);
         }
       }
   };
-  // probabilities of a page's scores: parts of the keys of step 16 k in ph, pl[k]
-  auto soft = [&](int nt, f32x16 (&s)[2], u32x4 (&ph)[4], u32x4 (&pl)[4]) __attribute__((always_inline)) {
-    float mx = s[0][0];
+  // A page that not every row sees whole: which of its slots row tile nt sees, bit 32 x + 16 y + e this lane's scores 8 y + e of
+  // s[.][x]; slots from `end` on are nobody's.
+  uint64_t mask[NT];
+  int end;
+  auto masks = [&]() __attribute__((always_inline)) {
+    const int seen = page < 0 ? 0 : min(max(w.s.len - p * P, 0), P);   // slots below are everybody's
+    end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * P, P);
 #pragma unroll
-    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+    for (int nt = 0; nt < NT; ++nt) {
+      uint64_t x = seen >= 64 ? ~0ull : (1ull << seen) - 1;
+      if (page >= 0 && seen < P)
+        for (int i = qj[nt]; i >= 0; i = s_up[i]) {
+          const int at = w.s.len + i - p * P;
+          if (at < 0) break;
+          if (at < P) x |= 1ull << at;
+        }
+      mask[nt] = x >> (8 * half);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!(mask[nt] >> (32 * (i >> 4) + 16 * ((i >> 3) & 1) + (i & 7)) & 1)) s[nt][i >> 4][i & 15] = -INFINITY;
+    }
+  };
+  // A row tile's scores to probabilities, the parts of the keys of step 16 k in ph, pl[k]; grow(f) is called where sums have
+  // to follow a maximum: when it has grown by 2^8.
+  auto soft = [&](int nt, auto grow) __attribute__((always_inline)) {
+    float mx = s[nt][0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[nt][i >> 4][i & 15]);
     mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
-    // sums follow a maximum only when it has grown by 2^8
     if (__any(mx > m[nt] + 8.f)) {
       const float now = fmaxf(m[nt], mx);
-      const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
+      const float f = m[nt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[nt] - now);   // (sums are zero yet)
       m[nt] = now;
-      l[nt] *= f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = o[nt][dt][i];
-          o[nt][dt][i] = careful && !finite(x) ? x : x * f;
-        }
+      if (__any(f != 1.f)) {
+        l[nt] *= f;
+        grow(f);
+      }
     }
     const float ref = m[nt] == -INFINITY ? 0.f : m[nt] + above;
     float sum = 0.f;
@@ -456,159 +499,164 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 8 * (k & 1) + 2 * e;
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][i], a.scale_log2, -ref));
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 1][i + 1], a.scale_log2, -ref));
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k >> 1][i], a.scale_log2, -ref));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k >> 1][i + 1], a.scale_log2, -ref));
         sum += x + y;
         uint32_t h, g;
         split2(x, y, h, g);
-        ph[k][e] = h, pl[k][e] = g;
+        ph[nt][k][e] = h, pl[nt][k][e] = g;
       }
     l[nt] += sum;
   };
-  for (;;) {                                        // once, or twice
-    while (p < w.hi) {
-      const bool more = p + 4 < w.hi;
-      const bool whole = p < tail && page >= 0 && !careful;
-      f32x16 s[NT][2];
-      u32x4 ph[NT][4], pl[NT][4];
-      loads_but<kLoads>();                          // the keys have come
-      scores(s);
-      lds_read();
-      if (more) load_k(next);
-      if (whole) {
+
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) soft(nt, s[nt], ph[nt], pl[nt]);
-        if (more)
-          loads_but<kLoads>();                      // the values have come
-        else
-          loads_but<0>();
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = -INFINITY, l[nt] = 0.f;
 #pragma unroll
-        for (int step = 0; step < 4; ++step)
+    for (int dt = 0; dt < DT; ++dt) zero(o[nt][dt]);
+  }
+  while (p < w.hi) {
+    const bool more = p + 4 < w.hi, whole = p < tail && page >= 0;
+    loads_but<kLoads>();                            // the keys have come
+    scores();
+    lds_read();
+    if (more) load_k(next);
+    if (!whole) masks();
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const u32x4 x = v_operand(dt, step);
+    for (int nt = 0; nt < NT; ++nt)
+      soft(nt, [&](float f) __attribute__((always_inline)) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              o[nt][dt] = mfma32x32x16(x, ph[nt][step], o[nt][dt]);
-              o[nt][dt] = mfma32x32x16(x, pl[nt][step], o[nt][dt]);
-            }
-          }
-      } else {
-        // slots of this page below `seen` are everybody's, those from `end` on nobody's
-        const int seen = page < 0 ? 0 : min(max(w.s.len - p * P, 0), P);
-        const int end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * P, P);
-        uint64_t mask[NT];
+        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+      });
+    if (more)
+      loads_but<kLoads>();                          // the values have come
+    else
+      loads_but<0>();
+    if (!whole) {
+      if (page < 0) flag(t);
+      // nobody's slots may hold anything, and zero times that is not zero
+      for (int d = lane; d < D; d += 64)
+        for (int c = end >> 3; c < 8; ++c) {
+          u32x4* const at = reinterpret_cast<u32x4*>(vbuf + d * 128 + ((c ^ (d & 7)) * 16));
+          u32x4 v = *at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] &= (uint32_t)((1ull << (16 * min(max(end - 8 * c - 2 * e, 0), 2))) - 1);
+          *at = v;
+        }
+    }
+#pragma unroll
+    for (int step = 0; step < 4; ++step)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x4 x = v_operand(dt, step);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          uint64_t x = seen >= 64 ? ~0ull : (1ull << seen) - 1;
-          if (page >= 0 && seen < P)
-            for (int i = qj[nt]; i >= 0; i = s_up[i]) {
-              const int at = w.s.len + i - p * P;
-              if (at < 0) break;
-              if (at < P) x |= 1ull << at;
-            }
-          mask[nt] = x >> (8 * half);
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (!(mask[nt] >> (32 * (i >> 4) + 16 * ((i >> 3) & 1) + (i & 7)) & 1)) s[nt][i >> 4][i & 15] = -INFINITY;
-          soft(nt, s[nt], ph[nt], pl[nt]);
+          o[nt][dt] = mfma32x32x16(x, ph[nt][step], o[nt][dt]);
+          o[nt][dt] = mfma32x32x16(x, pl[nt][step], o[nt][dt]);
         }
-        if (more)
-          loads_but<kLoads>();
-        else
-          loads_but<0>();
+      }
+    lds_read();
+    if (more) load_v(next);
+    p += 4;
+    page = next;
+    if (p + 4 < w.hi) next = page_at(p + 4);
+  }
+
+  bool bad = false;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float x = 0.f;                                  // 0 times what is not finite is NaN
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[nt][dt][i], 0.f, x);
+    bad |= row0 + 32 * nt + n32 < rows && x != 0.f;
+  }
+  if (__any(bad)) {
+    // once more, 32 dimensions at a time
+    above = 20.f;
+#pragma unroll 1
+    for (int dt = 0; dt < DT; ++dt) {
+      f32x16 z[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        m[nt] = -INFINITY, l[nt] = 0.f;
+        zero(z[nt]);
+      }
+#pragma unroll 1
+      for (p = w.lo + wave; p < w.hi; p += 4) {
+        page = page_at(p);
+        load_k(page);
+        load_v(page);
+        loads_but<0>();
+        scores();
+        masks();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          soft(nt, [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[nt][i] = finite(z[nt][i]) ? z[nt][i] * f : z[nt][i];
+          });
         uint32_t odd = 0;
+#pragma unroll
         for (int step = 0; step < 4; ++step) {
-          uint32_t keep[4];
+          u32x4 x = v_operand(dt, step), y;
           const int valid = end - 16 * step - 8 * half;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) keep[e] = (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-          u32x4 h[NT], g[NT];
+          for (int e = 0; e < 4; ++e) {
+            x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+            const uint32_t b = not_finite16(x[e]);
+            odd |= b;
+            y[e] = x[e] & ~((b >> 15) * 0xffffu);
+          }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              h[nt][e] = step & 2 ? (step & 1 ? ph[nt][3][e] : ph[nt][2][e]) : (step & 1 ? ph[nt][1][e] : ph[nt][0][e]);
-              g[nt][e] = step & 2 ? (step & 1 ? pl[nt][3][e] : pl[nt][2][e]) : (step & 1 ? pl[nt][1][e] : pl[nt][0][e]);
-            }
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            u32x4 x = v_operand(dt, step);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[e] &= keep[e];
-              const uint32_t bad = not_finite16(x[e]);
-              odd |= bad;
-              if (careful) x[e] &= ~((bad >> 15) * 0xffffu);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              o[nt][dt] = mfma32x32x16(x, h[nt], o[nt][dt]);
-              o[nt][dt] = mfma32x32x16(x, g[nt], o[nt][dt]);
-            }
+          for (int nt = 0; nt < NT; ++nt) {
+            z[nt] = mfma32x32x16(y, ph[nt][step], z[nt]);
+            z[nt] = mfma32x32x16(y, pl[nt][step], z[nt]);
           }
         }
-        if (careful && __any(odd != 0)) {
-          // how many infinities, negative infinities and NaN of each dimension a row sees: ones of 1, 2^8 and 2^16
+        if (__any(odd != 0))
+          // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
           // against a one for each slot that it sees
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x16 c;
+            zero(c);
+#pragma unroll 1
+            for (int step = 0; step < 4; ++step) {
+              u32x4 x = v_operand(dt, step), y;
+              const int valid = end - 16 * step - 8 * half;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              f32x16 c;
+              for (int e = 0; e < 4; ++e) {
+                x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+                uint32_t k = 0;
+                y[e] = 0;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) c[i] = 0.f;
-              for (int step = 0; step < 4; ++step) {
-                u32x4 x = v_operand(dt, step), y;
-                const int valid = end - 16 * step - 8 * half;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-                  uint32_t z = 0;
-                  y[e] = 0;
-#pragma unroll
-                  for (int b = 0; b < 2; ++b) {
-                    const uint32_t v = x[e] >> (16 * b) & 0xffff;
-                    z |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
-                    y[e] |= (mask[nt] >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
-                  }
-                  x[e] = z;
+                for (int b = 0; b < 2; ++b) {
+                  const uint32_t v = x[e] >> (16 * b) & 0xffff;
+                  k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
+                  y[e] |= (mask[nt] >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
                 }
-                c = mfma32x32x16(x, y, c);
+                x[e] = k;
               }
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int z = (int)c[i];
-                if (z & 0xff) o[nt][dt][i] += INFINITY;
-                if (z & 0xff00) o[nt][dt][i] -= INFINITY;
-                if (z >> 16) o[nt][dt][i] = NAN;
-              }
+              c = mfma32x32x16(x, y, c);
             }
-        }
-        if (page < 0) flag(t);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int k = (int)c[i];
+              if (k & 0xff) z[nt][i] += INFINITY;
+              if (k & 0xff00) z[nt][i] -= INFINITY;
+              if (k >> 16) z[nt][i] = NAN;
+            }
+          }
+        lds_read();
       }
-      lds_read();
-      if (more) load_v(next);
-      p += 4;
-      page = next;
-      if (p + 4 < w.hi) next = page_at(p + 4);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (d == dt)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[nt][d] = z[nt];
     }
-    bool bad = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float x = 0.f;                                // 0 times what is not finite is NaN
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[nt][dt][i], 0.f, x);
-      bad |= row0 + 32 * nt + n32 < rows && x != 0.f;
-    }
-    if (careful || !__any(bad)) break;
-    careful = true;
-    above = 20.f;
-    clear();
-    p = w.lo + wave;
-    first_pages();
   }
 
   // join the waves: each scales its sums by its part of the group's, wave w adds up the w-th quarter
@@ -827,6 +875,9 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
 }
 }  // namespace
 
+// Pages of a group at least: one for each wave; of short tables one group, which needs no second kernel.
+constexpr int kLeastPages = 4, kOneGroup = 8;
+
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
   p.tiles = (int64_t)((rows + batch - 1) / batch) * G > 32 ? 2 : 1;
@@ -835,7 +886,8 @@ TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stri
   p.units = (int)(nkv * (std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G)));
   p.target = D == 128 ? ncu : 2 * ncu;
   p.grid = std::max(p.target, p.units);
-  p.combine = stride > kMinPages;
+  p.least = stride <= kOneGroup ? kOneGroup : kLeastPages;
+  p.combine = stride > p.least;
   const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8, units = (size_t)(1 + p.units) * sizeof(TreeUnit);
   p.ml = (part + 255) / 256 * 256;
   p.unit = p.ml + (ml + 255) / 256 * 256;
@@ -849,6 +901,7 @@ hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void*
   a.ml = reinterpret_cast<float2*>(w + p.ml);
   a.units = reinterpret_cast<TreeUnit*>(w + p.unit);
   a.target = p.target;
+  a.least = p.least;
   if (D == 128) return p.tiles == 2 ? attn<128, 2>(a, p, s) : attn<128, 1>(a, p, s);
   return p.tiles == 2 ? attn<64, 2>(a, p, s) : attn<64, 1>(a, p, s);
 }
