@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "device.h"
 #include "tree.h"
@@ -119,28 +120,28 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 
 // ---------------------------------------------------------------------------
 // Attention.  A kv head's query rows r = j G + g of a sequence (pass row j, query head g of the
-// kv head's G) are cut into chunks of 32 NT.  A workgroup of four waves has one chunk and a group of
-// consecutive pages; wave w takes the group's pages w, w + 4, ... on its own, with a running maximum and
-// sum of each row, so that no wave waits for another before the end.  Per page
+// kv head's G) are cut into chunks of 32.  A workgroup of eight waves has one chunk and a group of
+// consecutive pages; wave w takes the group's half pages (32 slots) w, w + 8, ... on its own, with a running
+// maximum and sum of each row, so that no wave waits for another before the end.  Per half page
 //   S^T = K Q^T   (32x32x16 bf16 products, keys down, query rows across)
 //   p = 2^(scale log2e s - m), l += p
 //   O^T += V^T P^T, p as the sum of two bf16 numbers
 // and the waves' (m, l, O) are joined in LDS: the group gives O / L, (m, L) of every row.  One group of a
 // sequence is its result; several are joined by k_tree_combine.
 //
-// A wave's page lies in LDS, its keys and its values each in one buffer, copied there by loads
-// that pass no register: the next page's keys while this one's probabilities meet its values, the next values
-// while the next scores are formed.  The 16-byte chunks of a row are permuted by an xor, so that the eight
+// A wave's half page lies in LDS, its keys and its values each in one buffer, copied there by loads that pass no
+// register: the next keys while these probabilities meet their values, the next values while the next scores
+// are formed.  The 16-byte chunks of a row are permuted by an xor, so that the eight
 // lanes that an LDS read serves together fall in distinct banks: keys' row r, chunk c at
-// c ^ ((r & 3) + 4 ((r >> 3) & 1)), values' row d at c ^ (d & 7).  Row m of a 32-key score tile is key
+// c ^ ((r & 3) + 4 ((r >> 3) & 1)), values' row d at c ^ ((d >> 1) & 3).  Row m of a score tile is key
 // (m & 3) + 4 ((m >> 3) & 1) + 8 ((m >> 2) & 1) + 16 (m >> 4): a lane's eight scores of a 16-key step are
 // then eight consecutive keys, one 16-byte read of a value row.
 //
-// Masks: pages below the sequence's length are seen whole.  In the others, a lane walks up its row's ancestors and has 64
-// bits, one for each key.  Values of slots that no row sees are taken as zero there.
+// Masks: halves below the sequence's length are seen whole.  In the others, a lane walks up its row's ancestors and
+// has 32 bits, one for each key.  Values of slots that no row sees are set to zero there.
 //
 // What is not finite.  A value that is not finite (or sums that leave the range, of values near its end)
-// makes a sum that is not finite, which the end of the loop sees; the wave then goes over its pages once more, with
+// makes a sum that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with
 // such values taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
 // ---------------------------------------------------------------------------
 
@@ -171,6 +172,8 @@ __device__ __forceinline__ T total(T x) {
   return lane_of(scan(x), 63);
 }
 
+constexpr int kWaves = 8, kTileRows = 32;           // waves of an attention workgroup, its query rows
+
 // What workgroup i of an attention call does.
 struct Work {
   int b, kvh, chunk, groups, lo, hi;   // pages [lo, hi) of the sequence's
@@ -186,7 +189,6 @@ __device__ __forceinline__ int groups_of(int pages, int per) {
 
 // Workgroup x of a sequence's nc chunks x `groups` groups x nkv kv heads; its unit's first group and unit are numbered from
 // `part` and `unit` on.
-template <int NT>
 __device__ __forceinline__ void work_at(const TreeAttnArgs& a, int x, int nc, int pages, int part, int unit, Work& w) {
   const int nkv = a.t.nkv, keys = nkv * w.groups;   // key: (group, kv head)
   const int whole = (keys & ~7) * nc;
@@ -211,15 +213,14 @@ __device__ __forceinline__ void work_at(const TreeAttnArgs& a, int x, int nc, in
   const int u = w.kvh * nc + w.chunk;
   w.part = part + u * w.groups + group;
   if (group == 0 && threadIdx.x == 0)
-    a.units[1 + unit + u] = TreeUnit{part + u * w.groups, w.groups, w.s.first, w.chunk * 32 * NT, w.s.rows * a.G, w.kvh * a.G};
+    a.units[1 + unit + u] = TreeUnit{part + u * w.groups, w.groups, w.s.first, w.chunk * kTileRows, w.s.rows * a.G, w.kvh * a.G};
 }
 
 // Whether there is a workgroup i.  Every (sequence, kv head, chunk) has as many groups, of equal size or one page
 // less, as leave at most `target` workgroups, and none fewer than `least` pages.  The chunks of one group are eight
 // workgroups apart, where its size allows: on one XCD, whose L2 gives its pages to all of them.
-template <int NT>
 __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
-  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64, C = 32 * NT;
+  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64, C = kTileRows;
   const TreeRows& t = a.t;
   const bool one = i == 0 && threadIdx.x == 0;
   if (t.B == 1) {                                   // nothing to look up
@@ -235,7 +236,7 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
     w.s = Seq{first, n, len};
     w.groups = max(min(groups_of(pages, a.least), a.target / units), 1);
     if (i >= units * w.groups) return false;
-    work_at<NT>(a, i, nc, pages, 0, 0, w);
+    work_at(a, i, nc, pages, 0, 0, w);
     return true;
   }
   const int lane = threadIdx.x & 63;
@@ -299,7 +300,7 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
         w.s = Seq{of(first[k]), of(n[k]), of(len[k])};
         w.groups = of(g);
         const int begin = of(ends) - of(mine);
-        work_at<NT>(a, i - begin, of(chunks[k]) / t.nkv, of(pages[k]), begin, of(uends) - of(chunks[k]), w);
+        work_at(a, i - begin, of(chunks[k]) / t.nkv, of(pages[k]), begin, of(uends) - of(chunks[k]), w);
         return true;
       }
       at = lane_of(ends, 63), unit = lane_of(uends, 63);
@@ -325,209 +326,192 @@ __device__ __forceinline__ float other_half(float x) {   // of lane ^ 32
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// 64 x 16 bytes of a page to LDS: lane l's, `off` bytes into the page and `step` on, to `lds` + 16 l.  Written out, as
-// the compiler would wait for all such loads before every LDS read; a load has no register to write.
-__device__ __forceinline__ void page_to_lds(__amdgpu_buffer_rsrc_t page, uint32_t lds, uint32_t off, uint32_t step) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(off), "s"(page), "s"(step)
-               : "memory");
+// 4 KB of a page, from byte `step` on, to `lds`: lane l's 16 bytes of the i-th KB to 1024 i + 16 l, from an offset o0 .. o3 of its
+// own in that KB.  Written out, as the compiler would wait for all such loads before every LDS read; a load
+// has no register to write.  (An instruction's offset counts at both ends.)
+__device__ __forceinline__ void page_to_lds(__amdgpu_buffer_rsrc_t page, uint32_t lds, uint32_t step, uint32_t o0, uint32_t o1, uint32_t o2,
+                                            uint32_t o3) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "buffer_load_dwordx4 %3, %1, %2 offen lds\n\t"
+      "buffer_load_dwordx4 %4, %1, %2 offen offset:1024 lds\n\t"
+      "buffer_load_dwordx4 %5, %1, %2 offen offset:2048 lds\n\t"
+      "buffer_load_dwordx4 %6, %1, %2 offen offset:3072 lds"
+      ::"s"(lds), "s"(page), "s"(step), "v"(o0), "v"(o1), "v"(o2), "v"(o3)
+      : "memory");
 }
 // All LDS reads have returned (before their source is overwritten).
 __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void loads_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <int D, int NT>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArgs a) {
-  constexpr int P = SPEC_KV_PAGE, DT = D / 32, KS = D / 16, kOp = P * D * 2;   // bytes of a page's keys or values
-  constexpr int kLoads = kOp / 1024;
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
+  constexpr int DT = D / 32, KS = D / 16, H = 32, kHalf = H * D * 2;   // slots of a step, bytes of its keys or values
+  constexpr int kLoads = kHalf / 1024, KC = D / 8;
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ int16_t s_up[SPEC_MAX_ROWS];
-  __shared__ float s_m[4][32 * NT], s_l[4][32 * NT];
+  __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
   const TreeRows& t = a.t;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int n32 = lane & 31, half = lane >> 5;
   Work w;
-  if (!work_of<NT>(a, blockIdx.x, w)) return;
+  if (!work_of(a, blockIdx.x, w)) return;
   auto shared = [](int& x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };   // known to the compiler only so
   shared(w.b), shared(w.kvh), shared(w.chunk), shared(w.groups), shared(w.lo), shared(w.hi), shared(w.part);
   shared(w.s.first), shared(w.s.rows), shared(w.s.len);
-  const int row0 = w.chunk * 32 * NT, rows = w.s.rows * a.G;
-  const int tail = w.s.len / P;                     // pages from here on are not seen whole
+  const int row0 = w.chunk * kTileRows, rows = w.s.rows * a.G;
+  const int last = min(2 * w.hi, (w.s.len + w.s.rows + H - 1) / H), tail = w.s.len / H;   // halves: the group's end; seen whole before
   const int32_t* const table = t.table + (int64_t)w.b * t.stride;
-  auto page_at = [&](int p) __attribute__((always_inline)) {                       // pool page, or -1
-    const int x = shared_at(table, p);
+  auto page_at = [&](int hp) __attribute__((always_inline)) {   // pool page of a half, or -1
+    const int x = shared_at(table, hp >> 1);
     return x < t.pages ? max(x, -1) : -1;
   };
 
-  unsigned char* const kbuf = lds + wave * 2 * kOp;
-  unsigned char* const vbuf = kbuf + kOp;
+  unsigned char* const kbuf = lds + wave * 2 * kHalf;
+  unsigned char* const vbuf = kbuf + kHalf;
   const uint32_t klds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kbuf);
-  // chunk `lane` of 64: keys' row lane / KC (+ 64 / KC a load), values' row lane / 8 (+ 8 a load)
-  constexpr int KC = D / 8;
-  uint32_t koff[2];
+  // a lane's chunk of each KB: keys' row lane / KC, values' row lane / 4
+  uint32_t koff[2];                                 // by bit 3 of the row
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {                     // x: bit 3 of the row
-    const int r = lane / KC;
-    const int f = D == 128 ? (r & 3) + 4 * x : (r & 3);
-    koff[x] = r * D * 2 + ((lane % KC) ^ f) * 16;
-  }
-  const uint32_t voff = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
+  for (int x = 0; x < 2; ++x) koff[x] = (lane / KC) * D * 2 + ((lane % KC) ^ (((lane / KC) & 3) + 4 * x)) * 16;
+  const uint32_t voff = (lane >> 2) * 128 + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
   auto resource = [&](const bf16_t* pool, int page) __attribute__((always_inline)) {
-    const uint64_t at = (uint64_t)(pool + ((int64_t)max(page, 0) * t.nkv + w.kvh) * (P * D));
+    const uint64_t at = (uint64_t)(pool + ((int64_t)max(page, 0) * t.nkv + w.kvh) * (2 * H * D));
     // (the compiler does not see that it is the same for all lanes)
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, kOp, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, 2 * kHalf, 0x00020000);
   };
+  const int odd_half = wave & 1;                    // (a wave's halves are all first or all second ones)
   auto load_k = [&](int page) __attribute__((always_inline)) {
     const auto r = resource(a.kc, page);
+    // rows from 64 / KC i on in the i-th KB: bit 3 is bit 1 of i where a row is 256 bytes, bit 0 where it is 128
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      // rows of load i: from 64 / KC i on.  D = 128: 4 i, bit 3 is bit 1 of i.  D = 64: 8 i, bit 3 is bit 0 of i
-      const int x = D == 128 ? (i >> 1) & 1 : i & 1;
-      page_to_lds(r, klds + 1024 * i, D == 128 ? koff[x] : koff[0] ^ (64 * x), 1024 * i);
-    }
+    for (int i = 0; i < kLoads; i += 4) page_to_lds(r, klds + 1024 * i, odd_half * kHalf + 1024 * i, koff[0], koff[D == 64], koff[D == 128], koff[1]);
   };
   auto load_v = [&](int page) __attribute__((always_inline)) {
     const auto r = resource(a.vt, page);
+    // 16 rows of 64 bytes a KB, 128 bytes apart in the page
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) page_to_lds(r, klds + kOp + 1024 * i, voff, 1024 * i);
+    for (int i = 0; i < kLoads; i += 4)
+      page_to_lds(r, klds + kHalf + 1024 * i, odd_half * 64 + 2048 * i, voff, voff + 1024, voff + 2048, voff + 3072);
   };
 
-  int p = w.lo + wave, page = -1, next = -1;
-  auto first_pages = [&]() __attribute__((always_inline)) {
-    if (p < w.hi) {                                 // wave-uniform
-      page = page_at(p);
-      load_k(page);
-      load_v(page);
-      if (p + 4 < w.hi) next = page_at(p + 4);
-    }
+  int p = 2 * w.lo + wave, page = -1, next = -1;    // half pages
+  auto first_loads = [&]() __attribute__((always_inline)) {
+    page = page_at(p);
+    load_k(page);
+    load_v(page);
+    if (p + kWaves < last) next = page_at(p + kWaves);
   };
-  first_pages();
-  if (w.hi > tail) {                                // workgroup-uniform
-    for (int j = threadIdx.x; j < w.s.rows; j += 256) s_up[j] = (int16_t)parent_of(t, w.s, j);
-  }
-  // Q operands, of rows that there are
-  u32x4 q[NT][KS];
-  int qj[NT];
+  if (p < last) first_loads();
+  if (last > tail)                                  // workgroup-uniform
+    for (int j = threadIdx.x; j < w.s.rows; j += 64 * kWaves) s_up[j] = (int16_t)parent_of(t, w.s, j);
+  // Q operands, zeros for rows that there are not
+  const int r = row0 + n32, qj = r < rows ? r / a.G : 0, head = w.kvh * a.G + (r < rows ? r % a.G : 0);
+  u32x4 q[KS];
+  {
+    const bf16_t* src = a.q + (int64_t)(w.s.first + qj) * a.q_stride + (int64_t)head * D + 8 * half;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + 32 * nt + n32;
-    qj[nt] = r < rows ? r / a.G : 0;
-    const bf16_t* src = a.q + (int64_t)(w.s.first + qj[nt]) * a.q_stride + (int64_t)(w.kvh * a.G + (r < rows ? r % a.G : 0)) * D + 8 * half;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) q[nt][k] = ld16(src + 16 * k);
+    for (int k = 0; k < KS; ++k) q[k] = ld16(src + 16 * k);
     if (r >= rows)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[nt][k] = u32x4{0, 0, 0, 0};
+      for (int k = 0; k < KS; ++k) q[k] = u32x4{0, 0, 0, 0};
   }
   __syncthreads();
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(q[nt][k]));   // awaited here, not among the loads of the loop
+  for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(q[k]));   // awaited here, not among the loads of the loop
 
   // this lane's operand rows in LDS
   const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
   const int kswz = (krow & 3) + 4 * ((krow >> 3) & 1);
   const unsigned char* const kptr = kbuf + krow * D * 2;
-  const unsigned char* const vptr = vbuf + n32 * 128;
-  auto k_operand = [&](int tile, int k) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kptr + tile * 32 * D * 2 + (((2 * k + half) ^ kswz) * 16)); };
-  auto v_operand = [&](int dt, int step) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(vptr + dt * 32 * 128 + (((2 * step + half) ^ (n32 & 7)) * 16)); };
+  const unsigned char* const vptr = vbuf + n32 * 64;
+  auto k_operand = [&](int k) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kptr + (((2 * k + half) ^ kswz) * 16)); };
+  auto v_operand = [&](int dt, int step) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4*>(vptr + dt * 32 * 64 + (((2 * step + half) ^ ((n32 >> 1) & 3)) * 16));
+  };
 
-  float m[NT], l[NT], above = 0.f;
-  f32x16 o[NT][DT], s[NT][2];
-  u32x4 ph[NT][4], pl[NT][4];
+  float m, l, above = 0.f;
+  f32x16 o[DT], s;
+  u32x4 ph[2], pl[2];
   auto zero = [&](f32x16& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
   };
   auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int tile = 0; tile < 2; ++tile)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 x = k_operand(tile, k);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (k == 0) zero(s[nt][tile]);
-          s[nt][tile] = mfma32x32x16(x, q[nt][k], s[nt][tile]);
-        }
-      }
-  };
-  // A page that not every row sees whole: which of its slots row tile nt sees, bit 32 x + 16 y + e this lane's scores 8 y + e of
-  // s[.][x]; slots from `end` on are nobody's.
-  uint64_t mask[NT];
-  int end;
-  auto masks = [&]() __attribute__((always_inline)) {
-    const int seen = page < 0 ? 0 : min(max(w.s.len - p * P, 0), P);   // slots below are everybody's
-    end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * P, P);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      uint64_t x = seen >= 64 ? ~0ull : (1ull << seen) - 1;
-      if (page >= 0 && seen < P)
-        for (int i = qj[nt]; i >= 0; i = s_up[i]) {
-          const int at = w.s.len + i - p * P;
-          if (at < 0) break;
-          if (at < P) x |= 1ull << at;
-        }
-      mask[nt] = x >> (8 * half);
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (!(mask[nt] >> (32 * (i >> 4) + 16 * ((i >> 3) & 1) + (i & 7)) & 1)) s[nt][i >> 4][i & 15] = -INFINITY;
+    for (int k = 0; k < KS; ++k) {
+      if (k == 0) zero(s);
+      s = mfma32x32x16(k_operand(k), q[k], s);
     }
   };
-  // A row tile's scores to probabilities, the parts of the keys of step 16 k in ph, pl[k]; grow(f) is called where sums have
-  // to follow a maximum: when it has grown by 2^8.
-  auto soft = [&](int nt, auto grow) __attribute__((always_inline)) {
-    float mx = s[nt][0][0];
+  // A half that not every row sees whole: which of its slots the lane's row sees, bit 16 y + e this lane's score 8 y + e; slots
+  // from `end` on are nobody's.
+  uint32_t mask;
+  int end;
+  auto masks = [&]() __attribute__((always_inline)) {
+    const int seen = page < 0 ? 0 : min(max(w.s.len - p * H, 0), H);   // slots below are everybody's
+    end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * H, H);
+    uint32_t x = seen >= H ? ~0u : (1u << seen) - 1;
+    if (page >= 0 && seen < H)
+      for (int i = qj; i >= 0; i = s_up[i]) {
+        const int at = w.s.len + i - p * H;
+        if (at < 0) break;
+        if (at < H) x |= 1u << at;
+      }
+    mask = x >> (8 * half);
 #pragma unroll
-    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[nt][i >> 4][i & 15]);
+    for (int i = 0; i < 16; ++i)
+      if (!(mask >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = -INFINITY;
+  };
+  // Scores to probabilities, the parts of the keys of step 16 k in ph, pl[k]; grow(f) is called where sums have
+  // to follow a maximum: when it has grown by 2^8.
+  auto soft = [&](auto grow) __attribute__((always_inline)) {
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
-    if (__any(mx > m[nt] + 8.f)) {
-      const float now = fmaxf(m[nt], mx);
-      const float f = m[nt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[nt] - now);   // (sums are zero yet)
-      m[nt] = now;
+    if (__any(mx > m + 8.f)) {
+      const float now = fmaxf(m, mx);
+      const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);   // (sums are zero yet)
+      m = now;
       if (__any(f != 1.f)) {
-        l[nt] *= f;
+        l *= f;
         grow(f);
       }
     }
-    const float ref = m[nt] == -INFINITY ? 0.f : m[nt] + above;
+    const float ref = m == -INFINITY ? 0.f : m + above;
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 8 * (k & 1) + 2 * e;
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k >> 1][i], a.scale_log2, -ref));
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k >> 1][i + 1], a.scale_log2, -ref));
+        const int i = 8 * k + 2 * e;
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -ref));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.scale_log2, -ref));
         sum += x + y;
         uint32_t h, g;
         split2(x, y, h, g);
-        ph[nt][k][e] = h, pl[nt][k][e] = g;
+        ph[k][e] = h, pl[k][e] = g;
       }
-    l[nt] += sum;
+    l += sum;
   };
 
+  m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt] = -INFINITY, l[nt] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) zero(o[nt][dt]);
-  }
-  while (p < w.hi) {
-    const bool more = p + 4 < w.hi, whole = p < tail && page >= 0;
+  for (int dt = 0; dt < DT; ++dt) zero(o[dt]);
+  while (p < last) {
+    const bool more = p + kWaves < last, whole = p < tail && page >= 0;
     loads_but<kLoads>();                            // the keys have come
     scores();
     lds_read();
     if (more) load_k(next);
     if (!whole) masks();
+    soft([&](float f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      soft(nt, [&](float f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
-      });
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+    });
     if (more)
       loads_but<kLoads>();                          // the values have come
     else
@@ -536,8 +520,8 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
       if (page < 0) flag(t);
       // nobody's slots may hold anything, and zero times that is not zero
       for (int d = lane; d < D; d += 64)
-        for (int c = end >> 3; c < 8; ++c) {
-          u32x4* const at = reinterpret_cast<u32x4*>(vbuf + d * 128 + ((c ^ (d & 7)) * 16));
+        for (int c = end >> 3; c < 4; ++c) {
+          u32x4* const at = reinterpret_cast<u32x4*>(vbuf + d * 64 + ((c ^ ((d >> 1) & 3)) * 16));
           u32x4 v = *at;
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] &= (uint32_t)((1ull << (16 * min(max(end - 8 * c - 2 * e, 0), 2))) - 1);
@@ -545,61 +529,49 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
         }
     }
 #pragma unroll
-    for (int step = 0; step < 4; ++step)
+    for (int step = 0; step < 2; ++step)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const u32x4 x = v_operand(dt, step);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          o[nt][dt] = mfma32x32x16(x, ph[nt][step], o[nt][dt]);
-          o[nt][dt] = mfma32x32x16(x, pl[nt][step], o[nt][dt]);
-        }
+        o[dt] = mfma32x32x16(x, ph[step], o[dt]);
+        o[dt] = mfma32x32x16(x, pl[step], o[dt]);
       }
     lds_read();
     if (more) load_v(next);
-    p += 4;
+    p += kWaves;
     page = next;
-    if (p + 4 < w.hi) next = page_at(p + 4);
+    if (p + kWaves < last) next = page_at(p + kWaves);
   }
 
-  bool bad = false;
+  float x0 = 0.f;                                   // 0 times what is not finite is NaN
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float x = 0.f;                                  // 0 times what is not finite is NaN
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[nt][dt][i], 0.f, x);
-    bad |= row0 + 32 * nt + n32 < rows && x != 0.f;
-  }
-  if (__any(bad)) {
+    for (int i = 0; i < 16; ++i) x0 = __builtin_fmaf(o[dt][i], 0.f, x0);
+  const bool slow = __any(r < rows && x0 != 0.f);
+  if (slow) {
     // once more, 32 dimensions at a time
     above = 20.f;
 #pragma unroll 1
     for (int dt = 0; dt < DT; ++dt) {
-      f32x16 z[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = -INFINITY, l[nt] = 0.f;
-        zero(z[nt]);
-      }
+      f32x16 z;
+      m = -INFINITY, l = 0.f;
+      zero(z);
 #pragma unroll 1
-      for (p = w.lo + wave; p < w.hi; p += 4) {
+      for (p = 2 * w.lo + wave; p < last; p += kWaves) {
         page = page_at(p);
         load_k(page);
         load_v(page);
         loads_but<0>();
         scores();
         masks();
+        soft([&](float f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          soft(nt, [&](float f) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[nt][i] = finite(z[nt][i]) ? z[nt][i] * f : z[nt][i];
-          });
+          for (int i = 0; i < 16; ++i) z[i] = finite(z[i]) ? z[i] * f : z[i];
+        });
         uint32_t odd = 0;
 #pragma unroll
-        for (int step = 0; step < 4; ++step) {
+        for (int step = 0; step < 2; ++step) {
           u32x4 x = v_operand(dt, step), y;
           const int valid = end - 16 * step - 8 * half;
 #pragma unroll
@@ -609,137 +581,116 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_tree_attn(TreeAttnArg
             odd |= b;
             y[e] = x[e] & ~((b >> 15) * 0xffffu);
           }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            z[nt] = mfma32x32x16(y, ph[nt][step], z[nt]);
-            z[nt] = mfma32x32x16(y, pl[nt][step], z[nt]);
-          }
+          z = mfma32x32x16(y, ph[step], z);
+          z = mfma32x32x16(y, pl[step], z);
         }
-        if (__any(odd != 0))
+        if (__any(odd != 0)) {
           // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
           // against a one for each slot that it sees
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            f32x16 c;
-            zero(c);
+          f32x16 c;
+          zero(c);
 #pragma unroll 1
-            for (int step = 0; step < 4; ++step) {
-              u32x4 x = v_operand(dt, step), y;
-              const int valid = end - 16 * step - 8 * half;
+          for (int step = 0; step < 2; ++step) {
+            u32x4 x = v_operand(dt, step), y;
+            const int valid = end - 16 * step - 8 * half;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-                uint32_t k = 0;
-                y[e] = 0;
+            for (int e = 0; e < 4; ++e) {
+              x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+              uint32_t k = 0;
+              y[e] = 0;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  const uint32_t v = x[e] >> (16 * b) & 0xffff;
-                  k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
-                  y[e] |= (mask[nt] >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
-                }
-                x[e] = k;
+              for (int b = 0; b < 2; ++b) {
+                const uint32_t v = x[e] >> (16 * b) & 0xffff;
+                k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
+                y[e] |= (mask >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
               }
-              c = mfma32x32x16(x, y, c);
+              x[e] = k;
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int k = (int)c[i];
-              if (k & 0xff) z[nt][i] += INFINITY;
-              if (k & 0xff00) z[nt][i] -= INFINITY;
-              if (k >> 16) z[nt][i] = NAN;
-            }
+            c = mfma32x32x16(x, y, c);
           }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int k = (int)c[i];
+            if (k & 0xff) z[i] += INFINITY;
+            if (k & 0xff00) z[i] -= INFINITY;
+            if (k >> 16) z[i] = NAN;
+          }
+        }
         lds_read();
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        if (d == dt)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) o[nt][d] = z[nt];
+        if (d == dt) o[d] = z;
     }
   }
 
-  // join the waves: each scales its sums by its part of the group's, wave w adds up the w-th quarter
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l[nt] += other_half(l[nt]);
-    m[nt] += above;
-    if (half == 0) s_m[wave][32 * nt + n32] = m[nt], s_l[wave][32 * nt + n32] = l[nt];
-  }
+  // join the waves: each scales its sums by its part of the group's, then wave w adds up the w-th eighth
+  l += other_half(l);
+  m += above;
+  if (half == 0) s_m[wave][n32] = m, s_l[wave][n32] = l;
   __syncthreads();
-  float M[NT], L[NT];
-  f32x4* const sums = reinterpret_cast<f32x4*>(lds);   // [4][NT][DT][4][64], a wave's in its own pages' place
-  constexpr int Q = NT * DT * 4;
+  f32x4* const sums = reinterpret_cast<f32x4*>(lds);   // [waves][DT][4][64], in the place of their pages
+  constexpr int Q = DT * 4;
+  float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float x[4];
-    M[nt] = -INFINITY, L[nt] = 0.f;
+  for (int k = 0; k < kWaves; ++k) M = fmaxf(M, s_m[k][n32]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      x[k] = s_m[k][32 * nt + n32];
-      M[nt] = fmaxf(M[nt], x[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (x[k] != -INFINITY) L[nt] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[k] - M[nt]), s_l[k][32 * nt + n32], L[nt]);
-    const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - M[nt]) / L[nt];
+  for (int k = 0; k < kWaves; ++k) {
+    const float x = s_m[k][n32];
+    L = __builtin_fmaf(x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M), s_l[k][n32], L);
+  }
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;
+  if (slow) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x4 v;
+      for (int i = 0; i < 16; ++i) o[dt][i] = finite(o[dt][i]) ? o[dt][i] * f : o[dt][i];
+  } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = o[nt][dt][4 * i + e];
-          v[e] = finite(y) ? y * f : y;
-        }
-        sums[(wave * Q + (nt * DT + dt) * 4 + i) * 64 + lane] = v;
-      }
+    for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
   }
-  __syncthreads();
 #pragma unroll
-  for (int k = 0; k < Q / 4; ++k) {
-    const int g = 4 * k + wave, nt = k / DT, dt = k % DT, i = wave;
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sums[(wave * Q + dt * 4 + i) * 64 + lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+  __syncthreads();
+  if (r >= rows) return;
+#pragma unroll
+  for (int k = 0; k < Q / kWaves; ++k) {
+    const int g = k * kWaves + wave;
     f32x4 v = sums[g * 64 + lane];
 #pragma unroll
-    for (int x = 1; x < 4; ++x) v += sums[(x * Q + g) * 64 + lane];
-    const int r = row0 + 32 * nt + n32;
-    if (r < rows) {
-      if (w.groups == 1) {
-        if (L[nt] == 0.f) v = f32x4{NAN, NAN, NAN, NAN};
-        bf16_t* to = a.out + (int64_t)(w.s.first + qj[nt]) * a.out_stride + (int64_t)(w.kvh * a.G + r % a.G) * D + 32 * dt + 8 * i + 4 * half;
-        *reinterpret_cast<u32x2*>(to) = u32x2{pack2(v.x, v.y), pack2(v.z, v.w)};
-      } else {
-        a.part[((int64_t)w.part * Q + g) * 64 + lane] = v;
-      }
+    for (int x = 1; x < kWaves; ++x) v += sums[(x * Q + g) * 64 + lane];
+    if (w.groups == 1) {
+      if (L == 0.f) v = f32x4{NAN, NAN, NAN, NAN};
+      bf16_t* to = a.out + (int64_t)(w.s.first + qj) * a.out_stride + (int64_t)head * D + 8 * g + 4 * half;
+      *reinterpret_cast<u32x2*>(to) = u32x2{pack2(v.x, v.y), pack2(v.z, v.w)};
+    } else {
+      a.part[((int64_t)w.part * Q + g) * 64 + lane] = v;
     }
   }
-  if (wave == 0 && half == 0)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = row0 + 32 * nt + n32;
-      if (r < rows) {
-        if (w.groups > 1)
-          a.ml[(int64_t)w.part * 32 * NT + 32 * nt + n32] = make_float2(M[nt], L[nt]);
-        else if (a.lse)
-          a.lse[(int64_t)(w.s.first + qj[nt]) * a.nq + w.kvh * a.G + r % a.G] = (M[nt] + __builtin_amdgcn_logf(L[nt])) * 0.6931471805599453f;
-      }
-    }
+  if (wave == 0 && half == 0) {
+    if (w.groups > 1)
+      a.ml[(int64_t)w.part * kTileRows + n32] = make_float2(M, L);
+    else if (a.lse)
+      a.lse[(int64_t)(w.s.first + qj) * a.nq + head] = (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+  }
 }
 
 // Joins the groups of a (sequence, kv head, chunk): grid (units, quarters of 32-dimension tiles), four waves, of
 // which wave w takes the groups w, w + 4, ...  A lane has four dimensions of a row, as it wrote them.
-template <int D, int NT>
+template <int D>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
-  constexpr int Q = NT * (D / 32) * 4, U = 4;
+  constexpr int Q = D / 8, U = 4;
   __shared__ f32x4 s_o[4][64];
   __shared__ float s_m[4][64], s_a[4][64];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n32 = lane & 31, half = lane >> 5, g = blockIdx.y, nt = g / (D / 8), dt = g / 4 % (D / 32), i = g & 3;
+  const int n32 = lane & 31, half = lane >> 5, g = blockIdx.y;
   const int units = a.units[0].first;
   const TreeUnit u = a.units[1 + blockIdx.x];
   if ((int)blockIdx.x >= units || u.groups < 2) return;
-  const int r = u.row + 32 * nt + n32;
+  const int r = u.row + n32;
   const bool live = r < u.rows;
   float M = -INFINITY, A = 0.f;                     // maximum and sum of the groups' weights
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -749,7 +700,7 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int64_t part = u.part + min(k0 + 4 * k, u.groups - 1);
-      ml[k] = live ? a.ml[part * 32 * NT + 32 * nt + n32] : make_float2(-INFINITY, 0.f);
+      ml[k] = live ? a.ml[part * kTileRows + n32] : make_float2(-INFINITY, 0.f);
       x[k] = live ? a.part[(part * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
       if (k0 + 4 * k >= u.groups) ml[k].y = 0.f;
     }
@@ -787,9 +738,9 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
   if (!live) return;
   if (sum == 0.f) o = f32x4{NAN, NAN, NAN, NAN};
   const int j = r / a.G, h = u.head + r % a.G;
-  bf16_t* to = a.out + (int64_t)(u.first + j) * a.out_stride + (int64_t)h * D + 32 * dt + 8 * i + 4 * half;
+  bf16_t* to = a.out + (int64_t)(u.first + j) * a.out_stride + (int64_t)h * D + 8 * g + 4 * half;
   *reinterpret_cast<u32x2*>(to) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
-  if (a.lse && dt == 0 && i == 0 && half == 0) a.lse[(int64_t)(u.first + j) * a.nq + h] = (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (a.lse && g == 0 && half == 0) a.lse[(int64_t)(u.first + j) * a.nq + h] = (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // One workgroup of 256 threads per layer, sequence and kv head, and keys or values.  Every
@@ -861,34 +812,39 @@ hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s) {
 }
 
 namespace {
-template <int D, int NT>
+template <int D>
 hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
-  constexpr int lds = 4 * 2 * SPEC_KV_PAGE * D * 2;
-  static const hipError_t ready =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_tree_attn<D, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (ready != hipSuccess) return ready;
-  hipLaunchKernelGGL((k_tree_attn<D, NT>), dim3(p.grid), dim3(256), lds, s, a);
+  constexpr int lds = kWaves * 2 * 32 * D * 2;      // half pages
+  static std::atomic<uint64_t> ready{0};            // devices that know of the LDS it needs
+  int dev = 0;
+  if (const hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+  if (dev >= 64 || !(ready >> dev & 1)) {
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&k_tree_attn<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    if (dev < 64) ready |= 1ull << dev;
+  }
+  hipLaunchKernelGGL(k_tree_attn<D>, dim3(p.grid), dim3(64 * kWaves), lds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.combine) return e;
-  hipLaunchKernelGGL((k_tree_combine<D, NT>), dim3(p.units, NT * (D / 8)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_tree_combine<D>, dim3(p.units, D / 8), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 }  // namespace
 
-// Pages of a group at least: one for each wave; of short tables one group, which needs no second kernel.
-constexpr int kLeastPages = 4, kOneGroup = 8;
+// Pages of a group at least: a half for each wave; of short tables one group, which needs no second kernel.
+constexpr int kLeastPages = kWaves / 2, kOneGroup = 8;
 
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
-  p.tiles = (int64_t)((rows + batch - 1) / batch) * G > 32 ? 2 : 1;
-  const int64_t chunk = 32 * p.tiles;
   // (every sequence may end inside a chunk)
-  p.units = (int)(nkv * (std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G)));
-  p.target = D == 128 ? ncu : 2 * ncu;
+  p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + kTileRows - 1) / kTileRows + batch, (int64_t)rows * G));
+  p.target = ncu;
   p.grid = std::max(p.target, p.units);
   p.least = stride <= kOneGroup ? kOneGroup : kLeastPages;
   p.combine = stride > p.least;
-  const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8, units = (size_t)(1 + p.units) * sizeof(TreeUnit);
+  const size_t part = (size_t)p.target * kTileRows * D * 4, ml = (size_t)p.target * kTileRows * 8,
+               units = (size_t)(1 + p.units) * sizeof(TreeUnit);
   p.ml = (part + 255) / 256 * 256;
   p.unit = p.ml + (ml + 255) / 256 * 256;
   p.bytes = p.unit + (units + 255) / 256 * 256;
@@ -902,8 +858,7 @@ hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void*
   a.units = reinterpret_cast<TreeUnit*>(w + p.unit);
   a.target = p.target;
   a.least = p.least;
-  if (D == 128) return p.tiles == 2 ? attn<128, 2>(a, p, s) : attn<128, 1>(a, p, s);
-  return p.tiles == 2 ? attn<64, 2>(a, p, s) : attn<64, 1>(a, p, s);
+  return D == 128 ? attn<128>(a, p, s) : attn<64>(a, p, s);
 }
 
 hipError_t launch_tree_commit(const TreeCommitArgs& a, int D, hipStream_t s) {
