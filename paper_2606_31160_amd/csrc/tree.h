@@ -46,12 +46,13 @@ struct TreeAttnArgs {
   int nq, G;
   float scale_log2;
   int target, least;       // groups aimed at; pages of a group at least
-  float __attribute__((ext_vector_type(4)))* part;   // [groups][D / 8][64] outputs of groups
-  float2* ml;              // [groups][32] (maximum in log2 units, sum)
+  float __attribute__((ext_vector_type(4)))* part;   // [groups][tiles][D / 8][64] outputs of groups
+  float2* ml;              // [groups][tiles][32] (maximum in log2 units, sum)
   TreeUnit* units;         // [0].first: how many; then each
 };
 // How a call is laid out, and its workspace: part, ml, units.
 struct TreeAttnPlan {
+  int tiles;               // of 32 query rows of a kv head that a workgroup has
   int units, target, least, grid;
   bool combine;            // a sequence may have several groups
   size_t ml, unit, bytes;

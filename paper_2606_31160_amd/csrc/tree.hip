@@ -172,7 +172,7 @@ __device__ __forceinline__ T total(T x) {
   return lane_of(scan(x), 63);
 }
 
-constexpr int kWaves = 8, kTileRows = 32;           // waves of an attention workgroup, its query rows
+constexpr int kWaves = 8, kTileRows = 32;           // waves of an attention workgroup, query rows of a wave
 
 // What workgroup i of an attention call does.
 struct Work {
@@ -189,6 +189,7 @@ __device__ __forceinline__ int groups_of(int pages, int per) {
 
 // Workgroup x of a sequence's nc chunks x `groups` groups x nkv kv heads; its unit's first group and unit are numbered from
 // `part` and `unit` on.
+template <int RW>
 __device__ __forceinline__ void work_at(const TreeAttnArgs& a, int x, int nc, int pages, int part, int unit, Work& w) {
   const int nkv = a.t.nkv, keys = nkv * w.groups;   // key: (group, kv head)
   const int whole = (keys & ~7) * nc;
@@ -213,14 +214,15 @@ __device__ __forceinline__ void work_at(const TreeAttnArgs& a, int x, int nc, in
   const int u = w.kvh * nc + w.chunk;
   w.part = part + u * w.groups + group;
   if (group == 0 && threadIdx.x == 0)
-    a.units[1 + unit + u] = TreeUnit{part + u * w.groups, w.groups, w.s.first, w.chunk * kTileRows, w.s.rows * a.G, w.kvh * a.G};
+    a.units[1 + unit + u] = TreeUnit{part + u * w.groups, w.groups, w.s.first, w.chunk * kTileRows * RW, w.s.rows * a.G, w.kvh * a.G};
 }
 
 // Whether there is a workgroup i.  Every (sequence, kv head, chunk) has as many groups, of equal size or one page
 // less, as leave at most `target` workgroups, and none fewer than `least` pages.  The chunks of one group are eight
 // workgroups apart, where its size allows: on one XCD, whose L2 gives its pages to all of them.
+template <int RW>
 __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
-  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64, C = kTileRows;
+  constexpr int NS = (SPEC_MAX_ROWS + 63) / 64, C = kTileRows * RW;
   const TreeRows& t = a.t;
   const bool one = i == 0 && threadIdx.x == 0;
   if (t.B == 1) {                                   // nothing to look up
@@ -236,7 +238,7 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
     w.s = Seq{first, n, len};
     w.groups = max(min(groups_of(pages, a.least), a.target / units), 1);
     if (i >= units * w.groups) return false;
-    work_at(a, i, nc, pages, 0, 0, w);
+    work_at<RW>(a, i, nc, pages, 0, 0, w);
     return true;
   }
   const int lane = threadIdx.x & 63;
@@ -300,7 +302,7 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
         w.s = Seq{of(first[k]), of(n[k]), of(len[k])};
         w.groups = of(g);
         const int begin = of(ends) - of(mine);
-        work_at(a, i - begin, of(chunks[k]) / t.nkv, of(pages[k]), begin, of(uends) - of(chunks[k]), w);
+        work_at<RW>(a, i - begin, of(chunks[k]) / t.nkv, of(pages[k]), begin, of(uends) - of(chunks[k]), w);
         return true;
       }
       at = lane_of(ends, 63), unit = lane_of(uends, 63);
@@ -345,22 +347,22 @@ __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)"
 template <int N>
 __device__ __forceinline__ void loads_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <int D>
+template <int D, int RW>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
-  constexpr int DT = D / 32, KS = D / 16, H = 32, kHalf = H * D * 2;   // slots of a step, bytes of its keys or values
-  constexpr int kLoads = kHalf / 1024, KC = D / 8;
+  constexpr int DT = D / 32, KS = D / 16, H = 32, kHalf = H * D * 2;   // slots of a half, bytes of its keys or values
+  constexpr int kLoads = kHalf / 1024, KC = D / 8, KW = kWaves / RW;   // KW waves share a group's halves
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ int16_t s_up[SPEC_MAX_ROWS];
   __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
   const TreeRows& t = a.t;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n32 = lane & 31, half = lane >> 5;
+  const int kw = wave % KW, rw = wave / KW, n32 = lane & 31, half = lane >> 5;
   Work w;
-  if (!work_of(a, blockIdx.x, w)) return;
+  if (!work_of<RW>(a, blockIdx.x, w)) return;
   auto shared = [](int& x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };   // known to the compiler only so
   shared(w.b), shared(w.kvh), shared(w.chunk), shared(w.groups), shared(w.lo), shared(w.hi), shared(w.part);
   shared(w.s.first), shared(w.s.rows), shared(w.s.len);
-  const int row0 = w.chunk * kTileRows, rows = w.s.rows * a.G;
+  const int row0 = w.chunk * kTileRows * RW + rw * kTileRows, rows = w.s.rows * a.G;
   const int last = min(2 * w.hi, (w.s.len + w.s.rows + H - 1) / H), tail = w.s.len / H;   // halves: the group's end; seen whole before
   const int32_t* const table = t.table + (int64_t)w.b * t.stride;
   auto page_at = [&](int hp) __attribute__((always_inline)) {   // pool page of a half, or -1
@@ -368,9 +370,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
     return x < t.pages ? max(x, -1) : -1;
   };
 
-  unsigned char* const kbuf = lds + wave * 2 * kHalf;
-  unsigned char* const vbuf = kbuf + kHalf;
-  const uint32_t klds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kbuf);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
   // a lane's chunk of each KB: keys' row lane / KC, values' row lane / 4
   uint32_t koff[2];                                 // by bit 3 of the row
 #pragma unroll
@@ -383,28 +383,40 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, 2 * kHalf, 0x00020000);
   };
   const int odd_half = wave & 1;                    // (a wave's halves are all first or all second ones)
-  auto load_k = [&](int page) __attribute__((always_inline)) {
+  auto load_k = [&](int page, int to) __attribute__((always_inline)) {   // to `to` bytes into LDS
     const auto r = resource(a.kc, page);
     // rows from 64 / KC i on in the i-th KB: bit 3 is bit 1 of i where a row is 256 bytes, bit 0 where it is 128
 #pragma unroll
-    for (int i = 0; i < kLoads; i += 4) page_to_lds(r, klds + 1024 * i, odd_half * kHalf + 1024 * i, koff[0], koff[D == 64], koff[D == 128], koff[1]);
+    for (int i = 0; i < kLoads; i += 4)
+      page_to_lds(r, lds0 + to + 1024 * i, odd_half * kHalf + 1024 * i, koff[0], koff[D == 64], koff[D == 128], koff[1]);
   };
-  auto load_v = [&](int page) __attribute__((always_inline)) {
+  auto load_v = [&](int page, int to) __attribute__((always_inline)) {
     const auto r = resource(a.vt, page);
     // 16 rows of 64 bytes a KB, 128 bytes apart in the page
 #pragma unroll
     for (int i = 0; i < kLoads; i += 4)
-      page_to_lds(r, klds + kHalf + 1024 * i, odd_half * 64 + 2048 * i, voff, voff + 1024, voff + 2048, voff + 3072);
+      page_to_lds(r, lds0 + to + 1024 * i, odd_half * 64 + 2048 * i, voff, voff + 1024, voff + 2048, voff + 3072);
   };
-
-  int p = 2 * w.lo + wave, page = -1, next = -1;    // half pages
-  auto first_loads = [&]() __attribute__((always_inline)) {
+  // Buffers of 2 kHalf bytes, keys and then values.  RW = 1: a wave's own one.  RW = 2: two for each kw, which take
+  // turns; wave rw = 0 loads the keys and the other one the values.
+  auto load_both = [&](int page, int to) __attribute__((always_inline)) {
+    if (rw == 0)
+      load_k(page, to);
+    else
+      load_v(page, to + kHalf);
+  };
+  int p = 2 * w.lo + kw, page = -1, next = -1;      // half pages
+  const int mine = 2 * kHalf * (RW == 1 ? wave : 2 * kw);
+  if (p < last) {
     page = page_at(p);
-    load_k(page);
-    load_v(page);
-    if (p + kWaves < last) next = page_at(p + kWaves);
-  };
-  if (p < last) first_loads();
+    if (RW == 1) {
+      load_k(page, mine);
+      load_v(page, mine + kHalf);
+    } else {
+      load_both(page, mine);
+    }
+    if (p + KW < last) next = page_at(p + KW);
+  }
   if (last > tail)                                  // workgroup-uniform
     for (int j = threadIdx.x; j < w.s.rows; j += 64 * kWaves) s_up[j] = (int16_t)parent_of(t, w.s, j);
   // Q operands, zeros for rows that there are not
@@ -425,11 +437,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
   // this lane's operand rows in LDS
   const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
   const int kswz = (krow & 3) + 4 * ((krow >> 3) & 1);
-  const unsigned char* const kptr = kbuf + krow * D * 2;
-  const unsigned char* const vptr = vbuf + n32 * 64;
-  auto k_operand = [&](int k) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kptr + (((2 * k + half) ^ kswz) * 16)); };
-  auto v_operand = [&](int dt, int step) __attribute__((always_inline)) {
-    return *reinterpret_cast<const u32x4*>(vptr + dt * 32 * 64 + (((2 * step + half) ^ ((n32 >> 1) & 3)) * 16));
+  const int kat = krow * D * 2, vat = kHalf + n32 * 64;
+  u32x4 kx[KS], vx[2][DT];
+  auto keys = [&](int from) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kx[k] = *reinterpret_cast<const u32x4*>(lds + from + kat + (((2 * k + half) ^ kswz) * 16));
+  };
+  auto value = [&](int from, int dt, int step) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4*>(lds + from + vat + dt * 32 * 64 + (((2 * step + half) ^ ((n32 >> 1) & 3)) * 16));
   };
 
   float m, l, above = 0.f;
@@ -440,11 +455,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
   };
   auto scores = [&]() __attribute__((always_inline)) {
+    zero(s);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      if (k == 0) zero(s);
-      s = mfma32x32x16(k_operand(k), q[k], s);
-    }
+    for (int k = 0; k < KS; ++k) s = mfma32x32x16(kx[k], q[k], s);
   };
   // A half that not every row sees whole: which of its slots the lane's row sees, bit 16 y + e this lane's score 8 y + e; slots
   // from `end` on are nobody's.
@@ -501,27 +514,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
   m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) zero(o[dt]);
-  while (p < last) {
-    const bool more = p + kWaves < last, whole = p < tail && page >= 0;
-    loads_but<kLoads>();                            // the keys have come
-    scores();
-    lds_read();
-    if (more) load_k(next);
-    if (!whole) masks();
-    soft([&](float f) __attribute__((always_inline)) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
-    });
-    if (more)
-      loads_but<kLoads>();                          // the values have come
-    else
-      loads_but<0>();
+  // of a half in LDS: its values' operands
+  auto values = [&](int from, bool whole) __attribute__((always_inline)) {
     if (!whole) {
       if (page < 0) flag(t);
       // nobody's slots may hold anything, and zero times that is not zero
+      end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * H, H);
       for (int d = lane; d < D; d += 64)
         for (int c = end >> 3; c < 4; ++c) {
-          u32x4* const at = reinterpret_cast<u32x4*>(vbuf + d * 64 + ((c ^ ((d >> 1) & 3)) * 16));
+          u32x4* const at = reinterpret_cast<u32x4*>(lds + from + kHalf + d * 64 + ((c ^ ((d >> 1) & 3)) * 16));
           u32x4 v = *at;
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] &= (uint32_t)((1ull << (16 * min(max(end - 8 * c - 2 * e, 0), 2))) - 1);
@@ -531,16 +532,65 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
 #pragma unroll
     for (int step = 0; step < 2; ++step)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const u32x4 x = v_operand(dt, step);
-        o[dt] = mfma32x32x16(x, ph[step], o[dt]);
-        o[dt] = mfma32x32x16(x, pl[step], o[dt]);
+      for (int dt = 0; dt < DT; ++dt) vx[step][dt] = value(from, dt, step);
+  };
+  auto rest = [&](bool whole) __attribute__((always_inline)) {
+    if (!whole) masks();
+    soft([&](float f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+    });
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(vx[step][dt], ph[step], o[dt]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(vx[step][dt], pl[step], o[dt]);
+    }
+  };
+  if (RW == 1) {
+    while (p < last) {
+      const bool more = p + KW < last, whole = p < tail && page >= 0;
+      loads_but<kLoads>();                          // the keys have come
+      keys(mine);
+      scores();
+      lds_read();
+      if (more) {
+        load_k(next, mine);
+        loads_but<kLoads>();                        // the values have come
+      } else {
+        loads_but<0>();
       }
-    lds_read();
-    if (more) load_v(next);
-    p += kWaves;
-    page = next;
-    if (p + kWaves < last) next = page_at(p + kWaves);
+      values(mine, whole);
+      lds_read();
+      if (more) load_v(next, mine + kHalf);
+      rest(whole);
+      p += KW;
+      page = next;
+      if (p + KW < last) next = page_at(p + KW);
+    }
+  } else {
+    const bool busy = row0 < rows;                  // wave-uniform: the chunk's last tiles may have no rows
+    int at = mine;
+    for (int p0 = 2 * w.lo; p0 < last; p0 += KW) {  // workgroup-uniform
+      const bool whole = p < tail && page >= 0;
+      loads_but<0>();
+      asm volatile("s_barrier" ::: "memory");       // the halves have come, and the other buffers have been read
+      const int other = at ^ 2 * kHalf;
+      if (p + KW < last) load_both(next, other);
+      if (p < last && busy) {
+        keys(at);
+        scores();
+        values(at, whole);
+        rest(whole);
+      }
+      p += KW;
+      page = next;
+      at = other;
+      if (p + KW < last) next = page_at(p + KW);
+      lds_read();
+    }
+    __syncthreads();                                // every buffer has been read
   }
 
   float x0 = 0.f;                                   // 0 times what is not finite is NaN
@@ -558,11 +608,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
       m = -INFINITY, l = 0.f;
       zero(z);
 #pragma unroll 1
-      for (p = 2 * w.lo + wave; p < last; p += kWaves) {
+      for (p = 2 * w.lo + kw; p < last; p += KW) {
         page = page_at(p);
-        load_k(page);
-        load_v(page);
+        load_k(page, 2 * kHalf * wave);
+        load_v(page, 2 * kHalf * wave + kHalf);
         loads_but<0>();
+        keys(2 * kHalf * wave);
         scores();
         masks();
         soft([&](float f) __attribute__((always_inline)) {
@@ -572,7 +623,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
         uint32_t odd = 0;
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
-          u32x4 x = v_operand(dt, step), y;
+          u32x4 x = value(2 * kHalf * wave, dt, step), y;
           const int valid = end - 16 * step - 8 * half;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -591,7 +642,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
           zero(c);
 #pragma unroll 1
           for (int step = 0; step < 2; ++step) {
-            u32x4 x = v_operand(dt, step), y;
+            u32x4 x = value(2 * kHalf * wave, dt, step), y;
             const int valid = end - 16 * step - 8 * half;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -624,7 +675,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
     }
   }
 
-  // join the waves: each scales its sums by its part of the group's, then wave w adds up the w-th eighth
+  // join the waves: each scales its sums by its part of the group's, then each adds up its share
   l += other_half(l);
   m += above;
   if (half == 0) s_m[wave][n32] = m, s_l[wave][n32] = l;
@@ -633,11 +684,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
   constexpr int Q = DT * 4;
   float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) M = fmaxf(M, s_m[k][n32]);
+  for (int k = 0; k < KW; ++k) M = fmaxf(M, s_m[rw * KW + k][n32]);
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
-    const float x = s_m[k][n32];
-    L = __builtin_fmaf(x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M), s_l[k][n32], L);
+  for (int k = 0; k < KW; ++k) {
+    const float x = s_m[rw * KW + k][n32];
+    L = __builtin_fmaf(x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M), s_l[rw * KW + k][n32], L);
   }
   const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;
   if (slow) {
@@ -657,22 +708,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
   __syncthreads();
   if (r >= rows) return;
 #pragma unroll
-  for (int k = 0; k < Q / kWaves; ++k) {
-    const int g = k * kWaves + wave;
-    f32x4 v = sums[g * 64 + lane];
+  for (int k = 0; k < Q / KW; ++k) {
+    const int g = k * KW + kw;
+    f32x4 v = sums[(rw * KW * Q + g) * 64 + lane];
 #pragma unroll
-    for (int x = 1; x < kWaves; ++x) v += sums[(x * Q + g) * 64 + lane];
+    for (int x = 1; x < KW; ++x) v += sums[((rw * KW + x) * Q + g) * 64 + lane];
     if (w.groups == 1) {
       if (L == 0.f) v = f32x4{NAN, NAN, NAN, NAN};
       bf16_t* to = a.out + (int64_t)(w.s.first + qj) * a.out_stride + (int64_t)head * D + 8 * g + 4 * half;
       *reinterpret_cast<u32x2*>(to) = u32x2{pack2(v.x, v.y), pack2(v.z, v.w)};
     } else {
-      a.part[((int64_t)w.part * Q + g) * 64 + lane] = v;
+      a.part[(((int64_t)w.part * RW + rw) * Q + g) * 64 + lane] = v;
     }
   }
-  if (wave == 0 && half == 0) {
+  if (kw == 0 && half == 0) {
     if (w.groups > 1)
-      a.ml[(int64_t)w.part * kTileRows + n32] = make_float2(M, L);
+      a.ml[((int64_t)w.part * RW + rw) * kTileRows + n32] = make_float2(M, L);
     else if (a.lse)
       a.lse[(int64_t)(w.s.first + qj) * a.nq + head] = (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
   }
@@ -680,17 +731,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_tree_attn(TreeAttnArgs a) {
 
 // Joins the groups of a (sequence, kv head, chunk): grid (units, quarters of 32-dimension tiles), four waves, of
 // which wave w takes the groups w, w + 4, ...  A lane has four dimensions of a row, as it wrote them.
-template <int D>
+template <int D, int RW>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
   constexpr int Q = D / 8, U = 4;
   __shared__ f32x4 s_o[4][64];
   __shared__ float s_m[4][64], s_a[4][64];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n32 = lane & 31, half = lane >> 5, g = blockIdx.y;
+  const int n32 = lane & 31, half = lane >> 5, rw = blockIdx.y / Q, g = blockIdx.y % Q;
   const int units = a.units[0].first;
   const TreeUnit u = a.units[1 + blockIdx.x];
   if ((int)blockIdx.x >= units || u.groups < 2) return;
-  const int r = u.row + n32;
+  const int r = u.row + rw * kTileRows + n32;
   const bool live = r < u.rows;
   float M = -INFINITY, A = 0.f;                     // maximum and sum of the groups' weights
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -700,8 +751,8 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int64_t part = u.part + min(k0 + 4 * k, u.groups - 1);
-      ml[k] = live ? a.ml[part * kTileRows + n32] : make_float2(-INFINITY, 0.f);
-      x[k] = live ? a.part[(part * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
+      ml[k] = live ? a.ml[(part * RW + rw) * kTileRows + n32] : make_float2(-INFINITY, 0.f);
+      x[k] = live ? a.part[((part * RW + rw) * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
       if (k0 + 4 * k >= u.groups) ml[k].y = 0.f;
     }
 #pragma unroll
@@ -812,7 +863,7 @@ hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s) {
 }
 
 namespace {
-template <int D>
+template <int D, int RW>
 hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
   constexpr int lds = kWaves * 2 * 32 * D * 2;      // half pages
   static std::atomic<uint64_t> ready{0};            // devices that know of the LDS it needs
@@ -820,14 +871,14 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
   if (const hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
   if (dev >= 64 || !(ready >> dev & 1)) {
     const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(&k_tree_attn<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&k_tree_attn<D, RW>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     if (dev < 64) ready |= 1ull << dev;
   }
-  hipLaunchKernelGGL(k_tree_attn<D>, dim3(p.grid), dim3(64 * kWaves), lds, s, a);
+  hipLaunchKernelGGL((k_tree_attn<D, RW>), dim3(p.grid), dim3(64 * kWaves), lds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.combine) return e;
-  hipLaunchKernelGGL(k_tree_combine<D>, dim3(p.units, D / 8), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_tree_combine<D, RW>), dim3(p.units, RW * (D / 8)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 }  // namespace
@@ -837,13 +888,15 @@ constexpr int kLeastPages = kWaves / 2, kOneGroup = 8;
 
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
+  p.tiles = (int64_t)((rows + batch - 1) / batch) * G > kTileRows ? 2 : 1;
+  const int64_t chunk = kTileRows * p.tiles;
   // (every sequence may end inside a chunk)
-  p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + kTileRows - 1) / kTileRows + batch, (int64_t)rows * G));
+  p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G));
   p.target = ncu;
   p.grid = std::max(p.target, p.units);
   p.least = stride <= kOneGroup ? kOneGroup : kLeastPages;
   p.combine = stride > p.least;
-  const size_t part = (size_t)p.target * kTileRows * D * 4, ml = (size_t)p.target * kTileRows * 8,
+  const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8,
                units = (size_t)(1 + p.units) * sizeof(TreeUnit);
   p.ml = (part + 255) / 256 * 256;
   p.unit = p.ml + (ml + 255) / 256 * 256;
@@ -858,7 +911,8 @@ hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void*
   a.units = reinterpret_cast<TreeUnit*>(w + p.unit);
   a.target = p.target;
   a.least = p.least;
-  return D == 128 ? attn<128>(a, p, s) : attn<64>(a, p, s);
+  if (p.tiles == 2) return D == 128 ? attn<128, 2>(a, p, s) : attn<64, 2>(a, p, s);
+  return D == 128 ? attn<128, 1>(a, p, s) : attn<64, 1>(a, p, s);
 }
 
 hipError_t launch_tree_commit(const TreeCommitArgs& a, int D, hipStream_t s) {
