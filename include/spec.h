@@ -513,7 +513,7 @@ typedef struct spec_rows {
   const int32_t* d_first;    /* [batch + 1] device int32 */
   const int32_t* d_len;      /* [batch] slots in use before the pass */
   const int32_t* d_table;    /* [batch][table_stride]; entries of pages that a call does not touch are not read */
-  int32_t table_stride;      /* 1..2^25 - 1 */
+  int32_t table_stride;      /* 1..2^25 - 16 */
   const int32_t* d_parent;   /* [rows] row of the same sequence (counted from its first) that the row continues, an
                                 earlier one, or -1; NULL: chains, each row continues the one before it */
   int32_t* d_err;            /* device int32 or NULL */
@@ -536,7 +536,8 @@ typedef struct spec_rope {
  *           ancestors (then rows <= SPEC_MAX_ROWS if d_parent is given)
  *   q, k, v bf16 rows of [q_heads] and [kv_heads] x head_dim, 16-byte aligned, q_stride and
  *           kv_stride elements apart (multiples of 8; they may lie in a fused projection)
- * q_heads need not be a multiple of kv_heads; q_heads*head_dim <= 2^20.  Angles are
+ * q_heads need not be a multiple of kv_heads; q_heads*head_dim <= 2^20, q_heads +
+ * 2 kv_heads <= 65535.  Angles are
  * formed in 64 bits, a result is rounded to bf16 once, values are copied as they are. */
 spec_status spec_kv_append(const spec_kv* cache, int32_t layer, const spec_rows* rows, const spec_rope* rope,
                            const int32_t* d_pos, int32_t q_heads, const void* q, int64_t q_stride, const void* k,

@@ -78,7 +78,7 @@ const char* bad_scores(int32_t rows, int32_t vocab, int32_t top) {
   return nullptr;
 }
 
-constexpr int32_t kMaxTable = INT32_MAX / SPEC_KV_PAGE;
+constexpr int32_t kMaxTable = (1 << 25) - 16;   // (slots and a tree's rows behind them fit 32 bits)
 
 // What is wrong with a cache, or with a pass over it, or null.
 const char* bad_kv(const spec_kv* c) {
@@ -276,6 +276,7 @@ spec_status spec_kv_append(const spec_kv* c, int32_t layer, const spec_rows* r, 
   if (sec[0] < 0 || sec[1] < 0 || sec[2] < 0 || (int64_t)sec[0] + sec[1] + sec[2] != half)
     return fail(SPEC_E_INVAL, f, "section must be non-negative and sum to head_dim/2");
   if (q_heads < 0 || (int64_t)q_heads * c->head_dim > (1 << 20)) return fail(SPEC_E_INVAL, f, "q_heads out of range");
+  if (q_heads + 2 * c->kv_heads > 65535) return fail(SPEC_E_INVAL, f, "too many heads");   // a grid's second dimension
   const int64_t width = (int64_t)q_heads * c->head_dim;
   if (q_heads > 0 && (q_stride < width || q_stride % 8 || q_out_stride < width || q_out_stride % 8))
     return fail(SPEC_E_INVAL, f, "q_stride and q_out_stride must be multiples of 8 and at least q_heads*head_dim");
@@ -350,7 +351,6 @@ spec_status spec_tree_commit(const spec_kv* c, const spec_rows* r, const int32_t
   if (const char* w = bad_kv(c)) return fail(SPEC_E_INVAL, f, w);
   if (const char* w = bad_rows(r, SPEC_MAX_ROWS)) return fail(SPEC_E_INVAL, f, w);
   if (stop_token < -1) return fail(SPEC_E_INVAL, f, "stop_token must be -1 or a token");
-  if (c->kv_heads > 32767) return fail(SPEC_E_INVAL, f, "too many kv heads");
   const size_t rows = 4 * (size_t)r->rows, batch = 4 * (size_t)r->batch;
   const struct { const void* p; size_t n; } in[] = {{r->d_first, batch + 4}, {r->d_len, batch}, {r->d_table, batch * r->table_stride},
                                                     {r->d_parent, rows}, {d_tokens, rows}, {d_greedy, rows}, {d_budget, batch}},

@@ -26,8 +26,9 @@ struct AppendArgs {
   const int32_t* pos;      // [3][rows] or null
   int axis_end[2];         // pairs before it are on axis T, before the second on H; interleaved: -1
   double turns[64];        // theta_d / 2 pi
+  int heads;               // that a workgroup rotates
 };
-hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s);
+hipError_t launch_kv_append(AppendArgs& a, int D, hipStream_t s);
 
 // A (sequence, kv head, chunk of query rows), as the combine needs it.
 struct TreeUnit {

@@ -71,51 +71,193 @@ __device__ __forceinline__ int parent_of(const TreeRows& t, const Seq& s, int j)
   return -1;
 }
 
-// One workgroup of 256 threads per row.
+// Sum over the lanes up to and including each.
+template <class T>
+__device__ __forceinline__ T scan(T x) {
+#define SD_STEP(ctrl, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, false))
+  SD_STEP(0x111, 0xf);                              // row_shr:1, 2, 4, 8
+  SD_STEP(0x112, 0xf);
+  SD_STEP(0x114, 0xf);
+  SD_STEP(0x118, 0xf);
+  SD_STEP(0x142, 0xa);                              // row_bcast:15, rows 1 and 3
+  SD_STEP(0x143, 0xc);                              // row_bcast:31, rows 2 and 3
+#undef SD_STEP
+  return x;
+}
+template <class T>
+__device__ __forceinline__ T lane_of(T x, int l) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+}
+template <class T>
+__device__ __forceinline__ T total(T x) {
+  return lane_of(scan(x), 63);
+}
+
+// ---------------------------------------------------------------------------
+// Append.  The rows of a sequence that share a page are a tile.  A workgroup has a tile and either up to `heads` of the
+// heads that are rotated (queries, then keys) or one head of the values.
+//   Rotation: a thread has 8 dimensions of every 2048 / D-th row of the tile, whose 4 angles a row it forms once for all
+// heads: the turn theta_d p / 2 pi in 64 bits, of which the fraction remains, then sine and cosine in 32.
+//   Values: rows through LDS, columns out, 8 slots of a dimension in one store; the ends of a sequence's slots
+// one by one.
+// Bound by memory.
+// ---------------------------------------------------------------------------
+
+// The tile of workgroup x: its sequence, its page's index there.
+__device__ bool tile_of(const TreeRows& t, int x, bool one, Seq& s, int& b, int& index) {
+  const int lane = threadIdx.x & 63;
+  if (!sound(t)) {
+    if (one) flag(t);
+    return false;
+  }
+  int at = 0;
+  for (int b0 = 0; b0 < t.B; b0 += 64) {
+    const int k = min(b0 + lane, t.B - 1);
+    Seq q{t.first[k], t.first[k + 1], t.len[k]};
+    const bool in = b0 + lane < t.B, off = q.len < 0 || q.len > t.stride * SPEC_KV_PAGE;
+    if (one && in && off && q.rows > q.first) flag(t);
+    q.rows = in && !off ? q.rows - q.first : 0;
+    const int begin = q.len / SPEC_KV_PAGE;
+    const int tiles = q.rows > 0 ? (int)(((int64_t)q.len + q.rows - 1) / SPEC_KV_PAGE) - begin + 1 : 0;
+    const int ends = at + scan(tiles);
+    if (x < lane_of(ends, 63)) {
+      const int l = __builtin_ctzll(__ballot(ends > x));
+      b = b0 + l;
+      s = Seq{lane_of(q.first, l), lane_of(q.rows, l), lane_of(q.len, l)};
+      index = lane_of(begin, l) + x - (lane_of(ends, l) - lane_of(tiles, l));
+      return true;
+    }
+    at = lane_of(ends, 63);
+  }
+  return false;
+}
+
 template <int D>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
+  constexpr int P = SPEC_KV_PAGE, C = D / 8, R = 256 / C, U = P / R;   // chunks of a row; rows at once; rows of a thread
+  constexpr int kRow = D / 2 + 1;                   // LDS words of a row: odd, so that 8 rows on is 8 banks on
+  __shared__ uint32_t lds[P * kRow];
+  __shared__ int16_t s_up[SPEC_MAX_ROWS];
   const TreeRows& t = a.t;
-  const int r = blockIdx.x;
-  if (!sound(t)) return flag(t);
-  const int b = sequence_of(t, r);
-  if (b < 0) return;
-  const Seq s = sequence(t, b);
-  if (!s.rows) return flag(t);
-  const int j = r - s.first, slot = s.len + j, page = page_of(t, b, slot), off = slot % SPEC_KV_PAGE;
-  if (page < 0) flag(t);
-  int p[3];
-  if (a.pos) {
-    const int e0 = a.axis_end[0], e1 = a.axis_end[1];   // an axis without pairs is not read
-    p[0] = e0 ? a.pos[r] : 0;
-    p[1] = e0 < 0 || e1 > e0 ? a.pos[t.rows + (int64_t)r] : 0;
-    p[2] = e1 < D / 2 ? a.pos[2 * (int64_t)t.rows + r] : 0;
-  } else {
-    int deep = 0;
-    if (t.parent)
-      for (int i = parent_of(t, s, j); i >= 0; i = parent_of(t, s, i)) ++deep;
-    else
-      deep = j;
-    p[0] = p[1] = p[2] = s.len + deep;
+  const int rotated = a.nq + t.nkv, groups = (rotated + a.heads - 1) / a.heads;
+  const int tid = threadIdx.x, y = blockIdx.y;
+  const bool one = y == 0 && tid < 64;              // the wave that reports
+  Seq s;
+  int b, index;
+  if (!tile_of(t, blockIdx.x, one && blockIdx.x == 0, s, b, index)) return;
+  // the tile's rows [j0, j1) of the sequence, in slots from `off` on
+  const int64_t begin = (int64_t)index * P - s.len;
+  const int j0 = (int)max(begin, (int64_t)0), j1 = (int)min((int64_t)s.rows, begin + P), n = j1 - j0, off = (int)(j0 - begin);
+  int page = index < t.stride ? t.table[(int64_t)b * t.stride + index] : -1;
+  if (page >= t.pages) page = -1;
+  if (page < 0 && one) flag(t);
+  const int c = tid % C, r0 = tid / C;
+
+  if (y >= groups) {                                // values
+    if (page < 0) return;
+    const int h = y - groups;
+    const bf16_t* src = a.v + (int64_t)(s.first + j0) * a.kv_stride + (int64_t)h * D + 8 * c;
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + R * u < n) x[u] = ld16(src + (int64_t)(r0 + R * u) * a.kv_stride);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + R * u < n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds[(off + r0 + R * u) * kRow + 4 * c + e] = x[u][e];
+    __syncthreads();
+    bf16_t* const to = a.vt + ((int64_t)page * t.nkv + h) * D * P;
+    const int c0 = off >> 3, c1 = (off + n - 1) >> 3;
+    if (c0 == 0 && c1 == 7 && n == P) {
+#pragma unroll
+      for (int i = tid; i < D / 2 * 8; i += 256) {
+        const int k = i & 7, d = i >> 3;            // slots 8 k .., dimensions 2 d and 2 d + 1
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = lds[(8 * k + e) * kRow + d];
+        u32x4 lo, hi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x05040100);
+          hi[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x07060302);
+        }
+        *reinterpret_cast<u32x4*>(to + (2 * d) * P + 8 * k) = lo;
+        *reinterpret_cast<u32x4*>(to + (2 * d + 1) * P + 8 * k) = hi;
+      }
+    } else {
+      for (int i = tid; i < n * (D / 2); i += 256) {
+        const int d = i / n, slot = off + i - d * n;
+        const uint32_t w = lds[slot * kRow + d];
+        to[(2 * d) * P + slot] = (bf16_t)w;
+        to[(2 * d + 1) * P + slot] = (bf16_t)(w >> 16);
+      }
+    }
+    return;
   }
-  const int nr = a.nq + t.nkv;
-  for (int e = threadIdx.x; e < nr * (D / 2); e += 256) {
-    const int h = e / (D / 2), d = e % (D / 2);
-    const int axis = a.axis_end[0] < 0 ? d % 3 : (d >= a.axis_end[0]) + (d >= a.axis_end[1]);
-    const double x = a.turns[d] * p[axis];
-    float sn, cs;
-    sincospif(2.f * (float)(x - floor(x)), &sn, &cs);
-    const bf16_t* src = (h < a.nq ? a.q + (int64_t)r * a.q_stride + (int64_t)h * D : a.k + (int64_t)r * a.kv_stride + (int64_t)(h - a.nq) * D) + 2 * d;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(src);
-    const float x0 = __uint_as_float(w << 16), x1 = __uint_as_float(w & 0xffff0000u);
-    const uint32_t y = pack2(x0 * cs - x1 * sn, x0 * sn + x1 * cs);
-    if (h < a.nq)
-      *reinterpret_cast<uint32_t*>(a.q_out + (int64_t)r * a.q_out_stride + (int64_t)h * D + 2 * d) = y;
-    else if (page >= 0)
-      *reinterpret_cast<uint32_t*>(a.kc + (((int64_t)page * t.nkv + h - a.nq) * SPEC_KV_PAGE + off) * D + 2 * d) = y;
+
+  if (!a.pos && t.parent) {                         // workgroup-uniform: rows <= SPEC_MAX_ROWS
+    for (int j = tid; j < s.rows; j += 256) s_up[j] = (int16_t)parent_of(t, s, j);
+    __syncthreads();
   }
-  if (page >= 0)
-    for (int e = threadIdx.x; e < t.nkv * D; e += 256)
-      a.vt[((int64_t)page * t.nkv * D + e) * SPEC_KV_PAGE + off] = a.v[(int64_t)r * a.kv_stride + e];
+  double turns[4];
+  int axis[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int d = 4 * c + k;
+    turns[k] = a.turns[d];
+    axis[k] = a.axis_end[0] < 0 ? d % 3 : (d >= a.axis_end[0]) + (d >= a.axis_end[1]);
+  }
+  float cs[U][4], sn[U][4];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int j = j0 + r0 + R * u;
+    if (j >= j1) continue;
+    double p[3];
+    if (a.pos) {
+      const int e0 = a.axis_end[0], e1 = a.axis_end[1];   // an axis without pairs is not read
+      const int32_t* at = a.pos + s.first + j;
+      p[0] = e0 ? at[0] : 0;
+      p[1] = e0 < 0 || e1 > e0 ? at[t.rows] : 0;
+      p[2] = e1 < D / 2 ? at[2 * (int64_t)t.rows] : 0;
+    } else {
+      int deep = j;
+      if (t.parent) {
+        deep = 0;
+        for (int i = s_up[j]; i >= 0; i = s_up[i]) ++deep;
+      }
+      p[0] = p[1] = p[2] = (double)s.len + deep;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const double x = axis[k] == 0 ? p[0] : axis[k] == 1 ? p[1] : p[2];
+      sincospif(2.f * (float)__builtin_amdgcn_fract(turns[k] * x), &sn[u][k], &cs[u][k]);
+    }
+  }
+  const int h1 = min((y + 1) * a.heads, rotated);
+  for (int h = y * a.heads; h < h1; ++h) {          // workgroup-uniform
+    const bool query = h < a.nq;
+    if (!query && page < 0) break;
+    const bf16_t* src = query ? a.q + (int64_t)(s.first + j0) * a.q_stride + (int64_t)h * D + 8 * c
+                              : a.k + (int64_t)(s.first + j0) * a.kv_stride + (int64_t)(h - a.nq) * D + 8 * c;
+    bf16_t* to = query ? a.q_out + (int64_t)(s.first + j0) * a.q_out_stride + (int64_t)h * D + 8 * c
+                       : a.kc + (((int64_t)page * t.nkv + h - a.nq) * P + off) * D + 8 * c;
+    const int64_t step = query ? a.q_stride : a.kv_stride, step_to = query ? a.q_out_stride : D;
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + R * u < n) x[u] = ld16(src + (r0 + R * u) * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r0 + R * u < n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float e = __uint_as_float(x[u][k] << 16), o = __uint_as_float(x[u][k] & 0xffff0000u);
+          x[u][k] = pack2(e * cs[u][k] - o * sn[u][k], e * sn[u][k] + o * cs[u][k]);
+        }
+        *reinterpret_cast<u32x4*>(to + (r0 + R * u) * step_to) = x[u];
+      }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -148,28 +290,6 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma32x32x16(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Sum over the lanes up to and including each.
-template <class T>
-__device__ __forceinline__ T scan(T x) {
-#define SD_STEP(ctrl, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, false))
-  SD_STEP(0x111, 0xf);                              // row_shr:1, 2, 4, 8
-  SD_STEP(0x112, 0xf);
-  SD_STEP(0x114, 0xf);
-  SD_STEP(0x118, 0xf);
-  SD_STEP(0x142, 0xa);                              // row_bcast:15, rows 1 and 3
-  SD_STEP(0x143, 0xc);                              // row_bcast:31, rows 2 and 3
-#undef SD_STEP
-  return x;
-}
-template <class T>
-__device__ __forceinline__ T lane_of(T x, int l) {
-  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
-}
-template <class T>
-__device__ __forceinline__ T total(T x) {
-  return lane_of(scan(x), 63);
 }
 
 constexpr int kWaves = 8, kTileRows = 32;           // waves of an attention workgroup, query rows of a wave
@@ -794,71 +914,118 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
   if (a.lse && g == 0 && half == 0) a.lse[(int64_t)(u.first + j) * a.nq + h] = (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
-// One workgroup of 256 threads per layer, sequence and kv head, and keys or values.  Every
-// one walks the tree.  The rows move to lower slots only, in their order, 16 at a time: what a
-// step reads lies above everything that earlier ones wrote, and what it overwrites was
-// read by this step or earlier ones, the same dimension by the same wave.
+// ---------------------------------------------------------------------------
+// Commit.  One workgroup per layer, sequence and kv head.  Each wave walks the tree, a lane having every 64th row: the
+// row's children that hold its greedy token by one vote, the lowest of them next.  The rows move to lower slots only, in
+// their order, 16 at a time: what a step reads lies above everything that earlier ones wrote, and what it
+// overwrites was read by this step or earlier ones, the same dimensions by the same wave.  Bound by latency: the chain
+// first rows -> tree -> page table -> slots.
+// ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
+  constexpr int P = SPEC_KV_PAGE, NS = (SPEC_MAX_ROWS + 63) / 64;
   const TreeRows& t = a.t;
-  __shared__ int s_path[SPEC_MAX_ROWS], s_n;
-  const int layer = blockIdx.x, b = blockIdx.y, kvh = blockIdx.z >> 1, tid = threadIdx.x;
-  const bool val = blockIdx.z & 1, first = layer == 0 && blockIdx.z == 0;
+  __shared__ int16_t s_path[4][SPEC_MAX_ROWS];
+  const int layer = blockIdx.x, b = blockIdx.y, kvh = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool first = layer == 0 && kvh == 0 && wave == 0;
+  int16_t* const path = s_path[wave];
   const bool ok = sound(t);
-  const Seq s = ok ? sequence(t, b) : Seq{0, 0, 0};
-  if (!ok || (!s.rows && t.first[b + 1] > t.first[b])) flag(t);
-  if (tid == 0) {
-    const int most = min(s.rows, a.budget ? a.budget[b] : s.rows);
-    int n = 0;
-    for (int j = 0; j >= 0 && n < most;) {
-      s_path[n++] = j;
-      const int want = a.greedy[s.first + j];
-      if (want == a.stop && a.stop != -1) break;
-      int to = -1;
-      for (int i = s.rows - 1; i > j; --i)
-        if (parent_of(t, s, i) == j && a.tokens[s.first + i] == want) to = i;
-      j = to;
+  Seq s = ok ? sequence(t, b) : Seq{0, 0, 0};
+  s.first = __builtin_amdgcn_readfirstlane(s.first), s.rows = __builtin_amdgcn_readfirstlane(s.rows), s.len = __builtin_amdgcn_readfirstlane(s.len);
+  if (first && (!ok || (!s.rows && t.first[b + 1] > t.first[b]))) flag(t);
+  int up[NS], token[NS], greedy[NS];
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    const int j = 64 * k + lane;
+    up[k] = -2, token[k] = greedy[k] = 0;
+    if (j < s.rows) {
+      up[k] = t.parent ? t.parent[s.first + j] : j - 1;
+      token[k] = a.tokens[s.first + j], greedy[k] = a.greedy[s.first + j];
     }
-    s_n = n;
   }
-  __syncthreads();
-  const int n = s_n;
-  if (first) {
-    for (int i = tid; i < n; i += 256) {
-      if (a.path) a.path[s.first + i] = s_path[i];
-      if (a.committed) a.committed[s.first + i] = a.greedy[s.first + s_path[i]];
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    const int j = 64 * k + lane;
+    if (j < s.rows && (up[k] < -1 || up[k] >= j)) {
+      if (first) flag(t);
+      up[k] = -1;
     }
-    if (tid == 0) {
+  }
+  const int most = min(s.rows, a.budget ? __builtin_amdgcn_readfirstlane(a.budget[b]) : s.rows);
+  auto greedy_of = [&](int j) __attribute__((always_inline)) {
+    int x = lane_of(greedy[0], j & 63);
+#pragma unroll
+    for (int k = 1; k < NS; ++k)
+      if (j >= 64 * k) x = lane_of(greedy[k], j & 63);
+    return x;
+  };
+  int n = 0;
+  for (int j = 0; j >= 0 && n < most;) {            // wave-uniform
+    if (lane == 0) path[n] = (int16_t)j;
+    ++n;
+    const int want = greedy_of(j);
+    if (want == a.stop && a.stop != -1) break;
+    int to = -1;
+#pragma unroll
+    for (int k = NS - 1; k >= 0; --k) {
+      const uint64_t fit = __ballot(up[k] == j && token[k] == want && 64 * k + lane < s.rows);
+      if (fit) to = 64 * k + __builtin_ctzll(fit);
+    }
+    j = to;
+  }
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's path is in LDS
+  if (first) {
+    for (int i = lane; i < n; i += 64) {
+      const int j = path[i];
+      if (a.path) a.path[s.first + i] = j;
+      if (a.committed) a.committed[s.first + i] = a.greedy[s.first + j];
+    }
+    if (lane == 0) {
       if (a.n) a.n[b] = n;
       if (a.new_len) a.new_len[b] = t.len[b] + n;
     }
   }
-  bf16_t* pool = (val ? a.vt : a.kc) + layer * a.layer_stride;
-  const int i16 = tid & 15;
+  // step i of 16, and a sixteenth of the dimensions: of keys C consecutive ones, of values every 16th
+  constexpr int C = D / 16;
+  bf16_t *const kc = a.kc + layer * a.layer_stride, *const vt = a.vt + layer * a.layer_stride;
+  const int i16 = tid & 15, d0 = tid >> 4;
   for (int n0 = 0; n0 < n; n0 += 16) {
     const int i = n0 + i16;
-    bool move = i < n && s_path[min(i, n - 1)] != i;
-    int from = 0, to = 0;
-    if (move) {
-      from = s.len + s_path[i], to = s.len + i;
-      const int pf = page_of(t, b, from), pt = page_of(t, b, to);
-      if (pf < 0 || pt < 0) move = false, flag(t);
-      from = from % SPEC_KV_PAGE, to = to % SPEC_KV_PAGE;
-      const int64_t head_f = ((int64_t)pf * t.nkv + kvh) * SPEC_KV_PAGE * D, head_t = ((int64_t)pt * t.nkv + kvh) * SPEC_KV_PAGE * D;
-      bf16_t x[D / 16];
-      const int64_t step = val ? SPEC_KV_PAGE : 1;
-      if (move)
-        for (int u = 0; u < D / 16; ++u) x[u] = pool[head_f + (val ? from : from * D) + ((tid >> 4) + 16 * u) * step];
-      if (move)
-        for (int u = 0; u < D / 16; ++u) pool[head_t + (val ? to : to * D) + ((tid >> 4) + 16 * u) * step] = x[u];
+    if (i >= n || path[i] == i) continue;
+    const int from = s.len + path[i], to = s.len + i;
+    const int pf = page_of(t, b, from), pt = page_of(t, b, to);
+    if (pf < 0 || pt < 0) {
+      flag(t);
+      continue;
     }
+    const int64_t hf = ((int64_t)pf * t.nkv + kvh) * P * D, ht = ((int64_t)pt * t.nkv + kvh) * P * D;
+    const int sf = from % P, st = to % P;
+    uint32_t k[C / 2];
+    bf16_t v[C];
+#pragma unroll
+    for (int u = 0; u < C / 2; ++u) k[u] = reinterpret_cast<const uint32_t*>(kc + hf + sf * D + d0 * C)[u];
+#pragma unroll
+    for (int u = 0; u < C; ++u) v[u] = vt[hf + (d0 + 16 * u) * P + sf];
+#pragma unroll
+    for (int u = 0; u < C / 2; ++u) reinterpret_cast<uint32_t*>(kc + ht + st * D + d0 * C)[u] = k[u];
+#pragma unroll
+    for (int u = 0; u < C; ++u) vt[ht + (d0 + 16 * u) * P + st] = v[u];
   }
 }
 
 }  // namespace
 
-hipError_t launch_kv_append(const AppendArgs& a, int D, hipStream_t s) {
-  hipLaunchKernelGGL(D == 128 ? k_kv_append<128> : k_kv_append<64>, dim3(a.t.rows), dim3(256), 0, s, a);
+hipError_t launch_kv_append(AppendArgs& a, int D, hipStream_t s) {
+  // a tile at least for every sequence and 64 rows; at most two ends more for every sequence
+  const int64_t tiles = (int64_t)a.t.rows / SPEC_KV_PAGE + 2 * std::min(a.t.B, a.t.rows), rotated = a.nq + a.t.nkv;
+  a.heads = (int)std::min<int64_t>(8, std::max<int64_t>(1, tiles * rotated / 1024));
+  const dim3 grid((unsigned)tiles, (unsigned)((rotated + a.heads - 1) / a.heads + a.t.nkv));
+  if (D == 128)
+    hipLaunchKernelGGL(k_kv_append<128>, grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(k_kv_append<64>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -916,7 +1083,7 @@ hipError_t launch_tree_attn(TreeAttnArgs& a, const TreeAttnPlan& p, int D, void*
 }
 
 hipError_t launch_tree_commit(const TreeCommitArgs& a, int D, hipStream_t s) {
-  hipLaunchKernelGGL(D == 128 ? k_tree_commit<128> : k_tree_commit<64>, dim3(a.layers, a.t.B, 2 * a.t.nkv), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(D == 128 ? k_tree_commit<128> : k_tree_commit<64>, dim3(a.layers, a.t.B, a.t.nkv), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -72,7 +72,7 @@ def test_one_layer_needs_no_stride():
 
 @pytest.mark.parametrize("kw,text", [
     (dict(batch=0), "batch"), (dict(batch=161), "batch"), (dict(rows=0), "rows"), (dict(rows=161), "rows"),
-    (dict(table_stride=0), "table_stride"), (dict(table_stride=1 << 25), "table_stride"), (dict(d_first=0), "null"),
+    (dict(table_stride=0), "table_stride"), (dict(table_stride=(1 << 25) - 15), "table_stride"), (dict(d_first=0), "null"),
     (dict(d_len=P + 2), "misaligned"), (dict(d_table=0), "null"), (dict(d_parent=P + 1), "misaligned"), (dict(d_err=P + 2), "misaligned")])
 def test_bad_rows_are_refused(kw, text):
     for f in (lambda r: append(r=r, d_pos=0), lambda r: attn(r=r), lambda r: commit(r=r)):
@@ -124,7 +124,7 @@ def test_attention_refuses_bad_arguments(kw, text):
 
 
 def test_attention_refuses_what_no_grid_holds():
-    r = rows(batch=3, table_stride=(1 << 25) - 1)
+    r = rows(batch=3, table_stride=(1 << 25) - 16)
     refused(lambda: attn(r=r), INVAL, "batch*kv_heads*table_stride")
 
 
@@ -142,5 +142,5 @@ def test_commit_refuses_bad_arguments(kw, text):
     refused(lambda: commit(**kw), INVAL, text)
 
 
-def test_commit_refuses_more_heads_than_a_grid_holds():
-    refused(lambda: commit(cache(kv_heads=40000, layers=1)), INVAL, "kv heads")
+def test_append_refuses_more_heads_than_a_grid_holds():
+    refused(lambda: append(cache(kv_heads=32768, layers=1), kv_stride=1 << 24), INVAL, "too many heads")
