@@ -100,7 +100,9 @@ __device__ __forceinline__ T total(T x) {
 // heads: the turn theta_d p / 2 pi in 64 bits, of which the fraction remains, then sine and cosine in 32.
 //   Values: rows through LDS, columns out, 8 slots of a dimension in one store; the ends of a sequence's slots
 // one by one.
-// Bound by memory.
+// Bound by memory: 4096 rows of 32 + 2 x 8 heads of 128, 100 MB, 22.1 us a call in graphs (4.6 TB/s; a copy of 4 GiB
+// reaches 4.7), 29.1 with outputs left to the caches; 20 thousand rows of 28 + 2 x 4 heads 86.1 and 88.8.  One
+// head a workgroup, which forms every angle anew: 33.6 and 121.
 // ---------------------------------------------------------------------------
 
 // The tile of workgroup x: its sequence, its page's index there.
@@ -132,7 +134,16 @@ __device__ bool tile_of(const TreeRows& t, int x, bool one, Seq& s, int& b, int&
   return false;
 }
 
-template <int D>
+// A long pass streams its outputs past the caches, which its inputs then keep.
+template <bool STREAM>
+__device__ __forceinline__ void store16(bf16_t* to, u32x4 x) {
+  if (STREAM)
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to));
+  else
+    *reinterpret_cast<u32x4*>(to) = x;
+}
+
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   constexpr int P = SPEC_KV_PAGE, C = D / 8, R = 256 / C, U = P / R;   // chunks of a row; rows at once; rows of a thread
   constexpr int kRow = D / 2 + 1;                   // LDS words of a row: odd, so that 8 rows on is 8 banks on
@@ -182,8 +193,8 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
           lo[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x05040100);
           hi[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x07060302);
         }
-        *reinterpret_cast<u32x4*>(to + (2 * d) * P + 8 * k) = lo;
-        *reinterpret_cast<u32x4*>(to + (2 * d + 1) * P + 8 * k) = hi;
+        store16<STREAM>(to + (2 * d) * P + 8 * k, lo);
+        store16<STREAM>(to + (2 * d + 1) * P + 8 * k, hi);
       }
     } else {
       for (int i = tid; i < n * (D / 2); i += 256) {
@@ -255,7 +266,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
           const float e = __uint_as_float(x[u][k] << 16), o = __uint_as_float(x[u][k] & 0xffff0000u);
           x[u][k] = pack2(e * cs[u][k] - o * sn[u][k], e * sn[u][k] + o * cs[u][k]);
         }
-        *reinterpret_cast<u32x4*>(to + (r0 + R * u) * step_to) = x[u];
+        store16<STREAM>(to + (r0 + R * u) * step_to, x[u]);
       }
   }
 }
@@ -1020,12 +1031,14 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
 hipError_t launch_kv_append(AppendArgs& a, int D, hipStream_t s) {
   // a tile at least for every sequence and 64 rows; at most two ends more for every sequence
   const int64_t tiles = (int64_t)a.t.rows / SPEC_KV_PAGE + 2 * std::min(a.t.B, a.t.rows), rotated = a.nq + a.t.nkv;
+  // (more heads share their angles, but leave fewer workgroups: 2 heads here 29.1 us for the 4096 rows, 4 34.3, 8 45.4; for the
+  // 20 thousand 8 heads 88.9, 4 94.2, 1 121)
   a.heads = (int)std::min<int64_t>(8, std::max<int64_t>(1, tiles * rotated / 1024));
   const dim3 grid((unsigned)tiles, (unsigned)((rotated + a.heads - 1) / a.heads + a.t.nkv));
   if (D == 128)
-    hipLaunchKernelGGL(k_kv_append<128>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((a.heads > 1 ? k_kv_append<128, true> : k_kv_append<128, false>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL(k_kv_append<64>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((a.heads > 1 ? k_kv_append<64, true> : k_kv_append<64, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
