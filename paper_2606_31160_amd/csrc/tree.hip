@@ -547,20 +547,29 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   };
   const bool loader = RW == 2 && wave >= kWaves;    // wave-uniform
   // Buffers of 2 kHalf bytes, keys and then values.  RW = 1: a wave's own one.  RW = 2: two for each kw, which take turns.
+  int ids[KW];                                      // a loader's pages of the step to come
+  auto ids_of = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KW; ++k) ids[k] = p0 + k < last ? page_at(p0 + k) : -1;
+  };
   auto load_step = [&](int p0, int turn) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < KW; ++k)
       if (p0 + k < last) {
-        const int page = page_at(p0 + k), to = 2 * kHalf * (2 * k + turn);
+        const int to = 2 * kHalf * (2 * k + turn);
         if (wave == kWaves)
-          load_k(page, to, k & 1);
+          load_k(ids[k], to, k & 1);
         else
-          load_v(page, to, k & 1);
+          load_v(ids[k], to, k & 1);
       }
   };
   int p = 2 * w.lo + kw, page = -1, next = -1;      // half pages
   const int mine = 2 * kHalf * (RW == 1 ? wave : 2 * kw);
-  if (loader) load_step(2 * w.lo, 0);
+  if (loader) {
+    ids_of(2 * w.lo);
+    load_step(2 * w.lo, 0);
+    ids_of(2 * w.lo + KW);
+  }
   if (!loader && p < last) {
     page = page_at(p);
     if (RW == 1) {
@@ -600,7 +609,8 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
       loads_but<0>();
       asm volatile("s_barrier" ::: "memory");       // this step's halves have come, and the last one's have been read
       turn ^= 1;
-      if (p0 + KW < last) load_step(p0 + KW, turn);
+      load_step(p0 + KW, turn);
+      ids_of(p0 + 2 * KW);
     }
     return;
   }
@@ -762,12 +772,12 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     __syncthreads();                                // every buffer has been read
   }
 
-  float x0 = 0.f;                                   // 0 times what is not finite is NaN
+  float x0[4] = {0.f, 0.f, 0.f, 0.f};               // 0 times what is not finite is NaN
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x0 = __builtin_fmaf(o[dt][i], 0.f, x0);
-  const bool slow = __any(r < rows && x0 != 0.f);
+    for (int i = 0; i < 16; ++i) x0[i & 3] = __builtin_fmaf(o[dt][i], 0.f, x0[i & 3]);
+  const bool slow = __any(r < rows && (x0[0] + x0[1]) + (x0[2] + x0[3]) != 0.f);
   if (slow) {
     // once more, 32 dimensions at a time
     above = 20.f;
