@@ -557,7 +557,8 @@ spec_status spec_kv_append(const spec_kv* cache, int32_t layer, const spec_rows*
  *   d_lse   [rows][q_heads] device float, or NULL
  * q_heads is a multiple of kv_heads; q_heads*head_dim <= 2^20; batch*kv_heads*table_stride <= 2^27.
  * Scores, softmax and sums are formed in 32 bits, in an order fixed by the arguments and
- * lengths; p meets the values as the sum of two bf16 numbers, within 2^-16 of itself. */
+ * lengths; p meets the values as the sum of two bf16 numbers, within 2^-16 of itself.  A row
+ * with a score beyond 2^30, or one that is not a number, may be NaN. */
 spec_status spec_tree_attn(const spec_kv* cache, int32_t layer, const spec_rows* rows, int32_t q_heads, const void* q,
                            int64_t q_stride, float scale, void* out, int64_t out_stride, float* d_lse, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);

@@ -45,17 +45,6 @@ __device__ __forceinline__ Seq sequence(const TreeRows& t, int b) {
   return s;
 }
 
-// The sequence of row r, or -1; the whole wave asks, of a pass whose d_first makes sense.
-__device__ int sequence_of(const TreeRows& t, int r) {
-  const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < t.B; b0 += 64) {
-    const int b = b0 + lane;
-    const uint64_t in = __ballot(b < t.B && t.first[min(b, t.B - 1)] <= r && r < t.first[min(b, t.B - 1) + 1]);
-    if (in) return b0 + __builtin_ctzll(in);
-  }
-  return -1;
-}
-
 // The page of a slot, or -1.
 __device__ __forceinline__ int page_of(const TreeRows& t, int b, int slot) {
   const int i = slot / SPEC_KV_PAGE;
@@ -105,19 +94,21 @@ __device__ __forceinline__ T total(T x) {
 // head a workgroup, which forms every angle anew: 33.6 and 121.
 // ---------------------------------------------------------------------------
 
-// The tile of workgroup x: its sequence, its page's index there.
+// The tile of workgroup x: its sequence, its page's index there.  `one` wave reports what is wrong with the pass.
 __device__ bool tile_of(const TreeRows& t, int x, bool one, Seq& s, int& b, int& index) {
   const int lane = threadIdx.x & 63;
   if (!sound(t)) {
     if (one) flag(t);
     return false;
   }
+  if (one)
+    for (int k = lane; k < t.B; k += 64)
+      if ((t.len[k] < 0 || t.len[k] > t.stride * SPEC_KV_PAGE) && t.first[k + 1] > t.first[k]) flag(t);
   int at = 0;
   for (int b0 = 0; b0 < t.B; b0 += 64) {
     const int k = min(b0 + lane, t.B - 1);
     Seq q{t.first[k], t.first[k + 1], t.len[k]};
     const bool in = b0 + lane < t.B, off = q.len < 0 || q.len > t.stride * SPEC_KV_PAGE;
-    if (one && in && off && q.rows > q.first) flag(t);
     q.rows = in && !off ? q.rows - q.first : 0;
     const int begin = q.len / SPEC_KV_PAGE;
     const int tiles = q.rows > 0 ? (int)(((int64_t)q.len + q.rows - 1) / SPEC_KV_PAGE) - begin + 1 : 0;
@@ -272,30 +263,39 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention.  A kv head's query rows r = j G + g of a sequence (pass row j, query head g of the
-// kv head's G) are cut into chunks of 32.  A workgroup of eight waves has one chunk and a group of
-// consecutive pages; wave w takes the group's half pages (32 slots) w, w + 8, ... on its own, with a running
-// maximum and sum of each row, so that no wave waits for another before the end.  Per half page
+// Attention.  A kv head's query rows r = j G + g of a sequence (pass row j, query head g of the kv head's G) are cut
+// into chunks of RW tiles of 32.  A workgroup has one chunk and a group of consecutive pages, whose halves (32 slots)
+// its eight waves take in turn, each with a running maximum and sum of its tile's rows:
+//   RW = 1  wave w takes halves w, w + 8, ..., loads them itself, and waits for no other before the end;
+//   RW = 2  waves kw and kw + 4 share halves kw, kw + 4, ..., a tile each; two more waves load all keys and all
+//           values, a step ahead, as a wave that loads stands still until its loads have gone out.
+// Per half page
 //   S^T = K Q^T   (32x32x16 bf16 products, keys down, query rows across)
 //   p = 2^(scale log2e s - m), l += p
 //   O^T += V^T P^T, p as the sum of two bf16 numbers
 // and the waves' (m, l, O) are joined in LDS: the group gives O / L, (m, L) of every row.  One group of a
 // sequence is its result; several are joined by k_tree_combine.
 //
-// A wave's half page lies in LDS, its keys and its values each in one buffer, copied there by loads that pass no
-// register: the next keys while these probabilities meet their values, the next values while the next scores
-// are formed.  The 16-byte chunks of a row are permuted by an xor, so that the sixteen
-// lanes that an LDS read serves together (of 32 those whose number has an even number of ones in bits 2 to 4, then the
-// others) fall in distinct banks: 215 bytes a cycle and CU, where 136 were read with a permutation for eight lanes at a time. Row m of a score tile is key
-// (m & 3) + 4 ((m >> 3) & 1) + 8 ((m >> 2) & 1) + 16 (m >> 4): a lane's eight scores of a 16-key step are
-// then eight consecutive keys, one 16-byte read of a value row.
+// Halves lie in LDS, copied there by loads that pass no register.  RW = 1: keys and values each in one buffer, the
+// next keys while these probabilities meet their values, the next values while the next scores are formed.  The
+// 16-byte chunks of a row are permuted by an xor, so that the sixteen lanes that an LDS read serves together (of 32
+// those whose number has an even number of ones in bits 2 to 4, then the others) fall in distinct banks: 215 bytes a
+// cycle and CU, where 136 were read with a permutation for eight lanes at a time.  Row m of a score tile is key
+// (m & 3) + 4 ((m >> 3) & 1) + 8 ((m >> 2) & 1) + 16 (m >> 4): a lane's eight scores of a 16-key step are then eight
+// consecutive keys, one 16-byte read of a value row.
 //
 // Masks: halves below the sequence's length are seen whole.  In the others, a lane walks up its row's ancestors and
 // has 32 bits, one for each key.  Values of slots that no row sees are set to zero there.
 //
-// What is not finite.  A value that is not finite (or sums that leave the range, of values near its end)
-// makes a sum that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with
-// such values taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
+// What is not finite.  A value that is not finite (or sums that leave the range, of values near its end) makes a sum
+// that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with such values
+// taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
+//
+// What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 168 MB: 37 us, of
+// which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
+// joins and the combine; 144 rows of them 48, as chunks of more than 64 query rows are read twice.  25 rows over 131
+// thousand slots: 34 to 35, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
+// 40 rows over 4096 slots 17: three such steps, and 9 us that do not depend on the cache.
 // ---------------------------------------------------------------------------
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -303,7 +303,8 @@ __device__ __forceinline__ f32x16 mfma32x32x16(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-constexpr int kWaves = 8, kLoaders = 2, kTileRows = 32;           // waves of an attention workgroup, query rows of a wave
+// Waves of an attention workgroup that multiply, that load (RW = 2), query rows of a tile.
+constexpr int kWaves = 8, kLoaders = 2, kTileRows = 32;
 
 // What workgroup i of an attention call does.
 struct Work {
@@ -574,7 +575,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     page = page_at(p);
     if (RW == 1) {
       load_k(page, mine, wave & 1);
-      load_v(page, mine + 0, wave & 1);
+      load_v(page, mine, wave & 1);
     }
     if (p + KW < last) next = page_at(p + KW);
   }
@@ -955,7 +956,7 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
   for (int k = 0; k < 4; ++k) mx = fmaxf(mx, s_m[k][lane]);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    c[k] = s_m[k][lane] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][lane] - mx) * s_a[k][lane];
+    c[k] = s_a[k][lane] == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_m[k][lane] - mx) * s_a[k][lane];
     sum += c[k];
   }
   o = f32x4{0.f, 0.f, 0.f, 0.f};

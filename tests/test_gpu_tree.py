@@ -374,6 +374,60 @@ def test_what_a_row_does_not_see_has_no_influence(torch):
         a.check([(0, j) for j in range(7) if off not in p.line(0, j)])
 
 
+@pytest.mark.parametrize("length", [150, 3000])
+def test_a_key_of_nan_is_nan_for_the_rows_that_see_it(torch, length):
+    rng = np.random.default_rng(23)
+    p = ref.Pass([length], [5], [[-1, 0, 0, 1, 2]])
+    for slots, rows in (([length + 1], [1, 3]), (range(0, length // 2), range(5))):
+        a = Attn(torch, rng, p, 4, 2, 128)
+        for s in slots:
+            a.k[1, a.table[0, s // PAGE], 0, s % PAGE] = 0x7FC0       # of the first kv head only
+        a.dk = _dev(torch, a.k)
+        a.cache = _cache(torch, a.B, a.dk, a.dv)
+        out, lse = a.run()
+        out = ref.bf16_value(out).reshape(5, 4, 128)
+        for j in range(5):
+            assert np.isnan(out[j, :2]).all() == np.isnan(lse[j, :2]).all() == (j in rows)
+            assert np.isfinite(out[j, 2:]).all() and np.isfinite(lse[j, 2:]).all()
+        a.check([(0, j) for j in range(5) if j not in rows])
+
+
+def test_a_pass_without_rows_does_nothing(torch):
+    rng = np.random.default_rng(24)
+    for p in (ref.Pass([10, 20], [0, 0], [[], []], 3), ref.Pass([10], [0], None, 1)):
+        table, pages = ref.table_of(p, rng)
+        got = _append(torch, rng, p, table, pages, 2, 1, 64, (32, 0, 0))
+        _check_append(p, table, pages, 2, 1, 64, (32, 0, 0), 0, 1e4, None, 1, got)
+        a = Attn(torch, rng, p, 4, 2, 64)
+        a.check()
+        got = _commit(torch, rng, p, [0] * p.rows, [0] * p.rows)
+        _check_commit(p, [0] * p.rows, [[] for _ in p.lens], got)
+        assert got["err"] == int(a.rows.err) == 0
+
+
+def test_one_bad_length_among_many_sequences(torch):
+    """Sequence 130 of 150 has none: it is reported and has no rows, the others have theirs."""
+    rng = np.random.default_rng(25)
+    lens = [int(x) for x in rng.integers(0, 100, 150)]
+    p = ref.Pass(lens, [1] * 150, None, 2, stride=2)
+    table, pages = ref.table_of(p, rng)
+    bad = list(lens)
+    bad[130] = 129
+    got = _append(torch, rng, p, table, pages, 2, 1, 64, (32, 0, 0), rows=Rows(torch, p, table, lens=bad))
+    assert got["err"] == 1 and (got["q"][130] == 0x1234).all()
+    q = ref.bf16_value(got["q"][:, :128])
+    assert np.isfinite(q[:130]).all() and (got["q"][131:150, :128] != 0x1234).any(axis=1).all()
+    a = Attn(torch, rng, p, 4, 2, 64, table=table, pages=pages)
+    a.rows = Rows(torch, p, table, lens=bad)
+    out, lse = a.run()
+    assert int(a.rows.err) == 1 and (out[130] == 0x1234).all() and (lse[130] == -7).all()
+    want_out, want_lse = Attn(torch, rng, p, 4, 2, 64, table=table, pages=pages, k=a.k, v=a.v, q=a.q).run()
+    others = [r for r in range(150) if r != 130]
+    np.testing.assert_allclose(ref.bf16_value(out[others]), ref.bf16_value(want_out[others]), rtol=2.0 ** -7, atol=1e-6)
+    got = _commit(torch, rng, p, [0] * p.rows, [0] * p.rows, table=table, pages=pages, rows=Rows(torch, p, table, lens=bad))
+    assert got["err"] == 1 and got["n"] == [int(b != 130) for b in range(150)]
+
+
 @pytest.mark.parametrize("nq,nkv,D", [(4, 2, 64), (14, 2, 128)])
 @pytest.mark.parametrize("lens", [[150], [3000], [40, 700]])
 def test_infinite_values_that_a_row_sees(torch, nq, nkv, D, lens):
