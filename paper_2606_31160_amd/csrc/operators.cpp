@@ -300,8 +300,13 @@ spec_status spec_kv_append(const spec_kv* c, int32_t layer, const spec_rows* r, 
   a.pos = d_pos;
   a.axis_end[0] = rope->interleaved ? -1 : sec[0];
   a.axis_end[1] = rope->interleaved ? -1 : sec[0] + sec[1];
-  for (int d = 0; d < half; ++d)
-    a.turns[d] = std::pow((double)rope->base, -2.0 * d / c->head_dim) / 6.283185307179586476925286766559;
+  // base^(-2 d / head_dim) / 2 pi of d = 8 i + j as two factors: 16 powers a call instead of 64, which took 1.3 us
+  double low[8];
+  for (int j = 0; j < 8; ++j) low[j] = std::pow((double)rope->base, -2.0 * j / c->head_dim);
+  for (int i = 0; i < half; i += 8) {
+    const double high = std::pow((double)rope->base, -2.0 * i / c->head_dim) / 6.283185307179586476925286766559;
+    for (int j = 0; j < 8; ++j) a.turns[i + j] = high * low[j];
+  }
   return launched(launch_kv_append(a, c->head_dim, stream), f);
 }
 
