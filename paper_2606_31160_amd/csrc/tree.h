@@ -56,6 +56,7 @@ struct TreeAttnPlan {
   int tiles;               // of 32 query rows of a kv head that a workgroup has
   int units, target, least, grid;
   bool combine;            // a sequence may have several groups
+  int likely;              // groups of a sequence whose pages fill the table
   size_t ml, unit, bytes;
 };
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu);

@@ -492,12 +492,71 @@ __device__ __forceinline__ int key_swizzle(int r) {
   return D == 128 ? (r & 3) + 4 * ((r >> 3) & 1) + 8 * ((r >> 2) & 1) : ((r >> 1) & 1) + 2 * ((r >> 3) & 1) + 4 * ((r >> 2) & 1);
 }
 
+// The rows that each row of a sequence's tree sees, itself and its ancestors, as bits, by one wave whose lane l has the
+// parents of rows l, l + 64, ...  A row takes the bits of its ancestor 1, 2, 4, ... above: a chain of 160 rows takes 8
+// steps.  Words behind the last row are not written.
+constexpr int kLineWords = SPEC_MAX_ROWS / 32, kLaneRows = (SPEC_MAX_ROWS + 63) / 64;
+template <int K>
+__device__ __forceinline__ void lines_step(int rows, int (&up)[kLaneRows], uint32_t (&x)[kLaneRows][kLineWords]) {
+  if (64 * K >= rows) return;
+  const int from = up[K];
+  int next = -1;
+  uint32_t y[kLineWords] = {};
+#pragma unroll
+  for (int u = 0; u <= K; ++u) {
+    const bool here = from >= 0 && from >> 6 == u;
+    const int n = __builtin_amdgcn_ds_bpermute(4 * (from & 63), up[u]);
+    next = here ? n : next;
+#pragma unroll
+    for (int e = 0; e < kLineWords; ++e)
+      if (e < 2 * u + 2 && 32 * e < rows) {         // (a row of the u-th 64 has no others)
+        const uint32_t z = __builtin_amdgcn_ds_bpermute(4 * (from & 63), x[u][e]);
+        y[e] = here ? z : y[e];
+      }
+  }
+  up[K] = next;
+#pragma unroll
+  for (int e = 0; e < kLineWords; ++e) x[K][e] |= y[e];
+}
+__device__ __forceinline__ void lines(const TreeRows& t, int rows, int (&up)[kLaneRows], uint32_t (*line)[kLineWords]) {
+  constexpr int NS = kLaneRows;
+  const int lane = threadIdx.x & 63;
+  uint32_t x[NS][kLineWords];
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    const int j = 64 * k + lane;
+    if (j >= rows) up[k] = -1;
+    if (up[k] < -1 || up[k] >= j) {
+      flag(t);
+      up[k] = -1;
+    }
+#pragma unroll
+    for (int e = 0; e < kLineWords; ++e) x[k][e] = j >> 5 == e ? 1u << (j & 31) : 0;
+  }
+  for (;;) {
+    bool more = up[0] >= 0;
+#pragma unroll
+    for (int k = 1; k < NS; ++k) more |= up[k] >= 0;
+    if (!__any(more)) break;
+    static_assert(NS == 3, "one call for every 64 rows, parents behind their children");
+    lines_step<2>(rows, up, x);
+    lines_step<1>(rows, up, x);
+    lines_step<0>(rows, up, x);
+  }
+#pragma unroll
+  for (int k = 0; k < NS; ++k)
+    if (64 * k + lane < rows)
+#pragma unroll
+      for (int e = 0; e < kLineWords; ++e)
+        if (32 * e < rows) line[64 * k + lane][e] = x[k][e];
+}
+
 template <int D, int RW>
 __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ? 3 : 2) void k_tree_attn(TreeAttnArgs a) {
   constexpr int DT = D / 32, KS = D / 16, H = 32, kHalf = H * D * 2;   // slots of a half, bytes of its keys or values
   constexpr int kLoads = kHalf / 1024, KC = D / 8, KW = kWaves / RW;   // KW waves share a group's halves
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ int16_t s_up[SPEC_MAX_ROWS];
+  __shared__ uint32_t s_line[SPEC_MAX_ROWS][kLineWords];
   __shared__ float s_m[kWaves][kTileRows], s_l[kWaves][kTileRows];
   const TreeRows& t = a.t;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
@@ -579,25 +638,25 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     }
     if (p + KW < last) next = page_at(p + KW);
   }
-  if (last > tail)                                  // workgroup-uniform
-    for (int j = threadIdx.x; j < w.s.rows; j += blockDim.x) s_up[j] = (int16_t)parent_of(t, w.s, j);
+  const bool trees = last > tail && t.parent && wave == 0;   // wave-uniform
+  int up[kLaneRows];
+  if (trees)
+#pragma unroll
+    for (int k = 0; k < kLaneRows; ++k) up[k] = 64 * k + lane < w.s.rows ? t.parent[w.s.first + 64 * k + lane] : -1;
   // Q operands, zeros for rows that there are not
   const int r = row0 + n32, qj = r < rows ? r / a.G : 0, head = w.kvh * a.G + (r < rows ? r % a.G : 0);
   u32x4 q[KS];
   u32x4* const sq = reinterpret_cast<u32x4*>(lds + kWaves * 2 * kHalf) + (rw & 1) * KS * 64 + lane;   // RW = 2: in LDS
   if (!loader) {
     const bf16_t* src = a.q + (int64_t)(w.s.first + qj) * a.q_stride + (int64_t)head * D + 8 * half;
-    if (RW == 1) {
+    constexpr int QS = RW == 1 ? KS : KS / KW;      // a wave's operands
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[k] = ld16(src + 16 * k);
-      if (r >= rows)
+    for (int k = 0; k < QS; ++k) q[k] = ld16(src + 16 * (RW == 1 ? k : kw + KW * k));
+    if (trees) lines(t, w.s.rows, up, s_line);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) q[k] = u32x4{0, 0, 0, 0};
-    } else {
-      for (int k = kw; k < KS; k += KW) {
-        const u32x4 x = ld16(src + 16 * k);
-        sq[k * 64] = r < rows ? x : u32x4{0, 0, 0, 0};
-      }
+    for (int k = 0; k < QS; ++k) {
+      if (r >= rows) q[k] = u32x4{0, 0, 0, 0};
+      if (RW == 2) sq[(kw + KW * k) * 64] = q[k];
     }
   }
   __syncthreads();
@@ -649,12 +708,17 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     const int seen = page < 0 ? 0 : min(max(w.s.len - p * H, 0), H);   // slots below are everybody's
     end = page < 0 ? 0 : min(w.s.len + w.s.rows - p * H, H);
     uint32_t x = seen >= H ? ~0u : (1u << seen) - 1;
-    if (page >= 0 && seen < H)
-      for (int i = qj; i >= 0; i = s_up[i]) {
-        const int at = w.s.len + i - p * H;
-        if (at < 0) break;
-        if (at < H) x |= 1u << at;
+    if (page >= 0 && seen < H) {
+      const int off = p * H - w.s.len;              // wave-uniform: the first slot's row, or what is missing to row 0
+      if (!t.parent) {
+        x |= (uint32_t)((1ull << min(max(qj - off + 1, 0), H)) - 1);
+      } else if (off < 0) {
+        x |= s_line[qj][0] << -off;
+      } else {
+        const uint32_t lo = s_line[qj][off >> 5], hi = (off | 31) + 1 < w.s.rows ? s_line[qj][(off >> 5) + 1] : 0;
+        x |= (uint32_t)(((uint64_t)hi << 32 | lo) >> (off & 31));
       }
+    }
     mask = x >> (8 * half);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -909,15 +973,16 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   }
 }
 
-// Joins the groups of a (sequence, kv head, chunk): grid (units, quarters of 32-dimension tiles), four waves, of
-// which wave w takes the groups w, w + 4, ...  A lane has four dimensions of a row, as it wrote them.
-template <int D, int RW>
-__global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
-  constexpr int Q = D / 8, U = 4;
-  __shared__ f32x4 s_o[4][64];
-  __shared__ float s_m[4][64], s_a[4][64];
+// Joins the groups of a (sequence, kv head, chunk): grid (units, tiles x eights of the dimensions), W waves to an
+// eight, of which wave w takes the groups w, w + W, ...  A lane has four dimensions of a row, as it wrote them.
+template <int D, int RW, int W>
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void k_tree_combine(TreeAttnArgs a) {
+  constexpr int Q = D / 8, U = 4, GB = W < 4 ? 4 / W : 1;   // GB eights of the dimensions a workgroup
+  __shared__ f32x4 s_o[GB * W][64];
+  __shared__ float s_m[GB * W][64], s_a[GB * W][64];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n32 = lane & 31, half = lane >> 5, rw = blockIdx.y / Q, g = blockIdx.y % Q;
+  const int n32 = lane & 31, half = lane >> 5, rw = blockIdx.y / (Q / GB);
+  const int g = blockIdx.y % (Q / GB) * GB + wave / W, w0 = wave % W;
   const int units = a.units[0].first;
   const TreeUnit u = a.units[1 + blockIdx.x];
   if ((int)blockIdx.x >= units || u.groups < 2) return;
@@ -925,15 +990,15 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
   const bool live = r < u.rows;
   float M = -INFINITY, A = 0.f;                     // maximum and sum of the groups' weights
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = wave; k0 < u.groups; k0 += 4 * U) {
+  for (int k0 = w0; k0 < u.groups; k0 += W * U) {
     f32x4 x[U];
     float2 ml[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const int64_t part = u.part + min(k0 + 4 * k, u.groups - 1);
+      const int64_t part = u.part + min(k0 + W * k, u.groups - 1);
       ml[k] = live ? a.ml[(part * RW + rw) * kTileRows + n32] : make_float2(-INFINITY, 0.f);
       x[k] = live ? a.part[((part * RW + rw) * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
-      if (k0 + 4 * k >= u.groups) ml[k].y = 0.f;
+      if (k0 + W * k >= u.groups) ml[k].y = 0.f;
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
@@ -948,23 +1013,30 @@ __global__ __launch_bounds__(256) void k_tree_combine(TreeAttnArgs a) {
       M = now;
     }
   }
-  s_o[wave][lane] = o, s_m[wave][lane] = M, s_a[wave][lane] = A;
-  __syncthreads();
-  if (wave) return;
-  float mx = -INFINITY, sum = 0.f, c[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) mx = fmaxf(mx, s_m[k][lane]);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    c[k] = s_a[k][lane] == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_m[k][lane] - mx) * s_a[k][lane];
-    sum += c[k];
+  if (W > 1) {
+    s_o[wave][lane] = o, s_m[wave][lane] = M, s_a[wave][lane] = A;
+    __syncthreads();
+    if (w0) return;
   }
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  float mx = M, sum = A;
+  if (W > 1) {
+    float c[W];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const f32x4 x = s_o[k][lane];
+    for (int k = 1; k < W; ++k) mx = fmaxf(mx, s_m[wave + k][lane]);
+    sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += finite(x[e]) ? x[e] * (c[k] / sum) : x[e];
+    for (int k = 0; k < W; ++k) {
+      const float x = s_a[wave + k][lane];
+      c[k] = x == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_m[wave + k][lane] - mx) * x;
+      sum += c[k];
+    }
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const f32x4 x = s_o[wave + k][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += finite(x[e]) ? x[e] * (c[k] / sum) : x[e];
+    }
   }
   if (!live) return;
   if (sum == 0.f) o = f32x4{NAN, NAN, NAN, NAN};
@@ -1107,13 +1179,15 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
   hipLaunchKernelGGL((k_tree_attn<D, RW>), dim3(p.grid), dim3(threads), lds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.combine) return e;
-  hipLaunchKernelGGL((k_tree_combine<D, RW>), dim3(p.units, RW * (D / 8)), dim3(256), 0, s, a);
+  // (one wave where sequences have a group or two, eight where they have many.  W = 1, 4, 8, us in graphs with the attention:
+  // 144 rows of 16 scenes, two groups, 46.5, 48.1, -; 40 rows over 4096 slots, 10 groups, 17.7, 16.6, 17.1; one row over 8000, 42
+  // groups, 24.3, 15.0, 14.2; 25 rows over 131 thousand, 128 groups, 52.2, 35.3, 33.0)
+  const auto combine = p.likely > 16 ? k_tree_combine<D, RW, 8> : p.likely > 2 ? k_tree_combine<D, RW, 4> : k_tree_combine<D, RW, 1>;
+  const int waves = p.likely > 16 ? 8 : 4, eights = p.likely > 2 ? 1 : 4;
+  hipLaunchKernelGGL(combine, dim3(p.units, RW * (D / 8) / eights), dim3(64 * waves), 0, s, a);
   return hipGetLastError();
 }
 }  // namespace
-
-// Pages of a group at least: a half for each wave; of short tables one group, which needs no second kernel.
-constexpr int kLeastPages = kWaves / 2, kOneGroup = 8;
 
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
@@ -1125,8 +1199,14 @@ TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stri
   p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G));
   p.target = ncu;
   p.grid = std::max(p.target, p.units);
-  p.least = stride <= kOneGroup ? kOneGroup : kLeastPages;
+  // Pages of a group at least; short tables make one group, which needs no second kernel.  Us in graphs, 28 + 2 x 4 heads of
+  // 128, at least 2, 3 and 4 pages: 4 rows over 450, 1000, 4000 slots 11.1, 11.1, 11.8; 11.4, 11.3, 11.9; 13.4, 13.5, 12.6; 40 rows
+  // over 1000 and 2000 14.1, 13.7, 14.3; 15.9, 15.6, 14.5.  One group up to 8 pages and up to 6: 40 rows over 300 10.8 and 12.0, 4 rows
+  // over 380 9.2 and 10.7; up to 24: 5 rows over 700 and 960 13.7 and 16.1, several 12.2 and 12.4.
+  const int least = 3, whole = 8;
+  p.least = stride <= whole ? whole : least;
   p.combine = stride > p.least;
+  p.likely = std::min(stride / p.least, p.target / std::max(p.units, 1));
   const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8,
                units = (size_t)(1 + p.units) * sizeof(TreeUnit);
   p.ml = (part + 255) / 256 * 256;
