@@ -291,10 +291,13 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with such values
 // taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
 //
-// What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 168 MB: 37 us, of
+// Of a tree, wave 0 makes the ancestors of every row into bits while the first pages come: a masked half then takes two
+// words, where a walk up the tree took a chain of 160 rows over 2000 slots 36.6 us in graphs and takes 22.8.
+//
+// What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
-// joins and the combine; 144 rows of them 48, as chunks of more than 64 query rows are read twice.  25 rows over 131
-// thousand slots: 34 to 35, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
+// joins and the combine; 144 rows of them 46.5, as chunks of more than 64 query rows are read twice.  25 rows over 131
+// thousand slots: 33, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
 // 40 rows over 4096 slots 17: three such steps, and 9 us that do not depend on the cache.
 // ---------------------------------------------------------------------------
 
@@ -1048,10 +1051,12 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void k_tree_combine(TreeAttnA
 
 // ---------------------------------------------------------------------------
 // Commit.  One workgroup per layer, sequence and kv head.  Each wave walks the tree, a lane having every 64th row: the
-// row's children that hold its greedy token by one vote, the lowest of them next.  The rows move to lower slots only, in
-// their order, 16 at a time: what a step reads lies above everything that earlier ones wrote, and what it
-// overwrites was read by this step or earlier ones, the same dimensions by the same wave.  Bound by latency: the chain
-// first rows -> tree -> page table -> slots.
+// row's children that hold its greedy token by one vote, the lowest of them next.  The rows move to lower slots only,
+// in their order, 16 at a time: what a step reads lies above everything that earlier ones wrote, and what it
+// overwrites was read by this step or earlier ones, the same dimensions by the same wave.  A small commit is bound by
+// latency, the chain first rows -> tree -> page table -> slots: one launch, 3.3 us in graphs.  16 sequences of 28
+// layers and 4 kv heads of 128 take 10.4 for 5 MB: a slot's values are one element of each of 128 lines, so 26 MB are
+// fetched.  The page table's part in LDS first: 10.9.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
