@@ -79,8 +79,8 @@ def _append(torch, rng, p, table, pages, nq, nkv, D, section, inter=0, base=1000
 
 def _check_append(p, table, pages, nq, nkv, D, section, inter, base, pos, layer, got, in_place=False):
     """Rotations: cos and sin of an angle that 32 bits hold within pi 2^-24 of a turn's half, themselves within 2^-23, then
-    two products and a sum: under 2^-21 (|x0| + |x1|); an angle in 64 bits is off by 3 and here by 2 roundings of 2^-53
-    of itself; then half a step of bf16."""
+    two products and a sum: under 2^-21 (|x0| + |x1|); an angle in 64 bits is off by 3 and here by 5 roundings of 2^-53
+    of itself (two powers, a quotient and two products); then half a step of bf16."""
     theta = base ** (-2.0 * np.arange(D // 2) / D)
     ax = ref.axes(D, section, inter)
     k1, v1, q1 = got["k0"].copy(), got["v0"].copy(), None
@@ -94,7 +94,7 @@ def _check_append(p, table, pages, nq, nkv, D, section, inter, base, pos, layer,
             want = ref.rotate(x[r, :nq + nkv], theta * np.array([at[a] for a in ax], np.float64))
             mag = np.abs(x[r, :nq + nkv])
             mag = np.repeat(mag[:, 0::2] + mag[:, 1::2], 2, axis=1)
-            tol = 2.0 ** -8 * np.abs(want) + 1.01 * (2.0 ** -21 + 5 * 2.0 ** -53 * max(abs(int(x)) for x in at)) * mag
+            tol = 2.0 ** -8 * np.abs(want) + 1.01 * (2.0 ** -21 + 8 * 2.0 ** -53 * max(abs(int(x)) for x in at)) * mag
             have = ref.bf16_value(q_out[r, :nq * D]).reshape(nq, D)
             assert (np.abs(have - want[:nq]) <= tol[:nq]).all(), (b, j)
             page = table[b, slot // PAGE] if slot // PAGE < table.shape[1] else -1
@@ -217,6 +217,18 @@ def test_append_takes_broken_parents_as_roots(torch):
     got = _append(torch, rng, p, table, pages, 2, 1, 64, (32, 0, 0), rows=Rows(torch, p, table, parents=[-1, 0, 7, 2, 4, -2]))
     assert got["err"] == 1
     _check_append(p, table, pages, 2, 1, 64, (32, 0, 0), 0, 10000.0, None, 1, got)
+
+
+def test_append_of_many_rows_of_trees_at_given_positions(torch):
+    """Positions say where rows stand, so trees may be larger than a pass that is attended."""
+    rng = np.random.default_rng(8)
+    counts = [200, 150]
+    p = ref.Pass([30, 61], counts, [ref.random_tree(rng, c) for c in counts], 3)
+    table, pages = ref.table_of(p, rng)
+    pos = rng.integers(0, 9000, (3, p.rows))
+    got = _append(torch, rng, p, table, pages, 6, 2, 128, (16, 24, 24), pos=pos)
+    assert got["err"] == 0
+    _check_append(p, table, pages, 6, 2, 128, (16, 24, 24), 0, 10000.0, pos, 1, got)
 
 
 # -- attention ---------------------------------------------------------------------
@@ -447,6 +459,31 @@ def test_infinite_values_that_a_row_sees(torch, nq, nkv, D, lens):
     a.check()
 
 
+@pytest.mark.parametrize("nq,nkv,D,lens,count", [
+    (28, 4, 128, [5000] + [70] * 15, 9), (16, 8, 64, [2500] + [3] * 31, 5),      # a group or two of a sequence were likely
+    (28, 4, 128, [9000], 1), (7, 1, 128, [20000], 12)])                          # many groups
+def test_infinite_values_in_some_of_many_groups(torch, nq, nkv, D, lens, count):
+    rng = np.random.default_rng(26)
+    p = ref.Pass(lens, [count] * len(lens), _trees(rng, [count] * len(lens)), stride=max(lens) // PAGE + 2)
+    a = Attn(torch, rng, p, nq, nkv, D)
+    n = lens[0]
+    for slot, d, x in ((0, 0, INF), (n - 1, 0, INF), (n // 2, 1, -INF), (n // 3, 2, INF), (n // 4, 2, -INF), (n // 5, 3, NAN),
+                       (n + count - 1, 4, INF), (n + count // 2, D - 1, -INF)):
+        a.v[1, a.table[0, slot // PAGE], :, d, slot % PAGE] = ref.bf16(np.array(x))
+    a.dv = _dev(torch, a.v)
+    a.cache = _cache(torch, a.B, a.dk, a.dv)
+    a.check([(0, j) for j in {0, count // 2, count - 1}] + [(len(lens) - 1, j) for j in {0, count - 1}])
+
+
+@pytest.mark.parametrize("nq,nkv,D,lens,counts", [
+    (1024, 2, 64, [700], [2]), (300, 300, 64, [40, 700], [1, 2]), (96, 48, 128, [600, 0, 130], [5, 1, 1]), (640, 1, 128, [1], [40])])
+def test_attention_of_many_heads(torch, nq, nkv, D, lens, counts):
+    rng = np.random.default_rng(27)
+    a = Attn(torch, rng, ref.Pass(lens, counts, _trees(rng, counts), 1, stride=max(12, max(lens) // PAGE + 1)), nq, nkv, D)
+    a.check([(b, j) for b, c in enumerate(counts) for j in {0, c - 1}])
+    assert int(a.rows.err) == 0
+
+
 @pytest.mark.parametrize("lens", [[150], [3000]])
 def test_values_at_the_ends_of_their_range(torch, lens):
     """The largest bf16 values, whose sums leave the range, and the smallest normal ones."""
@@ -647,6 +684,45 @@ def test_commit_of_chains_and_without_outputs(torch):
     _check_commit(p, greedy, [list(range(9)), [0], list(range(4))], got)
     got = _commit(torch, rng, p, tokens, greedy, outs=False)
     _check_commit(p, greedy, [[0], [0], [0]], got, outs=False)
+
+
+def test_layers_apart_and_no_word_for_errors(torch):
+    """Layers with room between them, which stays as it was; and passes with faults that nobody asked to hear of."""
+    from paper_2606_31160_amd import binding as B
+    rng = np.random.default_rng(35)
+    p = ref.Pass([60, 5], [6, 3], [[-1, 0, 0, 2, 2, 4], [-1, 0, 0]], 1)
+    table, pages = ref.table_of(p, rng)
+    table[1, 0] = pages + 3
+    nkv, D, L, gap = 2, 64, 3, 8 * 37
+    one = pages * nkv * PAGE * D
+    k0, v0 = (ref.bf16(rng.standard_normal(L * (one + gap))) for _ in range(2))
+    rows = Rows(torch, p, table)
+    rows.desc.d_err = 0
+    tokens, greedy = [0, 1, 2, 3, 4, 5, 0, 1, 2, 0], [2, 9, 4, 9, 5, 9, 2, 9, 9, 0]
+    i32 = lambda x: _dev(torch, np.array(x, np.int32))  # noqa: E731
+    tok, gre = i32(tokens), i32(greedy)
+    q = _dev(torch, ref.bf16(rng.standard_normal((p.rows, 4 * D))))
+    x = _dev(torch, ref.bf16(rng.standard_normal((p.rows, 2 * nkv * D))))
+    ran = []
+    for stride, a, b in ((one + gap, k0, v0), (one, *(y.reshape(L, one + gap)[:, :one] for y in (k0, v0)))):
+        k, v = _dev(torch, a), _dev(torch, b)
+        cache = B.kv(nkv, D, pages, k.data_ptr(), v.data_ptr(), L, stride)
+        out = torch.full((p.rows, 4 * D), 0x1234, dtype=torch.int16, device="cuda")
+        ws = torch.empty(B.spec_tree_attn_workspace_bytes(cache, rows.desc, 4), dtype=torch.uint8, device="cuda")
+        for layer in range(L):
+            B.spec_kv_append(cache, layer, rows.desc, B.rope(1e4, (32, 0, 0)), 0, 0, 0, 0, x.data_ptr(), x.data_ptr() + 2 * nkv * D, x.stride(0),
+                             0, 0)
+        B.spec_tree_attn(cache, 2, rows.desc, 4, q.data_ptr(), 4 * D, 0.125, out.data_ptr(), 4 * D, 0, ws.data_ptr(), ws.numel())
+        B.spec_tree_commit(cache, rows.desc, tok.data_ptr(), gre.data_ptr())
+        torch.cuda.synchronize()
+        ran.append((_bits(k).reshape(L, stride), _bits(v).reshape(L, stride), _bits(out)))
+    far, near = ran
+    for i, before in ((0, k0), (1, v0)):
+        np.testing.assert_array_equal(far[i][:, :one], near[i])
+        np.testing.assert_array_equal(far[i][:, one:], before.reshape(L, one + gap)[:, one:])
+        assert (near[i] != before.reshape(L, one + gap)[:, :one]).any(axis=1).all()
+    np.testing.assert_array_equal(far[2], near[2])
+    assert np.isfinite(ref.bf16_value(far[2][:6])).all() and np.isnan(ref.bf16_value(far[2][6:9])).all()
 
 
 @pytest.mark.parametrize("stop", [-1, 1, 77])
