@@ -473,7 +473,7 @@ __device__ __forceinline__ float other_half(float x) {   // of lane ^ 32
                "buffer_load_dwordx4 %3, %1, %2 offen " hint "lds\n\t"         \
                "buffer_load_dwordx4 %4, %1, %2 offen offset:1024 " hint "lds\n\t" \
                "buffer_load_dwordx4 %5, %1, %2 offen offset:2048 " hint "lds\n\t" \
-               "buffer_load_dwordx4 %6, %1, %2 offen offset:3072 " hint "lds" ::"s"(lds), \
+               "buffer_load_dwordx4 %6, %1, %2 offen offset:3*1024 " hint "lds" ::"s"(lds), \
                "s"(page), "s"(step), "v"(o0), "v"(o1), "v"(o2), "v"(o3)       \
                : "memory")
 __device__ __forceinline__ void page_to_lds(bool once, __amdgpu_buffer_rsrc_t page, uint32_t lds, uint32_t step, uint32_t o0, uint32_t o1,
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     // 16 rows of 64 bytes a KB, 128 bytes apart in the page
 #pragma unroll
     for (int i = 0; i < kLoads; i += 4)
-      page_to_lds(once, r, lds0 + to + kHalf + 1024 * i, odd_half * 64 + 2048 * i, voff, voff + 1024, voff + 2048, voff + 3072);
+      page_to_lds(once, r, lds0 + to + kHalf + 1024 * i, odd_half * 64 + 2048 * i, voff, voff + 1024, voff + 2 * 1024, voff + 3 * 1024);
   };
   const bool loader = RW == 2 && wave >= kWaves;    // wave-uniform
   // Buffers of 2 kHalf bytes, keys and then values.  RW = 1: a wave's own one.  RW = 2: two for each kw, which take turns.
