@@ -296,9 +296,9 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 //
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
-// joins and the combine; 144 rows of them 46.5, as chunks of more than 64 query rows are read twice.  25 rows over 131
-// thousand slots: 33, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
-// 40 rows over 4096 slots 17: three such steps, and 9 us that do not depend on the cache.
+// joins and the combine; 144 rows of them 46, as chunks of more than 64 query rows are read twice.  25 rows over 131
+// thousand slots: 32, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
+// 40 rows over 4096 slots 16.5: three such steps, and 9 us that do not depend on the cache.
 // ---------------------------------------------------------------------------
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -977,52 +977,86 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
 }
 
 // Joins the groups of a (sequence, kv head, chunk): grid (units, tiles x eights of the dimensions), W waves to an
-// eight, of which wave w takes the groups w, w + W, ...  A lane has four dimensions of a row, as it wrote them.
+// eight.  A lane has four dimensions of a row, as it was written, of every (W subs)-th group: where there are many
+// groups of tiles of at most 8 or 16 rows, a wave has subs = 4 or 2 of them at once.  Bound by the latency of its rounds
+// of loads, of which the next is asked for before one is summed: one row of 7 query heads over 131 thousand slots, 256 groups,
+// takes 21.7 us in graphs with the attention, 29.5 without these two and with a quotient for every group.
 template <int D, int RW, int W>
 __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void k_tree_combine(TreeAttnArgs a) {
   constexpr int Q = D / 8, U = 4, GB = W < 4 ? 4 / W : 1;   // GB eights of the dimensions a workgroup
   __shared__ f32x4 s_o[GB * W][64];
   __shared__ float s_m[GB * W][64], s_a[GB * W][64];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int n32 = lane & 31, half = lane >> 5, rw = blockIdx.y / (Q / GB);
+  const int rw = blockIdx.y / (Q / GB);
   const int g = blockIdx.y % (Q / GB) * GB + wave / W, w0 = wave % W;
   const int units = a.units[0].first;
   const TreeUnit u = a.units[1 + blockIdx.x];
   if ((int)blockIdx.x >= units || u.groups < 2) return;
-  const int r = u.row + rw * kTileRows + n32;
-  const bool live = r < u.rows;
+  const int rows = u.rows - u.row - rw * kTileRows; // of this tile
+  if (rows <= 0) return;
+  const int bits = u.groups <= W * U || rows > 16 ? 5 : rows > 8 ? 4 : 3, subs = 32 >> bits;
+  const int row = lane & ((1 << bits) - 1), half = lane >> bits & 1, sub = lane >> (bits + 1);
+  const bool live = row < rows;
   float M = -INFINITY, A = 0.f;                     // maximum and sum of the groups' weights
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = w0; k0 < u.groups; k0 += W * U) {
-    f32x4 x[U];
-    float2 ml[U];
+  f32x4 x[U] = {}, y[U] = {};
+  float2 ml[U], next[U];
+  auto load = [&](int k0, f32x4 (&o)[U], float2 (&ml)[U]) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const int64_t part = u.part + min(k0 + W * k, u.groups - 1);
-      ml[k] = live ? a.ml[(part * RW + rw) * kTileRows + n32] : make_float2(-INFINITY, 0.f);
-      x[k] = live ? a.part[((part * RW + rw) * Q + g) * 64 + lane] : f32x4{0.f, 0.f, 0.f, 0.f};
-      if (k0 + W * k >= u.groups) ml[k].y = 0.f;
+      const int group = k0 + W * subs * k + sub;
+      const int64_t tile = (int64_t)(u.part + group) * RW + rw;
+      ml[k] = make_float2(-INFINITY, 0.f);
+      if (live && group < u.groups) {
+        ml[k] = a.ml[tile * kTileRows + row];
+        o[k] = a.part[(tile * Q + g) * 64 + row + 32 * half];
+      }
     }
+  };
+  if (w0 * subs < u.groups) load(w0 * subs, x, ml);
+  for (int k0 = w0 * subs; k0 < u.groups; k0 += W * subs * U) {
+    if (k0 + W * subs * U < u.groups) load(k0 + W * subs * U, y, next);
+    float now = M, c[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) now = ml[k].y == 0.f ? now : fmaxf(now, ml[k].x);   // (0: a group without slots that the row sees)
+    const float f = M == -INFINITY ? 0.f : A * __builtin_amdgcn_exp2f(M - now);
+    float sum = f;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      if (ml[k].y == 0.f) continue;                 // a group without slots that the row sees
-      const float now = fmaxf(M, ml[k].x);
-      const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - now), c = __builtin_amdgcn_exp2f(ml[k].x - now) * ml[k].y;
+      c[k] = ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - now) * ml[k].y;
+      sum += c[k];
+    }
+    if (sum != 0.f) {
       // o stays the average of the groups so far: sums of large values stay in range
-      const float sum = __builtin_fmaf(A, f, c), p = A * f / sum, q = c / sum;
+      const float r = 1.f / sum;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (finite(o[e]) ? o[e] * p : o[e]) + (finite(x[k][e]) ? x[k][e] * q : x[k][e]);
+      for (int e = 0; e < 4; ++e) o[e] = finite(o[e]) ? o[e] * (f * r) : o[e];
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += ml[k].y == 0.f ? 0.f : finite(x[k][e]) ? x[k][e] * (c[k] * r) : x[k][e];
       A = sum;
       M = now;
     }
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = y[k], ml[k] = next[k];
   }
-  if (W > 1) {
-    s_o[wave][lane] = o, s_m[wave][lane] = M, s_a[wave][lane] = A;
-    __syncthreads();
-    if (w0) return;
+  for (int d = 2 << bits; d < 64; d <<= 1) {        // the groups that a wave had at once
+    const float m2 = __shfl_xor(M, d), a2 = __shfl_xor(A, d), now = fmaxf(M, m2);
+    const float f = A == 0.f ? 0.f : A * __builtin_amdgcn_exp2f(M - now), c = a2 == 0.f ? 0.f : a2 * __builtin_amdgcn_exp2f(m2 - now);
+    const float r = 1.f / (f + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float o2 = __shfl_xor(o[e], d);
+      o[e] = (A == 0.f ? 0.f : finite(o[e]) ? o[e] * (f * r) : o[e]) + (a2 == 0.f ? 0.f : finite(o2) ? o2 * (c * r) : o2);
+    }
+    M = now, A = f + c;
   }
   float mx = M, sum = A;
   if (W > 1) {
+    s_o[wave][lane] = o, s_m[wave][lane] = M, s_a[wave][lane] = A;
+    __syncthreads();
+    if (w0 || sub) return;
     float c[W];
 #pragma unroll
     for (int k = 1; k < W; ++k) mx = fmaxf(mx, s_m[wave + k][lane]);
@@ -1033,17 +1067,18 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void k_tree_combine(TreeAttnA
       c[k] = x == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_m[wave + k][lane] - mx) * x;
       sum += c[k];
     }
+    const float r = 1.f / sum;
     o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       const f32x4 x = s_o[wave + k][lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += finite(x[e]) ? x[e] * (c[k] / sum) : x[e];
+      for (int e = 0; e < 4; ++e) o[e] += finite(x[e]) ? x[e] * (c[k] * r) : x[e];
     }
   }
-  if (!live) return;
+  if (!live || sub) return;
   if (sum == 0.f) o = f32x4{NAN, NAN, NAN, NAN};
-  const int j = r / a.G, h = u.head + r % a.G;
+  const int at = u.row + rw * kTileRows + row, j = at / a.G, h = u.head + at % a.G;
   bf16_t* to = a.out + (int64_t)(u.first + j) * a.out_stride + (int64_t)h * D + 8 * g + 4 * half;
   *reinterpret_cast<u32x2*>(to) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
   if (a.lse && g == 0 && half == 0) a.lse[(int64_t)(u.first + j) * a.nq + h] = (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
@@ -1185,7 +1220,7 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.combine) return e;
   // (one wave where sequences have a group or two, eight where they have many.  W = 1, 4, 8, us in graphs with the attention:
-  // 144 rows of 16 scenes, two groups, 46.5, 48.1, -; 40 rows over 4096 slots, 10 groups, 17.7, 16.6, 17.1; one row over 8000, 42
+  // an earlier form, 144 rows of 16 scenes, two groups, 46.5, 48.1, -; 40 rows over 4096 slots, 10 groups, 17.7, 16.6, 17.1; one row over 8000, 42
   // groups, 24.3, 15.0, 14.2; 25 rows over 131 thousand, 128 groups, 52.2, 35.3, 33.0)
   const auto combine = p.likely > 16 ? k_tree_combine<D, RW, 8> : p.likely > 2 ? k_tree_combine<D, RW, 4> : k_tree_combine<D, RW, 1>;
   const int waves = p.likely > 16 ? 8 : 4, eights = p.likely > 2 ? 1 : 4;
