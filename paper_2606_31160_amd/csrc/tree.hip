@@ -1219,11 +1219,12 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
   hipLaunchKernelGGL((k_tree_attn<D, RW>), dim3(p.grid), dim3(threads), lds, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.combine) return e;
-  // (one wave where sequences have a group or two, eight where they have many.  W = 1, 4, 8, us in graphs with the attention:
-  // an earlier form, 144 rows of 16 scenes, two groups, 46.5, 48.1, -; 40 rows over 4096 slots, 10 groups, 17.7, 16.6, 17.1; one row over 8000, 42
-  // groups, 24.3, 15.0, 14.2; 25 rows over 131 thousand, 128 groups, 52.2, 35.3, 33.0)
-  const auto combine = p.likely > 16 ? k_tree_combine<D, RW, 8> : p.likely > 2 ? k_tree_combine<D, RW, 4> : k_tree_combine<D, RW, 1>;
-  const int waves = p.likely > 16 ? 8 : 4, eights = p.likely > 2 ? 1 : 4;
+  // (one wave to an eighth where sequences have few groups, eight where they have many.  Us in graphs with the attention, W = 1
+  // and 4: 16 sequences of one row over 5000 slots, 3 groups, 36.2 and 36.6, 8 of 5 rows over 3000, 4 groups, 20.5 and 21.0; W = 4 and
+  // 8: one row over 20 thousand, 32 groups, 15.8 and 16.3, 63 over 20 thousand, 106 groups, 18.0 and 16.3, 175 over 131 thousand, 85
+  // groups, 33.9 and 32.3)
+  const auto combine = p.likely > 32 ? k_tree_combine<D, RW, 8> : p.likely > 4 ? k_tree_combine<D, RW, 4> : k_tree_combine<D, RW, 1>;
+  const int waves = p.likely > 32 ? 8 : 4, eights = p.likely > 4 ? 1 : 4;
   hipLaunchKernelGGL(combine, dim3(p.units, RW * (D / 8) / eights), dim3(64 * waves), 0, s, a);
   return hipGetLastError();
 }
