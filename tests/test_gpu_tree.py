@@ -475,6 +475,22 @@ def test_infinite_values_in_some_of_many_groups(torch, nq, nkv, D, lens, count):
     a.check([(0, j) for j in {0, count // 2, count - 1}] + [(len(lens) - 1, j) for j in {0, count - 1}])
 
 
+@pytest.mark.parametrize("count", [1, 2, 4])
+@pytest.mark.parametrize("nq,nkv,D", [(28, 4, 128), (6, 2, 64)])
+def test_attention_of_one_long_sequence_among_many_without_rows(torch, nq, nkv, D, count):
+    """Few groups were likely, and there are many: of tiles of 3 to 28 rows."""
+    rng = np.random.default_rng(28)
+    counts = [0] * 30 + [count] + [0] * 49
+    p = ref.Pass([12000 if c else 5 for c in counts], counts, _trees(rng, counts), 20)
+    a = Attn(torch, rng, p, nq, nkv, D)
+    for slot, d, x in ((100, 0, INF), (11900, 0, INF), (5000, 1, -INF), (7000, 2, NAN)):
+        a.v[1, a.table[30, slot // PAGE], 0, d, slot % PAGE] = ref.bf16(np.array(x))
+    a.dv = _dev(torch, a.v)
+    a.cache = _cache(torch, a.B, a.dk, a.dv)
+    a.check()
+    assert int(a.rows.err) == 0
+
+
 @pytest.mark.parametrize("nq,nkv,D,lens,counts", [
     (1024, 2, 64, [700], [2]), (300, 300, 64, [40, 700], [1, 2]), (96, 48, 128, [600, 0, 130], [5, 1, 1]), (640, 1, 128, [1], [40])])
 def test_attention_of_many_heads(torch, nq, nkv, D, lens, counts):
