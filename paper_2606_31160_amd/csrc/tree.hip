@@ -297,8 +297,9 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
 // joins and the combine; 144 rows of them 46, as chunks of more than 64 query rows are read twice.  25 rows over 131
-// thousand slots: 32, a step of 4 halves and 2 tiles takes 2600 cycles of which the matrix unit is busy 1536.
-// 40 rows over 4096 slots 16.5: three such steps, and 9 us that do not depend on the cache.
+// thousand slots: 32, of which 18 are 13 steps at 1.07 PFLOP/s of matrix operations (a large library product: 1.35), as
+// much with half of the operands' LDS reads and 2.4 less without any load.  40 rows over 4096 slots 16.5: three such
+// steps, and 9 us that do not depend on the cache.
 // ---------------------------------------------------------------------------
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
