@@ -284,15 +284,14 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // (m & 3) + 4 ((m >> 3) & 1) + 8 ((m >> 2) & 1) + 16 (m >> 4): a lane's eight scores of a 16-key step are then eight
 // consecutive keys, one 16-byte read of a value row.
 //
-// Masks: halves below the sequence's length are seen whole.  In the others, a lane walks up its row's ancestors and
-// has 32 bits, one for each key.  Values of slots that no row sees are set to zero there.
+// Masks: halves below the sequence's length are seen whole.  In the others a lane has 32 bits, one for each key: in a
+// chain by its row's number, in a tree two words of its ancestors' bits, which wave 0 makes while the first pages come
+// (a walk up the tree: a chain of 160 rows over 2000 slots 36.6 us in graphs, where it takes 22.8).  Values of slots that
+// no row sees are set to zero there.
 //
 // What is not finite.  A value that is not finite (or sums that leave the range, of values near its end) makes a sum
 // that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with such values
 // taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
-//
-// Of a tree, wave 0 makes the ancestors of every row into bits while the first pages come: a masked half then takes two
-// words, where a walk up the tree took a chain of 160 rows over 2000 slots 36.6 us in graphs and takes 22.8.
 //
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
