@@ -734,10 +734,11 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
-    if (__any(mx > m + 8.f)) {
-      const float now = fmaxf(m, mx);
-      const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);   // (sums are zero yet)
-      m = now;
+    const bool grown = mx > m + 8.f;
+    if (__any(grown)) {
+      // (each row by its own scores: no bit of it follows from what its siblings' slots hold)
+      const float f = grown && m != -INFINITY ? __builtin_amdgcn_exp2f(m - mx) : 1.f;   // (-infinity: sums are zero yet)
+      m = grown ? mx : m;
       if (__any(f != 1.f)) {
         l *= f;
         grow(f);

@@ -1,0 +1,49 @@
+"""Passes over trees where a row could notice what it does not see, and at the ends of lengths, tables and values."""
+import math
+
+import numpy as np
+import pytest
+
+from tests import _tree as ref
+from tests.test_gpu_tree import PAGE, Attn, Rows, _append, _bits, _cache, _check_append, _check_commit, _commit, _dev, _trees, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+NAN, INF = math.nan, math.inf
+
+# one row tile a workgroup and two; one group of a sequence and several
+SHAPES = [(4, 2, 64), (2, 1, 128), (28, 4, 128), (16, 2, 64)]
+BRANCHES = [-1, 0, 0, 1, 2, 3, 4]     # two branches, rows 1 3 5 and 2 4 6
+
+
+def _again(a):
+    """Outputs of a call whose cache has been changed on the host."""
+    a.dk, a.dv = _dev(a.torch, a.k), _dev(a.torch, a.v)
+    a.cache = _cache(a.torch, a.B, a.dk, a.dv)
+    return a.run()
+
+
+def _same(got, want, rows):
+    for x, y in zip(got, want):
+        np.testing.assert_array_equal(x[rows].view(np.uint16 if x.dtype == np.uint16 else np.uint32),
+                                      y[rows].view(np.uint16 if y.dtype == np.uint16 else np.uint32))
+
+
+@pytest.mark.parametrize("nq,nkv,D", [(256, 256, 64), (256, 256, 128), (1280, 256, 64), (1280, 256, 128)])
+@pytest.mark.parametrize("length", [300, 700])
+def test_scores_of_siblings_do_not_move_a_row(torch, nq, nkv, D, length):  # noqa: F811
+    """Bit for bit: a sibling's scores may be any number.  One group for each of many heads: its waves have several halves of
+    pages each, of which the last holds the rows' slots."""
+    rng = np.random.default_rng(31)
+    p = ref.Pass([length], [7], [BRANCHES])
+    a = Attn(torch, rng, p, nq, nkv, D, layers=1, layer=0)
+    want = a.run()
+    for j in (2, 6):
+        slot = length + j
+        page = a.table[0, slot // PAGE]
+        others, k = [r for r in range(7) if j not in p.line(0, r)], a.k.copy()
+        for factor in (30.0, -3.0, 1000.0):
+            # along a query of the row: its score against itself is large
+            q = ref.bf16_value(a.q[j]).reshape(nkv, nq // nkv, D)[:, 0]
+            a.k[0, page, :, slot % PAGE] = ref.bf16(factor * q)
+            _same(_again(a), want, others)
+        a.k = k
