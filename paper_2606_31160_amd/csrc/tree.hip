@@ -290,8 +290,9 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // no row sees are set to zero there.
 //
 // What is not finite.  A value that is not finite (or sums that leave the range, of values near its end) makes a sum
-// that is not finite, which the end of the loop sees; the wave then goes over its halves once more, with such values
-// taken as zero and the sums 2^20 lower, and adds them whole to the rows that see their slots.
+// that is not finite, which the end of the loop sees.  The wave then goes over its halves once more, with such values
+// taken as zero: sums that had none are the same bits again, and so are those of a row that does not see them as without them; the
+// others are infinite or NaN.  Sums that still leave the range do not in one more pass, with probabilities 2^20 lower.
 //
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
@@ -679,7 +680,8 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   }
 
   // this lane's operand rows in LDS
-  const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
+  auto key_row = [](int n) __attribute__((always_inline)) { return (n & 3) + 4 * ((n >> 3) & 1) + 8 * ((n >> 2) & 1) + 16 * (n >> 4); };
+  const int krow = key_row(n32);
   const int kswz = key_swizzle<D>(krow);
   const int kat = krow * D * 2, vat = kHalf + n32 * 64;
   u32x4 kx[KS], vx[2][DT];
@@ -691,7 +693,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     return *reinterpret_cast<const u32x4*>(lds + from + vat + dt * 32 * 64 + (((2 * step + half) ^ ((n32 >> 2) & 3)) * 16));
   };
 
-  float m, l, above = 0.f;
+  float m, l;
   f32x16 o[DT], s;
   u32x4 ph[2], pl[2];
   auto zero = [&](f32x16& x) __attribute__((always_inline)) {
@@ -728,8 +730,8 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
       if (!(mask >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = -INFINITY;
   };
   // Scores to probabilities, the parts of the keys of step 16 k in ph, pl[k]; grow(f) is called where sums have
-  // to follow a maximum: when it has grown by 2^8.
-  auto soft = [&](auto grow) __attribute__((always_inline)) {
+  // to follow a maximum: when it has grown by 2^8.  The parts are those of `unit` times the probabilities.
+  auto soft = [&](float unit, auto grow) __attribute__((always_inline)) {
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -744,7 +746,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
         grow(f);
       }
     }
-    const float ref = m == -INFINITY ? 0.f : m + above;
+    const float ref = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -755,7 +757,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.scale_log2, -ref));
         sum += x + y;
         uint32_t h, g;
-        split2(x, y, h, g);
+        split2(x * unit, y * unit, h, g);
         ph[k][e] = h, pl[k][e] = g;
       }
     l += sum;
@@ -786,7 +788,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   };
   auto rest = [&](bool whole) __attribute__((always_inline)) {
     if (!whole) masks();
-    soft([&](float f) __attribute__((always_inline)) {
+    soft(1.f, [&](float f) __attribute__((always_inline)) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
     });
@@ -838,97 +840,13 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
       if (p + KW < last) next = page_at(p + KW);
       lds_read();
     }
-    __syncthreads();                                // every buffer has been read
-  }
-
-  float x0[4] = {0.f, 0.f, 0.f, 0.f};               // 0 times what is not finite is NaN
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x0[i & 3] = __builtin_fmaf(o[dt][i], 0.f, x0[i & 3]);
-  const bool slow = __any(r < rows && (x0[0] + x0[1]) + (x0[2] + x0[3]) != 0.f);
-  if (slow) {
-    // once more, 32 dimensions at a time
-    above = 20.f;
-#pragma unroll 1
-    for (int dt = 0; dt < DT; ++dt) {
-      f32x16 z;
-      m = -INFINITY, l = 0.f;
-      zero(z);
-#pragma unroll 1
-      for (p = 2 * w.lo + kw; p < last; p += KW) {
-        page = page_at(p);
-        load_k(page, 2 * kHalf * wave, kw & 1);
-        load_v(page, 2 * kHalf * wave, kw & 1);
-        loads_but<0>();
-        keys(2 * kHalf * wave);
-        scores();
-        masks();
-        soft([&](float f) __attribute__((always_inline)) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[i] = finite(z[i]) ? z[i] * f : z[i];
-        });
-        uint32_t odd = 0;
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-          u32x4 x = value(2 * kHalf * wave, dt, step), y;
-          const int valid = end - 16 * step - 8 * half;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-            const uint32_t b = not_finite16(x[e]);
-            odd |= b;
-            y[e] = x[e] & ~((b >> 15) * 0xffffu);
-          }
-          z = mfma32x32x16(y, ph[step], z);
-          z = mfma32x32x16(y, pl[step], z);
-        }
-        if (__any(odd != 0)) {
-          // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
-          // against a one for each slot that it sees
-          f32x16 c;
-          zero(c);
-#pragma unroll 1
-          for (int step = 0; step < 2; ++step) {
-            u32x4 x = value(2 * kHalf * wave, dt, step), y;
-            const int valid = end - 16 * step - 8 * half;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-              uint32_t k = 0;
-              y[e] = 0;
-#pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                const uint32_t v = x[e] >> (16 * b) & 0xffff;
-                k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
-                y[e] |= (mask >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
-              }
-              x[e] = k;
-            }
-            c = mfma32x32x16(x, y, c);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int k = (int)c[i];
-            if (k & 0xff) z[i] += INFINITY;
-            if (k & 0xff00) z[i] -= INFINITY;
-            if (k >> 16) z[i] = NAN;
-          }
-        }
-        lds_read();
-      }
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        if (d == dt) o[d] = z;
-    }
   }
 
   // join the waves: each scales its sums by its part of the group's, then each adds up its share
   l += other_half(l);
-  m += above;
   if (half == 0) s_m[wave][n32] = m, s_l[wave][n32] = l;
-  __syncthreads();
-  f32x4* const sums = reinterpret_cast<f32x4*>(lds);   // [waves][DT][4][64], in the place of their pages
+  __syncthreads();                                  // (every buffer has been read, too)
+  f32x4* const sums = reinterpret_cast<f32x4*>(lds);   // [waves][DT][4][64], each in the place of a wave's pages
   constexpr int Q = DT * 4;
   float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -938,21 +856,122 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
     const float x = s_m[rw * KW + k][n32];
     L = __builtin_fmaf(x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - M), s_l[rw * KW + k][n32], L);
   }
-  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;
-  if (slow) {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[dt][i] = finite(o[dt][i]) ? o[dt][i] * f : o[dt][i];
-  } else {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
-  }
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M) / L;   // at most one
+
+  float x0[4] = {0.f, 0.f, 0.f, 0.f};               // 0 times what is not finite is NaN
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      sums[(wave * Q + dt * 4 + i) * 64 + lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    for (int i = 0; i < 16; ++i) x0[i & 3] = __builtin_fmaf(o[dt][i], 0.f, x0[i & 3]);
+  const bool slow = __any(r < rows && (x0[0] + x0[1]) + (x0[2] + x0[3]) != 0.f);
+  if (__builtin_expect_with_probability(slow, 0, 1.0)) {   // (else the loop above gives its registers to those here)
+    // once more, 32 dimensions at a time, operands straight from the pages; sums that leave the range once again, with lower
+    // probabilities
+    constexpr float kLow = 0x1p-20f;
+#pragma unroll 1
+    for (int dt = 0; dt < DT; ++dt) {
+      uint32_t open = 0;                            // which of these dimensions' sums have left the range
+#pragma unroll 1
+      for (int again = 0; again < 2; ++again) {
+        if (again && !__any(r < rows && open != 0)) break;
+        f32x16 z;
+        uint64_t seen = 0;                          // of each dimension 1: infinity, 2: minus infinity, 4: NaN
+        m = -INFINITY, l = 0.f;                     // (they become what they were)
+        zero(z);
+#pragma unroll 1
+        for (p = 2 * w.lo + kw; p < last; p += KW) {
+          page = page_at(p);
+          const int64_t at = ((int64_t)max(page, 0) * t.nkv + w.kvh) * (2 * H * D);
+          int n = n32;
+          asm volatile("" : "+v"(n));               // (addresses are formed anew each time, as there are no registers to keep them)
+          const bf16_t* const pk = a.kc + at + (p & 1) * H * D + key_row(n) * D + 8 * half;
+          const bf16_t* const pv = a.vt + at + (dt * 32 + n) * SPEC_KV_PAGE + (p & 1) * H + 8 * half;
+          if (RW == 1) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) kx[k] = ld16(pk + 16 * k);
+            scores();
+          } else {
+            zero(s);
+#pragma unroll 1
+            for (int k = 0; k < KS; ++k) s = mfma32x32x16(ld16(pk + 16 * k), sq[k * 64], s);
+          }
+          masks();
+          soft(again ? kLow : 1.f, [&](float f) __attribute__((always_inline)) { z *= f; });
+          u32x4 x[2];
+          uint32_t odd = 0;
+#pragma unroll
+          for (int step = 0; step < 2; ++step) {
+            x[step] = ld16(pv + 16 * step);
+            const int valid = end - 16 * step - 8 * half;
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[step][e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+              const uint32_t b = not_finite16(x[step][e]);
+              odd |= b;
+              y[e] = x[step][e] & ~((b >> 15) * 0xffffu);
+            }
+            z = mfma32x32x16(y, ph[step], z);
+            z = mfma32x32x16(y, pl[step], z);
+          }
+          if (!again && __any(odd != 0)) {
+            // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
+            // against a one for each slot that it sees
+            f32x16 c;
+            zero(c);
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+              u32x4 y;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                uint32_t k = 0;
+                y[e] = 0;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  const uint32_t v = x[step][e] >> (16 * b) & 0xffff;
+                  k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
+                  y[e] |= (mask >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
+                }
+                x[step][e] = k;
+              }
+              c = mfma32x32x16(x[step], y, c);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int k = (int)c[i];
+              seen |= (uint64_t)((k & 0xff ? 1 : 0) | (k & 0xff00 ? 2 : 0) | (k >> 16 ? 4 : 0)) << (3 * i);
+            }
+          }
+        }
+        int at = lane;
+        asm volatile("" : "+v"(at));
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4* const to = &sums[(wave * Q + dt * 4 + g) * 64 + at];
+          f32x4 v = again ? *to : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * g + e, k = (int)(seen >> (3 * i)) & 7;
+            if (again)
+              v[e] = open >> i & 1 ? z[i] * (f * (1.f / kLow)) : v[e];
+            else if (k)                             // (f is NaN where a score is)
+              v[e] = (k == 1 ? INFINITY : k == 2 ? -INFINITY : NAN) + 0.f * f;
+            else
+              v[e] = z[i] * f, open |= finite(z[i]) ? 0 : 1u << i;
+          }
+          *to = v;
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      o[dt] *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sums[(wave * Q + dt * 4 + i) * 64 + lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    }
+  }
   __syncthreads();
   if (r >= rows) return;
 #pragma unroll

@@ -47,3 +47,41 @@ def test_scores_of_siblings_do_not_move_a_row(torch, nq, nkv, D, length):  # noq
             a.k[0, page, :, slot % PAGE] = ref.bf16(factor * q)
             _same(_again(a), want, others)
         a.k = k
+
+
+@pytest.mark.parametrize("nq,nkv,D", SHAPES)
+@pytest.mark.parametrize("length", [20, 100, 3000])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -120, 2.0 ** 100])
+def test_what_siblings_hold_does_not_move_a_row(torch, nq, nkv, D, length, size):  # noqa: F811
+    """Bit for bit: a sibling's slot may hold values that are not finite, and the row's own be small or large."""
+    rng = np.random.default_rng(32)
+    p = ref.Pass([length], [7], [BRANCHES])
+    a = Attn(torch, rng, p, nq, nkv, D)
+    fine = np.isfinite(ref.bf16_value(a.v))
+    a.v[fine] = ref.bf16(size * ref.bf16_value(a.v))[fine]
+    want = _again(a)
+    for j, what in ((2, NAN), (4, INF), (6, -INF)):
+        slot = length + j
+        page = a.table[0, slot // PAGE]
+        k, v = a.k.copy(), a.v.copy()
+        a.k[1, page, :, slot % PAGE, ::7] = ref.bf16(np.array(what))
+        a.v[1, page, :, ::3, slot % PAGE] = ref.bf16(np.array(what))
+        _same(_again(a), want, [r for r in range(7) if j not in p.line(0, r)])
+        a.k, a.v = k, v
+
+
+@pytest.mark.parametrize("nq,nkv,D", SHAPES)
+@pytest.mark.parametrize("length", [100, 3000])
+def test_values_not_finite_in_one_dimension_leave_the_others(torch, nq, nkv, D, length):  # noqa: F811
+    """Bit for bit, also of rows that see them."""
+    rng = np.random.default_rng(33)
+    p = ref.Pass([length], [7], [BRANCHES])
+    a = Attn(torch, rng, p, nq, nkv, D)
+    out, lse = a.run()
+    for slot, d, what in ((3, 5, INF), (length // 2, 17, NAN), (length + 1, D - 1, -INF)):
+        a.v[1, a.table[0, slot // PAGE], :, d, slot % PAGE] = ref.bf16(np.array(what))
+    got, glse = _again(a)
+    np.testing.assert_array_equal(glse, lse)
+    keep = [d for d in range(D) if d not in (5, 17, D - 1)]
+    np.testing.assert_array_equal(got.reshape(7, nq, D)[:, :, keep], out.reshape(7, nq, D)[:, :, keep])
+    a.check()
