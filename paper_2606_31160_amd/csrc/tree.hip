@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // What is not finite.  A value that is not finite (or sums that leave the range, of values near its end) makes a sum
 // that is not finite, which the end of the loop sees.  The wave then goes over its halves once more, with such values
 // taken as zero: sums that had none are the same bits again, and so are those of a row that does not see them as without them; the
-// others are infinite or NaN.  Sums that still leave the range do not in one more pass, with probabilities 2^20 lower.
+// others are infinite or NaN.  Sums that still leave the range do not in one more pass, with probabilities 2^40 lower.
 //
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
@@ -866,8 +866,8 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   const bool slow = __any(r < rows && (x0[0] + x0[1]) + (x0[2] + x0[3]) != 0.f);
   if (__builtin_expect_with_probability(slow, 0, 1.0)) {   // (else the loop above gives its registers to those here)
     // once more, 32 dimensions at a time, operands straight from the pages; sums that leave the range once again, with lower
-    // probabilities
-    constexpr float kLow = 0x1p-20f;
+    // probabilities: up to 2^8 times the largest value for each slot, of which a wave has fewer than 2^31
+    constexpr float kLow = 0x1p-40f;
 #pragma unroll 1
     for (int dt = 0; dt < DT; ++dt) {
       uint32_t open = 0;                            // which of these dimensions' sums have left the range

@@ -85,3 +85,29 @@ def test_values_not_finite_in_one_dimension_leave_the_others(torch, nq, nkv, D, 
     keep = [d for d in range(D) if d not in (5, 17, D - 1)]
     np.testing.assert_array_equal(got.reshape(7, nq, D)[:, :, keep], out.reshape(7, nq, D)[:, :, keep])
     a.check()
+
+
+@pytest.mark.parametrize("nq,nkv", [(256, 256), (10240, 256)])
+def test_large_values_of_many_slots_of_one_wave(torch, nq, nkv):  # noqa: F811
+    """A wave's own sum: 12 thousand slots (24 thousand where two waves share a half) of the largest values, whose
+    weights are 2^7.9 times its first slots'."""
+    D, stride = 64, 1501
+    pages = 2
+    rng = np.random.default_rng(35)
+    k = np.zeros((1, pages, nkv, PAGE, D), np.uint16)
+    k[0, 1, :, :, 0] = ref.bf16(np.array(8.0 * 7.9 * math.log(2)))     # scores of the second page: 7.9 ln 2
+    sign = np.where(rng.random(D) < 0.5, 1.0, -1.0)
+    v = np.broadcast_to(ref.bf16(sign * 255 * 2.0 ** 120)[None, None, None, :, None], (1, pages, nkv, D, PAGE)).copy()
+    q = ref.bf16(np.broadcast_to((np.arange(D) == 0) * 1.0, (1, nq, D)).reshape(1, nq * D))
+    table = np.ones((1, stride), np.int32)
+    table[0, :4] = 0                                                   # every wave begins with a low score
+    p = ref.Pass([(stride - 1) * PAGE + 10], [1], None, stride=stride)
+    a = Attn(torch, rng, p, nq, nkv, D, layers=1, layer=0, table=table, pages=pages, k=k, v=v, q=q)
+    out, lse = a.run()
+    np.testing.assert_array_equal(ref.bf16_value(out).reshape(nq, D), np.broadcast_to(sign * 255 * 2.0 ** 120, (nq, D)))
+    z = ref.bf16_value(k[0, 1, 0, 0, 0]) / 8
+    low = PAGE * int((table == 0).sum())
+    want = math.log(low + (p.lens[0] + 1 - low) * math.exp(z))
+    # (a wave's sum of a row's terms and the sum of waves, an exponential, a logarithm)
+    assert np.abs(lse - want).max() <= (p.lens[0] / 4 + 64) * 2.0 ** -24 + 2.0 ** -21 * (1 + want)
+    assert int(a.rows.err) == 0
