@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // What is not finite.  A value that is not finite (or sums that leave the range, of values near its end) makes a sum
 // that is not finite, which the end of the loop sees.  The wave then goes over its halves once more, with such values
 // taken as zero: sums that had none are the same bits again, and so are those of a row that does not see them as without them; the
-// others are infinite or NaN.  Sums that still leave the range do not in one more pass, with probabilities 2^40 lower.
+// others are infinite or NaN.  Where a sum still leaves the range, one of values 2^40 lower, formed beside it, does not.
 //
 // What bounds it (in graphs, with the combine).  16 scenes of 2 to 8 thousand slots, one row each, 158 MB: 37 us, of
 // which a group's loads take 28 (5.6 TB/s) and the rest are the chain lengths -> plan -> page table -> first page,
@@ -680,8 +680,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   }
 
   // this lane's operand rows in LDS
-  auto key_row = [](int n) __attribute__((always_inline)) { return (n & 3) + 4 * ((n >> 3) & 1) + 8 * ((n >> 2) & 1) + 16 * (n >> 4); };
-  const int krow = key_row(n32);
+  const int krow = (n32 & 3) + 4 * ((n32 >> 3) & 1) + 8 * ((n32 >> 2) & 1) + 16 * (n32 >> 4);
   const int kswz = key_swizzle<D>(krow);
   const int kat = krow * D * 2, vat = kHalf + n32 * 64;
   u32x4 kx[KS], vx[2][DT];
@@ -730,8 +729,8 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
       if (!(mask >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = -INFINITY;
   };
   // Scores to probabilities, the parts of the keys of step 16 k in ph, pl[k]; grow(f) is called where sums have
-  // to follow a maximum: when it has grown by 2^8.  The parts are those of `unit` times the probabilities.
-  auto soft = [&](float unit, auto grow) __attribute__((always_inline)) {
+  // to follow a maximum: when it has grown by 2^8.
+  auto soft = [&](auto grow) __attribute__((always_inline)) {
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -757,7 +756,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.scale_log2, -ref));
         sum += x + y;
         uint32_t h, g;
-        split2(x * unit, y * unit, h, g);
+        split2(x, y, h, g);
         ph[k][e] = h, pl[k][e] = g;
       }
     l += sum;
@@ -788,7 +787,7 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
   };
   auto rest = [&](bool whole) __attribute__((always_inline)) {
     if (!whole) masks();
-    soft(1.f, [&](float f) __attribute__((always_inline)) {
+    soft([&](float f) __attribute__((always_inline)) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
     });
@@ -864,112 +863,103 @@ __global__ __launch_bounds__(64 * (kWaves + (RW == 2 ? kLoaders : 0)), RW == 2 ?
 #pragma unroll
     for (int i = 0; i < 16; ++i) x0[i & 3] = __builtin_fmaf(o[dt][i], 0.f, x0[i & 3]);
   const bool slow = __any(r < rows && (x0[0] + x0[1]) + (x0[2] + x0[3]) != 0.f);
-  if (__builtin_expect_with_probability(slow, 0, 1.0)) {   // (else the loop above gives its registers to those here)
-    // once more, 32 dimensions at a time, operands straight from the pages; sums that leave the range once again, with lower
-    // probabilities: up to 2^8 times the largest value for each slot, of which a wave has fewer than 2^31
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    o[dt] *= f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sums[(wave * Q + dt * 4 + i) * 64 + lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+  }
+  if (slow) {
+    // Once more, 32 dimensions at a time, operands straight from the pages.  Beside each sum one of lower values: a slot adds up
+    // to 2^8 times the largest value, and a wave has fewer than 2^31.
     constexpr float kLow = 0x1p-40f;
 #pragma unroll 1
     for (int dt = 0; dt < DT; ++dt) {
-      uint32_t open = 0;                            // which of these dimensions' sums have left the range
-#pragma unroll 1
-      for (int again = 0; again < 2; ++again) {
-        if (again && !__any(r < rows && open != 0)) break;
-        f32x16 z;
-        uint64_t seen = 0;                          // of each dimension 1: infinity, 2: minus infinity, 4: NaN
-        m = -INFINITY, l = 0.f;                     // (they become what they were)
-        zero(z);
-#pragma unroll 1
-        for (p = 2 * w.lo + kw; p < last; p += KW) {
-          page = page_at(p);
-          const int64_t at = ((int64_t)max(page, 0) * t.nkv + w.kvh) * (2 * H * D);
-          int n = n32;
-          asm volatile("" : "+v"(n));               // (addresses are formed anew each time, as there are no registers to keep them)
-          const bf16_t* const pk = a.kc + at + (p & 1) * H * D + key_row(n) * D + 8 * half;
-          const bf16_t* const pv = a.vt + at + (dt * 32 + n) * SPEC_KV_PAGE + (p & 1) * H + 8 * half;
-          if (RW == 1) {
+      bool open = false;                            // one of these dimensions' sums is not finite
 #pragma unroll
-            for (int k = 0; k < KS; ++k) kx[k] = ld16(pk + 16 * k);
-            scores();
-          } else {
-            zero(s);
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = sums[(wave * Q + dt * 4 + g) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) open |= !finite(v[e]);
+      }
+      if (!__any(r < rows && open)) continue;
+      f32x16 z, low;
+      uint64_t seen = 0;                            // of each dimension 1: infinity, 2: minus infinity, 4: NaN
+      m = -INFINITY, l = 0.f;                       // (they become what they were)
+      zero(z);
+      zero(low);
 #pragma unroll 1
-            for (int k = 0; k < KS; ++k) s = mfma32x32x16(ld16(pk + 16 * k), sq[k * 64], s);
+      for (p = 2 * w.lo + kw; p < last; p += KW) {
+        page = page_at(p);
+        const int64_t at = ((int64_t)max(page, 0) * t.nkv + w.kvh) * (2 * H * D);
+        const bf16_t* const pk = a.kc + at + (p & 1) * H * D + krow * D + 8 * half;
+        const bf16_t* const pv = a.vt + at + (dt * 32 + n32) * SPEC_KV_PAGE + (p & 1) * H + 8 * half;
+        u32x4 x[2] = {ld16(pv), ld16(pv + 16)};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) kx[k] = ld16(pk + 16 * k);
+        scores();
+        masks();
+        soft([&](float f) __attribute__((always_inline)) { z *= f, low *= f; });
+        uint32_t odd = 0;
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+          const int valid = end - 16 * step - 8 * half;
+          u32x4 y, y2;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[step][e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
+            const uint32_t b = not_finite16(x[step][e]);
+            odd |= b;
+            y[e] = x[step][e] & ~((b >> 15) * 0xffffu);
+            y2[e] = pack2(__uint_as_float(y[e] << 16) * kLow, __uint_as_float(y[e] & 0xffff0000u) * kLow);
           }
-          masks();
-          soft(again ? kLow : 1.f, [&](float f) __attribute__((always_inline)) { z *= f; });
-          u32x4 x[2];
-          uint32_t odd = 0;
+          z = mfma32x32x16(y, ph[step], z);
+          z = mfma32x32x16(y, pl[step], z);
+          low = mfma32x32x16(y2, ph[step], low);
+          low = mfma32x32x16(y2, pl[step], low);
+        }
+        if (__any(odd != 0)) {
+          // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
+          // against a one for each slot that it sees
+          f32x16 c;
+          zero(c);
 #pragma unroll
           for (int step = 0; step < 2; ++step) {
-            x[step] = ld16(pv + 16 * step);
-            const int valid = end - 16 * step - 8 * half;
             u32x4 y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              x[step][e] &= (uint32_t)((1ull << (16 * min(max(valid - 2 * e, 0), 2))) - 1);
-              const uint32_t b = not_finite16(x[step][e]);
-              odd |= b;
-              y[e] = x[step][e] & ~((b >> 15) * 0xffffu);
-            }
-            z = mfma32x32x16(y, ph[step], z);
-            z = mfma32x32x16(y, pl[step], z);
-          }
-          if (!again && __any(odd != 0)) {
-            // how many infinities, negative infinities and NaN of each dimension a row sees: 1, 2^8 and 2^16 for each
-            // against a one for each slot that it sees
-            f32x16 c;
-            zero(c);
+              uint32_t k = 0;
+              y[e] = 0;
 #pragma unroll
-            for (int step = 0; step < 2; ++step) {
-              u32x4 y;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                uint32_t k = 0;
-                y[e] = 0;
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  const uint32_t v = x[step][e] >> (16 * b) & 0xffff;
-                  k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
-                  y[e] |= (mask >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
-                }
-                x[step][e] = k;
+              for (int b = 0; b < 2; ++b) {
+                const uint32_t v = x[step][e] >> (16 * b) & 0xffff;
+                k |= (v == 0x7f80 ? 0x3f80u : v == 0xff80 ? 0x4380u : (v & 0x7fff) > 0x7f80 ? 0x4780u : 0u) << (16 * b);
+                y[e] |= (mask >> (16 * step + 2 * e + b) & 1 ? 0x3f80u : 0u) << (16 * b);
               }
-              c = mfma32x32x16(x[step], y, c);
+              x[step][e] = k;
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int k = (int)c[i];
-              seen |= (uint64_t)((k & 0xff ? 1 : 0) | (k & 0xff00 ? 2 : 0) | (k >> 16 ? 4 : 0)) << (3 * i);
-            }
+            c = mfma32x32x16(x[step], y, c);
           }
-        }
-        int at = lane;
-        asm volatile("" : "+v"(at));
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          f32x4* const to = &sums[(wave * Q + dt * 4 + g) * 64 + at];
-          f32x4 v = again ? *to : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * g + e, k = (int)(seen >> (3 * i)) & 7;
-            if (again)
-              v[e] = open >> i & 1 ? z[i] * (f * (1.f / kLow)) : v[e];
-            else if (k)                             // (f is NaN where a score is)
-              v[e] = (k == 1 ? INFINITY : k == 2 ? -INFINITY : NAN) + 0.f * f;
-            else
-              v[e] = z[i] * f, open |= finite(z[i]) ? 0 : 1u << i;
+          for (int i = 0; i < 16; ++i) {
+            const int k = (int)c[i];
+            seen |= (uint64_t)((k & 0xff ? 1 : 0) | (k & 0xff00 ? 2 : 0) | (k >> 16 ? 4 : 0)) << (3 * i);
           }
-          *to = v;
         }
       }
-    }
-  } else {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      o[dt] *= f;
+      for (int g = 0; g < 4; ++g) {
+        f32x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        sums[(wave * Q + dt * 4 + i) * 64 + lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * g + e, k = (int)(seen >> (3 * i)) & 7;
+          v[e] = k             ? (k == 1 ? INFINITY : k == 2 ? -INFINITY : NAN) + 0.f * f   // (f is NaN where a score is)
+                 : finite(z[i]) ? z[i] * f
+                                : low[i] * (f * (1.f / kLow));
+        }
+        sums[(wave * Q + dt * 4 + g) * 64 + lane] = v;
+      }
     }
   }
   __syncthreads();
