@@ -87,6 +87,49 @@ def test_values_not_finite_in_one_dimension_leave_the_others(torch, nq, nkv, D, 
     a.check()
 
 
+def _small_bounds(out, absum, big, D, slots):
+    """How far out may be off where values are small.  Relative to the sum of p |v| as in attention_bounds.  At the
+    lower end of the range: a weight under 2^-126 of the largest is lost, 2^-126 of the values' size, which absum's
+    2^-24 holds many times over; every product, sum and factor in 32 bits is off by 2^-150 at most, of which there are two
+    products with two sums a slot, and 8 + 256 groups' shares of three operations, the sums in units of at least the result's;
+    then out is rounded to bf16, half a step, 2^-134 at least."""
+    e = 2 * (D + 4) * 2.0 ** -24 * big
+    rel = 2 * e + 2.0 ** -22 + 2.0 ** -16 + 2 * (slots + 64) * 2.0 ** -24
+    return np.maximum(2.0 ** -8 * np.abs(out), 2.0 ** -134) + 1.01 * rel * absum + (4 * slots + 3 * 264) * 2.0 ** -150
+
+
+@pytest.mark.parametrize("nq,nkv,D", SHAPES)
+@pytest.mark.parametrize("length", [150, 3000])
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -118, 2.0 ** -125])
+@pytest.mark.parametrize("infinite", [False, True])
+def test_small_values(torch, nq, nkv, D, length, size, infinite):  # noqa: F811
+    """Values down to the smallest normal ones, in bounds that outputs of zero do not pass; beside infinite ones too."""
+    rng = np.random.default_rng(34)
+    p = ref.Pass([length], [7], [BRANCHES])
+    a = Attn(torch, rng, p, nq, nkv, D)
+    fine = np.isfinite(ref.bf16_value(a.v))
+    a.v[fine] = ref.bf16(size * np.where(rng.random(a.v.shape) < 0.95, 1, 0.5))[fine]
+    if infinite:
+        a.v[1, a.table[0, 0], :, ::8, 7] = 0x7F80
+        a.v[1, a.table[0, (length + 2) // PAGE], :, 1::2, (length + 2) % PAGE] = 0xFF80
+    out, _ = _again(a)
+    for j in range(7):
+        s = np.array(a.slots(0, j), int)
+        pg, off = a.table[0, s // PAGE], s % PAGE
+        for h in range(nq):
+            k = ref.bf16_value(a.k[1, pg, h // (nq // nkv), off])
+            v = ref.bf16_value(a.v[1, pg, h // (nq // nkv), :, off])
+            w, _, absum, big = ref.attention(ref.bf16_value(a.q[j, h * D:(h + 1) * D]), k, v, a.scale)
+            fin = np.isfinite(w)
+            assert infinite or fin.all()
+            tol = _small_bounds(w[fin], absum[fin], big, D, len(s))
+            assert (tol < np.abs(w[fin]) / 8).all()
+            have = ref.bf16_value(out[j, h * D:(h + 1) * D])
+            np.testing.assert_array_equal(have[~fin], w[~fin])
+            off_by = np.abs(have[fin] - w[fin])
+            assert (off_by <= tol).all(), (j, h, float((off_by / tol).max()))
+
+
 @pytest.mark.parametrize("nq,nkv", [(256, 256), (10240, 256)])
 def test_large_values_of_many_slots_of_one_wave(torch, nq, nkv):  # noqa: F811
     """A wave's own sum: 12 thousand slots (24 thousand where two waves share a half) of the largest values, whose
