@@ -154,3 +154,42 @@ def test_large_values_of_many_slots_of_one_wave(torch, nq, nkv):  # noqa: F811
     # (a wave's sum of a row's terms and the sum of waves, an exponential, a logarithm)
     assert np.abs(lse - want).max() <= (p.lens[0] / 4 + 64) * 2.0 ** -24 + 2.0 ** -21 * (1 + want)
     assert int(a.rows.err) == 0
+
+
+class Chains(ref.Pass):
+    """Long chains, whose rows need no walk."""
+
+    def line(self, b, j):
+        return list(range(j + 1))
+
+
+# heads of a workgroup, 2, 5, 8 and 4 of them, and its last share of the heads, 1, 1, 7 and 3: of passes with enough tiles of
+# slots times rotated heads for several, which stream their outputs
+@pytest.mark.parametrize("nq,nkv,D,lens,counts,given", [
+    (28, 3, 128, [37, 0, 100], [4000, 1, 2002], True), (41, 5, 64, [130, 63], [5000, 3300], False),
+    (60, 3, 64, [1, 64, 7, 500], [64, 8000, 100, 136], True), (12, 3, 128, [0], [20000], False)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_of_many_heads_of_many_rows(torch, nq, nkv, D, lens, counts, given, in_place):  # noqa: F811
+    rng = np.random.default_rng(sum(lens) + nq)
+    p = Chains(lens, counts, None, 5)
+    table, pages = ref.table_of(p, rng)
+    pos = rng.integers(0, 5000, (3, p.rows)) if given else None
+    section = (D // 8, 3 * D // 16, D // 2 - D // 8 - 3 * D // 16)
+    got = _append(torch, rng, p, table, pages, nq, nkv, D, section, pos=pos, pad=8, in_place=in_place)
+    assert got["err"] == 0
+    _check_append(p, table, pages, nq, nkv, D, section, 0, 10000.0, pos, 1, got, in_place)
+
+
+@pytest.mark.parametrize("nq,nkv,D", [(31, 4, 128), (28, 4, 128), (62, 4, 64)])
+@pytest.mark.parametrize("count", [1, 2])
+def test_append_of_many_sequences_of_few_rows(torch, nq, nkv, D, count):  # noqa: F811
+    """79 to 160 sequences: a workgroup has several heads here too."""
+    rng = np.random.default_rng(nq + count)
+    batch = 160 // count
+    counts = [count] * (batch - 1) + [0] * (nq == 31)
+    lens = [int(x) for x in rng.integers(0, 200, len(counts))]
+    p = ref.Pass(lens, counts, _trees(rng, counts), 160 - sum(counts))
+    table, pages = ref.table_of(p, rng)
+    got = _append(torch, rng, p, table, pages, nq, nkv, D, (D // 2, 0, 0))
+    assert got["err"] == 0
+    _check_append(p, table, pages, nq, nkv, D, (D // 2, 0, 0), 0, 10000.0, None, 1, got)
