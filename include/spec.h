@@ -503,9 +503,10 @@ typedef struct spec_kv {
  * every output.
  * What the host cannot see is checked on the device, which sets *d_err to SPEC_E_INVAL
  * (else leaves it alone) and goes on in bounds: if d_first decreases or leaves [0, rows], no
- * sequence has rows; one whose d_len is negative or more than its table's slots has none; a
- * parent that is not an earlier row of the sequence counts as -1; slots past the table, and
- * pages outside the pool, are not written, not moved and not visible.
+ * sequence has rows; one whose d_len is negative or more than its table's slots has none (one
+ * without rows anyway may have any d_len and is not reported); a parent that is not an earlier
+ * row of the sequence counts as -1; slots past the table, and pages outside the pool, are not
+ * written, not moved and not visible.
  * No page may belong to two sequences where one of them writes it. */
 typedef struct spec_rows {
   int32_t batch;             /* 1..SPEC_MAX_ROWS */

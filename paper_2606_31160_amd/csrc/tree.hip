@@ -366,7 +366,7 @@ __device__ bool work_of(const TreeAttnArgs& a, int i, Work& w) {
     const int first = shared_at(t.first, 0), end = shared_at(t.first, 1), len = shared_at(t.len, 0);
     const bool bad = first < 0 || end < first || end > t.rows, off = len < 0 || len > t.stride * SPEC_KV_PAGE;
     const int n = bad || off ? 0 : end - first;
-    if (one && (bad || (off && end > first) || len + n > t.stride * SPEC_KV_PAGE)) flag(t);
+    if (one && (bad || (end > first && (off || len + n > t.stride * SPEC_KV_PAGE)))) flag(t);
     const int nc = (n * a.G + C - 1) / C, units = nc * t.nkv;
     const int pages = min((len + n + SPEC_KV_PAGE - 1) / SPEC_KV_PAGE, t.stride);
     if (one) a.units[0].first = units;

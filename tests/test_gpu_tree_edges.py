@@ -156,6 +156,36 @@ def test_large_values_of_many_slots_of_one_wave(torch, nq, nkv):  # noqa: F811
     assert int(a.rows.err) == 0
 
 
+@pytest.mark.parametrize("batch", [1, 2, 70])
+def test_lengths_of_sequences_without_rows_are_not_reported(torch, batch):  # noqa: F811
+    rng = np.random.default_rng(36)
+    for stale in (2 * PAGE + 1, 10 ** 9, -1, 2 ** 31 - 1):
+        counts = [0] * batch
+        if batch > 1:
+            counts[0] = 2
+        p = ref.Pass([5] * batch, counts, _trees(rng, counts), 1, stride=2)
+        table, pages = ref.table_of(p, rng)
+        lens = [5] * (batch - 1) + [stale]
+        got = _append(torch, rng, p, table, pages, 2, 1, 64, (32, 0, 0), rows=Rows(torch, p, table, lens=lens))
+        _check_append(p, table, pages, 2, 1, 64, (32, 0, 0), 0, 1e4, None, 1, got)
+        assert got["err"] == 0
+        a = Attn(torch, rng, p, 4, 2, 64, table=table, pages=pages, rows=Rows(torch, p, table, lens=lens))
+        a.check()
+        assert int(a.rows.err) == 0
+        tokens = [0] * p.rows
+        got = _commit(torch, rng, p, tokens, tokens, table=table, pages=pages, rows=Rows(torch, p, table, lens=lens))
+        assert got["err"] == 0 and got["n"][-1] == 0 and got["new"][-1] == stale
+    # with rows they are
+    if batch > 1:
+        counts[-1] = 1
+    else:
+        counts = [1]
+    p = ref.Pass([5] * batch, counts, _trees(rng, counts), 1, stride=2)
+    a = Attn(torch, rng, p, 4, 2, 64, rows=Rows(torch, p, ref.table_of(p, rng)[0], lens=[5] * (batch - 1) + [2 * PAGE + 1]))
+    a.run()
+    assert int(a.rows.err) == 1
+
+
 class Chains(ref.Pass):
     """Long chains, whose rows need no walk."""
 
