@@ -1254,9 +1254,10 @@ TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stri
   // 128, at least 2, 3 and 4 pages: 4 rows over 450, 1000, 4000 slots 11.1, 11.1, 11.8; 11.4, 11.3, 11.9; 13.4, 13.5, 12.6; 40 rows
   // over 1000 and 2000 14.1, 13.7, 14.3; 15.9, 15.6, 14.5.  One group up to 8 pages and up to 6: 40 rows over 300 10.8 and 12.0, 4 rows
   // over 380 9.2 and 10.7; up to 24: 5 rows over 700 and 960 13.7 and 16.1, several 12.2 and 12.4.
+  // (a group of so many that the reciprocal's rounding leaves no second one, which nothing would join)
   const int least = 3, whole = 8;
-  p.least = stride <= whole ? whole : least;
-  p.combine = stride > p.least;
+  p.combine = stride > whole;
+  p.least = p.combine ? least : 1 << 30;
   p.likely = std::min(stride / p.least, p.target / std::max(p.units, 1));
   const size_t part = (size_t)p.target * chunk * D * 4, ml = (size_t)p.target * chunk * 8,
                units = (size_t)(1 + p.units) * sizeof(TreeUnit);

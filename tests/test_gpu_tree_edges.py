@@ -186,6 +186,21 @@ def test_lengths_of_sequences_without_rows_are_not_reported(torch, batch):  # no
     assert int(a.rows.err) == 1
 
 
+@pytest.mark.parametrize("nq,nkv,D", SHAPES)
+@pytest.mark.parametrize("stride", [8, 9])
+@pytest.mark.parametrize("slots", [448, 449, 511, 512, 513, 575])
+def test_attention_at_the_width_of_a_table_of_one_group(torch, nq, nkv, D, stride, slots):  # noqa: F811
+    """Tables of up to eight pages make one group, whose result no second kernel joins."""
+    if slots > stride * PAGE:
+        slots = stride * PAGE - 1
+    rng = np.random.default_rng(37)
+    for lens, counts in (([slots - 1], [1]), ([slots - 9], [9]), ([slots - 3, slots - 1, 5, slots - 20], [3, 1, 0, 20])):
+        p = ref.Pass(lens, counts, _trees(rng, counts), 1, stride=stride)
+        a = Attn(torch, rng, p, nq, nkv, D)
+        a.check()
+        assert int(a.rows.err) == 0
+
+
 class Chains(ref.Pass):
     """Long chains, whose rows need no walk."""
 
