@@ -468,15 +468,16 @@ __device__ __forceinline__ float other_half(float x) {   // of lane ^ 32
 
 // 4 KB of a page, from byte `step` on, to `lds`: lane l's 16 bytes of the i-th KB to 1024 i + 16 l, from an offset o0 .. o3 of its
 // own in that KB.  Written out, as the compiler would wait for all such loads before every LDS read; a load
-// has no register to write.  (An instruction's offset counts at both ends.)  `once`: nobody else reads the page.
+// has no register to write.  (An instruction's offset counts at both ends.)  The first load is five wait states into the block:
+// so long after a vector instruction, a lane's read for instance, has written `page` or `step`.  `once`: nobody else reads the page.
 #define SD_PAGE_TO_LDS(hint)                                                  \
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"                             \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\t"                             \
                "buffer_load_dwordx4 %3, %1, %2 offen " hint "lds\n\t"         \
                "buffer_load_dwordx4 %4, %1, %2 offen offset:1024 " hint "lds\n\t" \
                "buffer_load_dwordx4 %5, %1, %2 offen offset:2048 " hint "lds\n\t" \
                "buffer_load_dwordx4 %6, %1, %2 offen offset:3*1024 " hint "lds" ::"s"(lds), \
                "s"(page), "s"(step), "v"(o0), "v"(o1), "v"(o2), "v"(o3)       \
-               : "memory")
+               : "m0", "memory")
 __device__ __forceinline__ void page_to_lds(bool once, __amdgpu_buffer_rsrc_t page, uint32_t lds, uint32_t step, uint32_t o0, uint32_t o1,
                                             uint32_t o2, uint32_t o3) {
   if (once)
