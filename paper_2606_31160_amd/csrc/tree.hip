@@ -90,7 +90,7 @@ __device__ __forceinline__ T total(T x) {
 //   Values: rows through LDS, columns out, 8 slots of a dimension in one store; the ends of a sequence's slots
 // one by one.
 // Bound by memory: 4096 rows of 32 + 2 x 8 heads of 128, 100 MB, 22.1 us a call in graphs (4.6 TB/s; a copy of 4 GiB
-// reaches 4.7), 29.1 with outputs left to the caches; 20 thousand rows of 28 + 2 x 4 heads 86.1 and 88.8.  One
+// reaches 4.78), 29.1 with outputs left to the caches; 20 thousand rows of 28 + 2 x 4 heads 86.1 and 88.8.  One
 // head a workgroup, which forms every angle anew: 33.6 and 121.
 // ---------------------------------------------------------------------------
 
@@ -125,7 +125,7 @@ __device__ bool tile_of(const TreeRows& t, int x, bool one, Seq& s, int& b, int&
   return false;
 }
 
-// A long pass streams its outputs past the caches, which its inputs then keep.
+// A pass of several heads a workgroup streams its outputs past the caches, which its inputs then keep.
 template <bool STREAM>
 __device__ __forceinline__ void store16(bf16_t* to, u32x4 x) {
   if (STREAM)
@@ -454,7 +454,9 @@ __device__ __forceinline__ uint32_t not_finite16(uint32_t w) {
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
-// (hi, lo) bf16 pairs whose sums are x and y within 2^-16.
+// (hi, lo) bf16 pairs whose sums are x and y within 2^-16.  A matrix operand holds eight bits of p; one alone would be off as much
+// as the result's own rounding to bf16, two are far below it, and three would take a third more products in all.  Sums of p are of
+// p as it is.
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
   hi = pack2(x, y);
   asm("" : "+v"(hi));                               // (else the compiler rounds x a second time on its own)
@@ -1203,7 +1205,8 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
 hipError_t launch_kv_append(AppendArgs& a, int D, hipStream_t s) {
   // a tile at least for every sequence and 64 rows; at most two ends more for every sequence
   const int64_t tiles = (int64_t)a.t.rows / SPEC_KV_PAGE + 2 * std::min(a.t.B, a.t.rows), rotated = a.nq + a.t.nkv;
-  // (more heads share their angles, but leave fewer workgroups: 2 heads here 29.1 us for the 4096 rows, 4 34.3, 8 45.4; for the
+  // Heads of a workgroup, from the tiles that there may be at most: long passes have several, and so have passes of one row of 32
+  // sequences and more.  (More heads share their angles, but leave fewer workgroups: 2 heads here 29.1 us for the 4096 rows, 4 34.3, 8 45.4; for the
   // 20 thousand 8 heads 88.9, 4 94.2, 1 121)
   a.heads = (int)std::min<int64_t>(8, std::max<int64_t>(1, tiles * rotated / 1024));
   const dim3 grid((unsigned)tiles, (unsigned)((rotated + a.heads - 1) / a.heads + a.t.nkv));
@@ -1243,7 +1246,7 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
 
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
-  // Two tiles of an average sequence share a workgroup's pages: 144 rows of 16 scenes 59.5 -> 50 us a call, 25 rows over 131
+  // Two tiles of an average sequence (the host knows no other; those without rows count too) share a workgroup's pages: 144 rows of 16 scenes 59.5 -> 50 us a call, 25 rows over 131
   // thousand slots 38.6 -> 34.2, 64 rows of the paper's heads over 4117 20.4 -> 18.3.
   p.tiles = (int64_t)((rows + batch - 1) / batch) * G > kTileRows ? 2 : 1;
   const int64_t chunk = kTileRows * p.tiles;
@@ -1251,7 +1254,8 @@ TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stri
   p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G));
   p.target = ncu;
   p.grid = std::max(p.target, p.units);
-  // Pages of a group at least; short tables make one group, which needs no second kernel.  Us in graphs, 28 + 2 x 4 heads of
+  // Pages of a group at least; short tables make one group, which needs no second kernel.  (The table's width bounds the lengths, which
+  // only the device knows: short sequences in a wide table take several groups and the second kernel.)  Us in graphs, 28 + 2 x 4 heads of
   // 128, at least 2, 3 and 4 pages: 4 rows over 450, 1000, 4000 slots 11.1, 11.1, 11.8; 11.4, 11.3, 11.9; 13.4, 13.5, 12.6; 40 rows
   // over 1000 and 2000 14.1, 13.7, 14.3; 15.9, 15.6, 14.5.  One group up to 8 pages and up to 6: 40 rows over 300 10.8 and 12.0, 4 rows
   // over 380 9.2 and 10.7; up to 24: 5 rows over 700 and 960 13.7 and 16.1, several 12.2 and 12.4.
