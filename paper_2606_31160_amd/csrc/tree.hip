@@ -470,8 +470,9 @@ __device__ __forceinline__ float other_half(float x) {   // of lane ^ 32
 
 // 4 KB of a page, from byte `step` on, to `lds`: lane l's 16 bytes of the i-th KB to 1024 i + 16 l, from an offset o0 .. o3 of its
 // own in that KB.  Written out, as the compiler would wait for all such loads before every LDS read; a load
-// has no register to write.  (An instruction's offset counts at both ends.)  The first load is five wait states into the block:
-// so long after a vector instruction, a lane's read for instance, has written `page` or `step`.  `once`: nobody else reads the page.
+// has no register to write.  (An instruction's offset counts at both ends.)  The first load is five wait states into the
+// block, as a vector instruction (a lane's read for instance) may have written `page` or `step` right before it.  `once`: nobody
+// else reads the page.
 #define SD_PAGE_TO_LDS(hint)                                                  \
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\t"                             \
                "buffer_load_dwordx4 %3, %1, %2 offen " hint "lds\n\t"         \
@@ -1205,9 +1206,9 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
 hipError_t launch_kv_append(AppendArgs& a, int D, hipStream_t s) {
   // a tile at least for every sequence and 64 rows; at most two ends more for every sequence
   const int64_t tiles = (int64_t)a.t.rows / SPEC_KV_PAGE + 2 * std::min(a.t.B, a.t.rows), rotated = a.nq + a.t.nkv;
-  // Heads of a workgroup, from the tiles that there may be at most: long passes have several, and so have passes of one row of 32
-  // sequences and more.  (More heads share their angles, but leave fewer workgroups: 2 heads here 29.1 us for the 4096 rows, 4 34.3, 8 45.4; for the
-  // 20 thousand 8 heads 88.9, 4 94.2, 1 121)
+  // Heads of a workgroup, from the tiles that there may be at most: long passes have several, and so have passes of one row of many
+  // sequences (32 of them with 32 rotated heads).  More heads share their angles, but leave fewer workgroups: 2 heads here 29.1 us
+  // for the 4096 rows, 4 34.3, 8 45.4; for the 20 thousand 8 heads 88.9, 4 94.2, 1 121.
   a.heads = (int)std::min<int64_t>(8, std::max<int64_t>(1, tiles * rotated / 1024));
   const dim3 grid((unsigned)tiles, (unsigned)((rotated + a.heads - 1) / a.heads + a.t.nkv));
   if (D == 128)
@@ -1246,19 +1247,21 @@ hipError_t attn(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t s) {
 
 TreeAttnPlan tree_attn_plan(int batch, int rows, int nkv, int G, int D, int stride, int ncu) {
   TreeAttnPlan p;
-  // Two tiles of an average sequence (the host knows no other; those without rows count too) share a workgroup's pages: 144 rows of 16 scenes 59.5 -> 50 us a call, 25 rows over 131
-  // thousand slots 38.6 -> 34.2, 64 rows of the paper's heads over 4117 20.4 -> 18.3.
+  // Two tiles of an average sequence (the host knows no other; those without rows count too) share a workgroup's pages: 144
+  // rows of 16 scenes 59.5 -> 50 us a call, 25 rows over 131 thousand slots 38.6 -> 34.2, 64 rows of the paper's heads over 4117
+  // 20.4 -> 18.3.
   p.tiles = (int64_t)((rows + batch - 1) / batch) * G > kTileRows ? 2 : 1;
   const int64_t chunk = kTileRows * p.tiles;
   // (every sequence may end inside a chunk)
   p.units = (int)(nkv * std::min<int64_t>(((int64_t)rows * G + chunk - 1) / chunk + batch, (int64_t)rows * G));
   p.target = ncu;
   p.grid = std::max(p.target, p.units);
-  // Pages of a group at least; short tables make one group, which needs no second kernel.  (The table's width bounds the lengths, which
-  // only the device knows: short sequences in a wide table take several groups and the second kernel.)  Us in graphs, 28 + 2 x 4 heads of
-  // 128, at least 2, 3 and 4 pages: 4 rows over 450, 1000, 4000 slots 11.1, 11.1, 11.8; 11.4, 11.3, 11.9; 13.4, 13.5, 12.6; 40 rows
-  // over 1000 and 2000 14.1, 13.7, 14.3; 15.9, 15.6, 14.5.  One group up to 8 pages and up to 6: 40 rows over 300 10.8 and 12.0, 4 rows
-  // over 380 9.2 and 10.7; up to 24: 5 rows over 700 and 960 13.7 and 16.1, several 12.2 and 12.4.
+  // Pages of a group at least; short tables make one group, which needs no second kernel.  (The table's width bounds the
+  // lengths, which only the device knows: short sequences in a wide table take several groups and the second kernel.)  Us in
+  // graphs, 28 + 2 x 4 heads of 128, at least 2, 3 and 4 pages: 4 rows over 450, 1000, 4000 slots 11.1, 11.1, 11.8; 11.4, 11.3,
+  // 11.9; 13.4, 13.5, 12.6; 40 rows over 1000 and 2000 14.1, 13.7, 14.3; 15.9, 15.6, 14.5.  One group up to 8 pages and up to 6:
+  // 40 rows over 300 10.8 and 12.0, 4 rows over 380 9.2 and 10.7; up to 24: 5 rows over 700 and 960 13.7 and 16.1, several 12.2
+  // and 12.4.
   // (a group of so many that the reciprocal's rounding leaves no second one, which nothing would join)
   const int least = 3, whole = 8;
   p.combine = stride > whole;
